@@ -433,6 +433,120 @@ size_t cham_conv3x3_workspace_bytes(int64_t B, int64_t H, int64_t W, int64_t C, 
 int cham_linear_plan(int64_t M, int64_t N, int64_t K, int32_t code_bits, int32_t* out, int32_t out_len);
 
 /* ---------------------------------------------------------------------------------------
+ * 5. operators around 8-bit linear layers
+ *
+ * What a transformer block runs between its matrix products when those read 8-bit codes: the
+ * residual's addition with the root-mean-square norm, and the activation function between two
+ * feed-forward products, each ending in codes and scales in one pass; and a product whose
+ * scales follow blocks of 128.  The two passes write either the block format below, which
+ * cham_block_linear reads, or one of the activation formats of section 3 with one scale per
+ * token, which cham_mixed_linear reads.  Rows may be strided; element types are CHAM_T_*.
+ * Row starts must be 16-byte aligned (base pointers and row strides), K % 32 == 0.  M = 0 is
+ * an empty call: nothing launched, CHAM_OK (its row pointers may be NULL).
+ * ------------------------------------------------------------------------------------- */
+#define CHAM_T_F32 0
+#define CHAM_T_F16 1
+#define CHAM_T_BF16 2
+#define CHAM_T_N 3
+
+/* The block format: E4M3 codes with one scale per row and 128 consecutive elements (the last
+ * block of a row holds K mod 128 if 128 does not divide K):
+ *   s = amax / 448, floored at FLT_MIN, or (pow2) the next power of two at or above that
+ *   c = E4M3(clamp(y fl(1/s), +-448)), round to nearest even
+ * A block that holds a NaN or an infinity has the scale NaN (byte 255), so everything computed
+ * from it is NaN; its codes are unspecified. */
+typedef struct cham_bq {
+    int64_t M, K;      /* codes of [M][K]                                                    */
+    int32_t pow2;      /* 0: binary32 scales; 1: powers of two, held as E8M0 bytes (E + 127)  */
+    uint8_t* codes;    /* [M][K] E4M3, 16-byte aligned                                       */
+    void* scale;       /* [ceil(K / 128)][M], block-major: the scales of one block of all rows
+                          are consecutive (float, or uint8_t if pow2)                         */
+} cham_bq;
+
+/* Weights in the block format: one scale for each 128 x 128 block (ragged at both ends). */
+typedef struct cham_bw {
+    int64_t N, K;      /* codes of [N][K]                                                    */
+    int32_t pow2;      /* as in cham_bq                                                       */
+    uint8_t* codes;    /* [N][K] E4M3, 16-byte aligned                                       */
+    void* scale;       /* [ceil(N / 128)][ceil(K / 128)] (float, or uint8_t if pow2)          */
+} cham_bw;
+
+/* h = x + r (binary32), y = h / sqrt(mean(h^2) + eps) * g: the norm sees the unrounded sum; h is
+ * written rounded to its own type.  The mean is taken over the row in binary32 (rows whose sum
+ * of squares overflows binary32 come out as zeros). */
+typedef struct cham_norm {
+    int64_t M, K;      /* K <= 32768                                                         */
+    const void* x;     /* [M][K], row stride ldx elements                                    */
+    int64_t ldx;
+    const void* r;     /* the residual [M][K], row stride ldr; NULL = none                   */
+    int64_t ldr;
+    void* h;           /* [M][K], row stride ldh, of r's type; may be r itself (same stride);
+                          NULL = not written                                                  */
+    int64_t ldh;
+    const void* g;     /* [K] weights, 16-byte aligned; NULL = ones                          */
+    int32_t x_type;
+    int32_t r_type;    /* type of r and h: x_type or CHAM_T_F32                              */
+    int32_t g_type;
+    float eps;         /* >= 0 (a row of zeros with eps = 0 is NaN)                          */
+} cham_norm;
+
+/* The norm of n, written in the block format (out->M, K equal n's).
+ * Errors: CHAM_EINVAL (NULL, sizes, strides, alignment, eps), CHAM_EFORMAT (types),
+ * CHAM_ESHAPE (K % 32, K > 32768, M >= 2^31), CHAM_EHIP. */
+int cham_rms_norm_quantize_block(const cham_norm* n, cham_bq* out, void* stream);
+
+/* The norm of n, written in activation format fmt of section 3 with dynamic scales of each
+ * token: out->nsamples must be M (scale [M], zero [M]; e8m0 [M][K/32] for MX formats), codes
+ * 8-byte aligned.  A row that holds a NaN or an infinity takes the scale NaN (MX formats take
+ * finite rows only).  Errors: as above, CHAM_EFORMAT also for fmt. */
+int cham_rms_norm_quantize(const cham_norm* n, int32_t fmt, cham_aq* out, void* stream);
+
+/* Activation functions */
+#define CHAM_ACT_NONE 0       /* x                                                            */
+#define CHAM_ACT_SILU 1       /* x / (1 + exp(-x))                                            */
+#define CHAM_ACT_GELU 2       /* x Phi(x), Phi the normal distribution function               */
+#define CHAM_ACT_GELU_TANH 3  /* x / (1 + exp(-2 sqrt(2/pi) (x + 0.044715 x^3))): GELU's tanh
+                                 form, 0.5 x (1 + tanh(...)), written without cancellation    */
+#define CHAM_ACT_N 4
+
+/* y = f(x) u (u = NULL: y = f(x)); x and u may be the two halves of one matrix.  With
+ * CHAM_ACT_NONE and no u this is the quantizer alone. */
+typedef struct cham_gate {
+    int64_t M, K;      /* K <= 32768 for the per-token formats                               */
+    const void* x;     /* [M][K], row stride ldx elements                                    */
+    int64_t ldx;
+    const void* u;     /* [M][K], row stride ldu; NULL = none                                */
+    int64_t ldu;
+    int32_t type;      /* of x and u                                                          */
+    int32_t act;       /* CHAM_ACT_*                                                          */
+} cham_gate;
+
+/* The gate of a, written in the block format (out->M, K equal a's), or in an activation
+ * format with one scale per token (as cham_rms_norm_quantize).  Errors: CHAM_EINVAL,
+ * CHAM_EFORMAT (types, act, fmt), CHAM_ESHAPE, CHAM_EHIP. */
+int cham_gated_quantize_block(const cham_gate* a, cham_bq* out, void* stream);
+int cham_gated_quantize(const cham_gate* a, int32_t fmt, cham_aq* out, void* stream);
+
+/* Weights W [N][K] (row stride ldw elements) brought to the block format: out->N, K and pow2
+ * are given.  N >= 1.  Errors: CHAM_EINVAL, CHAM_EFORMAT, CHAM_ESHAPE, CHAM_EHIP. */
+int cham_block_quantize_weights(const void* W, int32_t type, int64_t ldw, cham_bw* out, void* stream);
+
+/* Y[m][n] = sum over blocks b of xs[b][m] ws[n / 128][b] sum_{k in b} xc[m][k] wc[n][k], the
+ * inner sums and their total in binary32, rounded once to y_type.  Y [M][N], row stride ldy
+ * elements (any; any N).  x->pow2 must equal w->pow2.  Products and partial sums are added in a fixed order (no atomics on values): Y is bitwise reproducible run to run.
+ * The product of an activation's and a weight's scale must not overflow binary32.  Limits:
+ * K <= 2^20, M and N < 2^31.  No workspace.  Errors: CHAM_EINVAL, CHAM_EFORMAT (y_type), CHAM_ESHAPE,
+ * CHAM_EHIP. */
+int cham_block_linear(const cham_bq* x, const cham_bw* w, void* Y, int32_t y_type, int64_t ldy,
+                      void* stream);
+
+/* The launch plan cham_block_linear takes for M x N x K (diagnostics; host only): out (host,
+ * out_len >= 3) receives {tile rows, tile channels, wavefront groups that split k inside a
+ * workgroup}; tiles of 16 x 16 are the few-row kernel's.  Depends on the current device's CU
+ * count (256 when no device is visible).  Errors: CHAM_EINVAL, CHAM_EFORMAT, CHAM_ESHAPE. */
+int cham_block_linear_plan(int64_t M, int64_t N, int64_t K, int32_t y_type, int32_t* out, int32_t out_len);
+
+/* ---------------------------------------------------------------------------------------
  * workspace sizes
  * ------------------------------------------------------------------------------------- */
 #define CHAM_OP_SELECT 0

@@ -72,6 +72,25 @@ class _AQ(ctypes.Structure):
                 ("codes", _P), ("e8m0", _P), ("scale", _P), ("zero", _P)]
 
 
+class _BQ(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("K", ctypes.c_int64), ("pow2", ctypes.c_int32), ("codes", _P), ("scale", _P)]
+
+
+class _BW(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("K", ctypes.c_int64), ("pow2", ctypes.c_int32), ("codes", _P), ("scale", _P)]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("K", ctypes.c_int64), ("x", _P), ("ldx", ctypes.c_int64), ("r", _P),
+                ("ldr", ctypes.c_int64), ("h", _P), ("ldh", ctypes.c_int64), ("g", _P), ("x_type", ctypes.c_int32),
+                ("r_type", ctypes.c_int32), ("g_type", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class _Gate(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("K", ctypes.c_int64), ("x", _P), ("ldx", ctypes.c_int64), ("u", _P),
+                ("ldu", ctypes.c_int64), ("type", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -122,6 +141,13 @@ def lib():
     L.cham_packed_bytes.argtypes = [i64, i64]
     L.cham_packed_bytes.restype = sz
     L.cham_linear_plan.argtypes = [i64, i64, i64, i32, ctypes.POINTER(ctypes.c_int32), i32]
+    L.cham_rms_norm_quantize_block.argtypes = [ctypes.POINTER(_Norm), ctypes.POINTER(_BQ), _P]
+    L.cham_rms_norm_quantize.argtypes = [ctypes.POINTER(_Norm), i32, ctypes.POINTER(_AQ), _P]
+    L.cham_gated_quantize_block.argtypes = [ctypes.POINTER(_Gate), ctypes.POINTER(_BQ), _P]
+    L.cham_gated_quantize.argtypes = [ctypes.POINTER(_Gate), i32, ctypes.POINTER(_AQ), _P]
+    L.cham_block_quantize_weights.argtypes = [_P, i32, i64, ctypes.POINTER(_BW), _P]
+    L.cham_block_linear.argtypes = [ctypes.POINTER(_BQ), ctypes.POINTER(_BW), _P, i32, i64, _P]
+    L.cham_block_linear_plan.argtypes = [i64, i64, i64, i32, ctypes.POINTER(i32), i32]
     for name in ("cham_select_weight_formats", "cham_select_weight_formats_batch", "cham_pack_weights_batch",
                  "cham_act_stats_reset", "cham_act_stats_accumulate",
                  "cham_act_stats_accumulate_batch",
@@ -129,7 +155,9 @@ def lib():
                  "cham_quantize_act_lut_accumulate_batch",
                  "cham_mixed_linear", "cham_mixed_linear_grouped", "cham_select_group_formats", "cham_conv3x3_mixed",
                  "cham_act_colsq_accumulate",
-                 "cham_linear_plan"):
+                 "cham_linear_plan", "cham_rms_norm_quantize_block", "cham_rms_norm_quantize",
+                 "cham_gated_quantize_block", "cham_gated_quantize", "cham_block_quantize_weights",
+                 "cham_block_linear", "cham_block_linear_plan"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -666,3 +694,251 @@ def conv3x3_mixed(xq: AQ, B: int, H: int, W: int, wq: WQ, Y: Optional[torch.Tens
                                     _stream(stream)), "conv3x3_mixed")
     return Y
 
+
+
+# -------------------------------------------------------------------------------------------
+# operators around 8-bit linear layers
+# -------------------------------------------------------------------------------------------
+BLOCK = 128
+#: format of an operator's output besides the activation formats A_*: E4M3 codes with one scale
+#: per row and 128 elements (a BQ, which block_linear reads)
+A_BLOCK128 = 16
+ACT_NONE, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(4)
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+@dataclass
+class BQ:
+    """Activations in the block format (device tensors, see cham_bq).  scale: float32, or uint8
+    where the scales are powers of two (exponent bytes)."""
+    M: int
+    K: int
+    codes: torch.Tensor              # [M, K] u8
+    scale: torch.Tensor              # [ceil(K / 128), M]
+
+    def struct(self) -> _BQ:
+        return _BQ(self.M, self.K, _scales(self.scale, _cdiv(self.K, BLOCK), self.M, self.codes, self.M, self.K),
+                   self.codes.data_ptr(), self.scale.data_ptr())
+
+
+@dataclass
+class BW:
+    """Weights in the block format (device tensors, see cham_bw)."""
+    N: int
+    K: int
+    codes: torch.Tensor              # [N, K] u8
+    scale: torch.Tensor              # [ceil(N / 128), ceil(K / 128)]
+
+    def struct(self) -> _BW:
+        return _BW(self.N, self.K,
+                   _scales(self.scale, _cdiv(self.N, BLOCK), _cdiv(self.K, BLOCK), self.codes, self.N, self.K),
+                   self.codes.data_ptr(), self.scale.data_ptr())
+
+
+def _cdiv(a: int, b: int) -> int:
+    return -(-a // b)
+
+
+def _scales(scale, rows, cols, codes, n, k) -> int:
+    """Check a block-format pair of tensors; whether its scales are powers of two."""
+    if codes.dtype != torch.uint8 or codes.shape != (n, k) or not codes.is_contiguous() or not codes.is_cuda:
+        raise ValueError(f"codes must be a contiguous device uint8 [{n}, {k}]")
+    pow2 = scale.dtype == torch.uint8
+    if (not pow2 and scale.dtype != torch.float32) or scale.shape != (rows, cols) or not scale.is_contiguous():
+        raise ValueError(f"scale must be a contiguous float32 or uint8 [{rows}, {cols}]")
+    if scale.device != codes.device:
+        raise ValueError("codes and scale must be on one device")
+    return int(pow2)
+
+
+def alloc_bq(M: int, K: int, device="cuda", pow2: bool = False) -> BQ:
+    return BQ(M, K, torch.empty((M, K), dtype=torch.uint8, device=device),
+              torch.empty((_cdiv(K, BLOCK), M), dtype=torch.uint8 if pow2 else torch.float32, device=device))
+
+
+def alloc_bw(N: int, K: int, device="cuda", pow2: bool = False) -> BW:
+    return BW(N, K, torch.empty((N, K), dtype=torch.uint8, device=device),
+              torch.empty((_cdiv(N, BLOCK), _cdiv(K, BLOCK)), dtype=torch.uint8 if pow2 else torch.float32, device=device))
+
+
+def _matrix(t: torch.Tensor, name: str, shape=None, device=None) -> int:
+    """Check a [rows, columns] device tensor with unit column stride; its element type."""
+    ty = _TYPES.get(t.dtype)
+    if ty is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16")
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be a matrix" + (f" of shape {tuple(shape)}" if shape is not None else ""))
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be a device tensor" + (f" on {device}" if device is not None else ""))
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise ValueError(f"{name} must have unit stride along its columns")
+    return ty
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Row stride in elements; a single row's stride says nothing, so it counts as packed."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class _On:
+    """The launch stream, with its device current.  What a call allocates comes from that
+    stream's pool: memory of another stream's pool may still be in use there."""
+    __slots__ = ("device", "stream", "prev")
+
+    def __init__(self, device, stream):
+        if stream is not None and stream.device != device:
+            raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
+        self.device, self.stream, self.prev = device, stream, None
+
+    def __enter__(self):
+        if self.device.index != torch.cuda.current_device():
+            self.prev = torch.cuda.current_device()
+            torch.cuda.set_device(self.device)
+        return (self.stream or torch.cuda.current_stream(self.device)).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.prev is not None:
+            torch.cuda.set_device(self.prev)
+
+    def alloc(self, make, *args, **kw):
+        if self.stream is None:
+            return make(*args, **kw)
+        with torch.cuda.stream(self.stream):
+            return make(*args, **kw)
+
+
+def _out_of(out, fmt, M, K, device, pow2, on):
+    """The output descriptor of a row pass: the caller's, else a new one."""
+    block = fmt == A_BLOCK128
+    if out is None:
+        if block:
+            out = on.alloc(alloc_bq, M, K, device, pow2)
+        else:
+            out = on.alloc(alloc_aq, M, K, device, with_e8m0=fmt in (A_MXFP8, A_MXINT8), nsamples=M)
+    elif isinstance(out, BQ) != block or (out.M, out.K) != (M, K) or out.codes.device != device:
+        raise ValueError("out must be a %s of shape (%d, %d) on %s" % ("BQ" if block else "AQ", M, K, device))
+    elif block and (out.scale.dtype == torch.uint8) != bool(pow2):
+        raise ValueError("out's scales are not of the kind pow2 asks for")
+    elif not block:
+        _check_token_aq(out, fmt)
+    return out, block
+
+
+def _check_token_aq(out, fmt):
+    M, K = out.M, out.K
+    if out.codes.shape != (M, K) or out.codes.dtype != torch.uint8 or not out.codes.is_contiguous():
+        raise ValueError(f"out.codes must be a contiguous uint8 [{M}, {K}]")
+    for t in (out.scale, out.zero):
+        if t.shape != (M,) or t.dtype != torch.float32 or not t.is_contiguous():
+            raise ValueError(f"out.scale and out.zero must be contiguous float32 [{M}] (one scale per token)")
+    if fmt in (A_MXFP8, A_MXINT8) and (out.e8m0 is None or out.e8m0.shape != (M, K // 32) or
+                                       out.e8m0.dtype != torch.uint8 or not out.e8m0.is_contiguous()):
+        raise ValueError(f"out.e8m0 must be a contiguous uint8 [{M}, {K // 32}]")
+
+
+def rms_norm_quantize(X: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6, *,
+                      residual: Optional[torch.Tensor] = None, residual_out: Optional[torch.Tensor] = None,
+                      fmt: int = A_BLOCK128, pow2: bool = False, out=None, stream=None):
+    """h = X + residual, y = h / sqrt(mean(h^2) + eps) * weight, in 8 bits: (BQ, h) for
+    A_BLOCK128 (pow2: scales that are powers of two), else (AQ, h) with one scale per token.
+    h has the residual's type (None without a residual); pass residual_out=residual to update
+    it in place.  X, residual and residual_out [M, K] may have strided rows."""
+    xt = _matrix(X, "X")
+    M, K = X.shape
+    dev = X.device
+    on = _On(dev, stream)
+    rt = r_ptr = ldr = h_ptr = ldh = 0
+    if residual is not None:
+        rt = _matrix(residual, "residual", X.shape, dev)
+        r_ptr, ldr = residual.data_ptr(), _ld(residual)
+        if residual_out is None:
+            residual_out = on.alloc(torch.empty, (M, K), dtype=residual.dtype, device=dev)
+        elif _matrix(residual_out, "residual_out", X.shape, dev) != rt:
+            raise ValueError("residual_out must have the residual's type")
+        h_ptr, ldh = residual_out.data_ptr(), _ld(residual_out)
+    elif residual_out is not None:
+        raise ValueError("residual_out needs a residual")
+    gt = g_ptr = 0
+    if weight is not None:
+        gt = _TYPES.get(weight.dtype, -1)
+        if gt < 0 or weight.shape != (K,) or weight.device != dev or not weight.is_contiguous():
+            raise ValueError(f"weight must be a contiguous float32, float16 or bfloat16 [{K}] on {dev}")
+        g_ptr = weight.data_ptr()
+    out, block = _out_of(out, fmt, M, K, dev, pow2, on)
+    n = _Norm(M, K, X.data_ptr(), _ld(X), r_ptr, ldr, h_ptr, ldh, g_ptr, xt, rt, gt, eps)
+    st = out.struct()
+    with on as s:
+        if block:
+            rc = lib().cham_rms_norm_quantize_block(ctypes.byref(n), ctypes.byref(st), s)
+        else:
+            rc = lib().cham_rms_norm_quantize(ctypes.byref(n), fmt, ctypes.byref(st), s)
+            out.fmt = fmt
+    _check(rc, "rms_norm_quantize")
+    return out, residual_out
+
+
+def gated_quantize(X: torch.Tensor, up: Optional[torch.Tensor] = None, act: int = ACT_SILU, *, fmt: int = A_BLOCK128,
+                   pow2: bool = False, out=None, stream=None):
+    """y = act(X) * up (up=None: act(X)) in 8 bits: a BQ for A_BLOCK128, else an AQ with one
+    scale per token.  X and up [M, K] may have strided rows (the halves of one matrix)."""
+    xt = _matrix(X, "X")
+    M, K = X.shape
+    dev = X.device
+    on = _On(dev, stream)
+    u_ptr = ldu = 0
+    if up is not None:
+        if _matrix(up, "up", X.shape, dev) != xt:
+            raise ValueError("X and up must have one type")
+        u_ptr, ldu = up.data_ptr(), _ld(up)
+    out, block = _out_of(out, fmt, M, K, dev, pow2, on)
+    g = _Gate(M, K, X.data_ptr(), _ld(X), u_ptr, ldu, xt, act)
+    st = out.struct()
+    with on as s:
+        if block:
+            rc = lib().cham_gated_quantize_block(ctypes.byref(g), ctypes.byref(st), s)
+        else:
+            rc = lib().cham_gated_quantize(ctypes.byref(g), fmt, ctypes.byref(st), s)
+            out.fmt = fmt
+    _check(rc, "gated_quantize")
+    return out
+
+
+def block_quantize_weights(W: torch.Tensor, pow2: bool = False, out: Optional[BW] = None, stream=None) -> BW:
+    """W [N, K] (rows may be strided) in the block format: a scale for each 128 x 128 block."""
+    ty = _matrix(W, "W")
+    N, K = W.shape
+    on = _On(W.device, stream)
+    if out is None:
+        out = on.alloc(alloc_bw, N, K, W.device, pow2)
+    elif (out.N, out.K) != (N, K) or out.codes.device != W.device or (out.scale.dtype == torch.uint8) != bool(pow2):
+        raise ValueError("out does not fit W and pow2")
+    st = out.struct()
+    with on as s:
+        rc = lib().cham_block_quantize_weights(W.data_ptr(), ty, _ld(W), ctypes.byref(st), s)
+    _check(rc, "block_quantize_weights")
+    return out
+
+
+def block_linear(xb: BQ, wb: BW, Y: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                 stream=None) -> torch.Tensor:
+    """Y [M, N] = activations times weights^T, both in the block format; Y (rows may be strided)
+    decides the type where it is given, else dtype."""
+    dev = xb.codes.device
+    if wb.codes.device != dev:
+        raise ValueError(f"the weights must be on {dev}")
+    on = _On(dev, stream)
+    if Y is None:
+        Y = on.alloc(torch.empty, (xb.M, wb.N), dtype=dtype, device=dev)
+    ty = _matrix(Y, "Y", (xb.M, wb.N), dev)
+    a, w = xb.struct(), wb.struct()
+    with on as s:
+        rc = lib().cham_block_linear(ctypes.byref(a), ctypes.byref(w), Y.data_ptr(), ty, _ld(Y), s)
+    _check(rc, "block_linear")
+    return Y
+
+
+def block_linear_plan(M: int, N: int, K: int, dtype: torch.dtype = torch.bfloat16) -> tuple:
+    """(tile rows, tile channels, k groups) block_linear takes for these sizes (host only)."""
+    out = (ctypes.c_int32 * 3)()
+    _check(lib().cham_block_linear_plan(M, N, K, _TYPES[dtype], out, 3), "block_linear_plan")
+    return tuple(out)

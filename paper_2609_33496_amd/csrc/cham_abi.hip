@@ -1,5 +1,7 @@
 // Host-side parts of the C ABI that are not tied to one kernel: status strings, version,
 // workspace sizes.
+#include <atomic>
+
 #include "cham_device.h"
 
 size_t cham_stats_workspace_bytes(int64_t numel);
@@ -33,4 +35,18 @@ extern "C" size_t cham_workspace_bytes(int32_t op, int64_t M, int64_t N, int64_t
     case CHAM_OP_COLSQ: return cham_colsq_workspace_bytes(K);
     default: return 0;
     }
+}
+
+// CU count of the current device, queried once per device (every thread that races to
+// fill the cache stores the same value, so relaxed atomics suffice)
+int cham_device_cus() {
+    static std::atomic<int> cached[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+    int n = cached[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+        cached[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
 }

@@ -1,0 +1,677 @@
+// Block-scaled product Y = (xc xs) (wc ws)^T on the 8-bit matrix cores.
+//
+//   Y[m][n] = sum_b xs[b][m] ws[n/128][b] sum_{k in b} xc[m][k] wc[n][k]
+//
+// v_mfma_f32_16x16x128_f8f6f4 contracts one block of 128 at once.  The weights are its first
+// operand and the activations its second, so a lane's four results lie in one row of Y (one
+// activation scale) and four channels of one weight block (one weight scale): the factor of a
+// block is one number per lane and 16 rows.  With binary32 scales each block's product starts
+// from zero and is added as acc += factor * product (one v_fma per result, 16 cycles beside the
+// 32 of the matrix instruction); with powers of two the instruction applies the scale bytes
+// itself and accumulates in place.
+#include <algorithm>
+#include <type_traits>
+
+#include "cham_device.h"
+
+namespace cham {
+namespace {
+
+typedef int int8v __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef int int4v __attribute__((ext_vector_type(4)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+
+constexpr int BK = 128;                 // one block of the format: bytes of a row per step
+constexpr int kBufferFlags = 0x00020000;  // buffer descriptor word 3: 32-bit data, raw
+constexpr uint32_t kOutside = 0x80000000u;  // an offset past every buffer: such loads give zeros
+
+struct BlockArgs {
+    const uint8_t* xc;
+    const void* xs;
+    const uint8_t* wc;
+    const void* ws;
+    void* Y;
+    int64_t ldy;
+    int M, N, K, nkb;
+    int tm, tn;    // tiles
+    int vec;       // rows of Y start at multiples of 16 bytes
+};
+
+// How the products of a block are formed.  The 8-bit matrix instructions align the products of
+// a group of neighbouring k to the largest one and drop what lies more than 13 bits below it
+// (a relative error of 3e-5 of the result on heavy-tailed data; a result of 16 bits is itself
+// rounded at 5e-4 or more).  A binary32 result takes the exact route: the codes as half
+// precision (exact) through the f16 instructions, whose sums lose no more than binary32 does, at
+// half the rate.
+enum { kCodes, kCodesPow2, kHalf, kHalfPow2 };
+constexpr bool byte_scales(int mode) { return mode == kCodesPow2 || mode == kHalfPow2; }
+constexpr bool exact(int mode) { return mode == kHalf || mode == kHalfPow2; }
+template <bool BYTES>
+struct ScaleOf {
+    using type = float;
+};
+template <>
+struct ScaleOf<true> {
+    using type = uint8_t;
+};
+CHAM_DEV float factor(float s) { return s; }
+CHAM_DEV float factor(uint8_t e) {  // 2^(e - 127); 255 is NaN
+    return __uint_as_float(e == 0 ? 0x400000u : e == 255 ? 0x7fc00000u : (uint32_t)e << 23);
+}
+
+// One operand of a lane: 32 codes of a row, in any order of k that both operands share
+union Codes {
+    int8v v;
+    int4v q[2];
+    uint32_t u[8];
+};
+// The same as half precision, 8 codes for each of four f16 instructions
+union Halves {
+    half8v h[4];
+    uint32_t u[16];
+};
+CHAM_DEV Halves to_half(const Codes& c) {
+    Halves r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        r.u[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c.u[i], 1.0f, false));
+        r.u[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c.u[i], 1.0f, true));
+    }
+    return r;
+}
+CHAM_DEV const Codes& operand_as(const Codes& c, const Codes*) { return c; }
+CHAM_DEV Halves operand_as(const Codes& c, const Halves*) { return to_half(c); }
+template <int MODE>
+using Operand = typename std::conditional<exact(MODE), Halves, Codes>::type;
+
+CHAM_DEV float4v mfma(const Codes& a, const Codes& b, float4v c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, c, 0, 0, 0, 0, 0, 0);
+}
+CHAM_DEV float4v mfma_pow2(const Codes& a, const Codes& b, float4v c, int sa, int sb) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, c, 0, 0, 0, sa, 0, sb);
+}
+CHAM_DEV float4v mfma_half(half8v a, half8v b, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+CHAM_DEV uint32_t bf16_bits(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return (u & 0x7fffffffu) > 0x7f800000u ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+}
+
+template <int YT>
+CHAM_DEV void store1(void* Y, int64_t i, float v) {
+    if constexpr (YT == CHAM_T_F32) ((float*)Y)[i] = v;
+    else if constexpr (YT == CHAM_T_F16) ((_Float16*)Y)[i] = (_Float16)v;
+    else ((uint16_t*)Y)[i] = (uint16_t)bf16_bits(v);
+}
+
+template <int YT>
+CHAM_DEV uint32_t pack2(float a, float b) {
+    if constexpr (YT == CHAM_T_F16) {
+        const half2v h = {(_Float16)a, (_Float16)b};
+        return __builtin_bit_cast(uint32_t, h);
+    } else {
+        return bf16_bits(a) | bf16_bits(b) << 16;
+    }
+}
+
+// 4 and 8 consecutive channels of one row of Y
+template <int YT>
+CHAM_DEV void store4(const BlockArgs& a, int64_t m, int64_t n, float4v p) {
+    if (m >= a.M) return;
+    const int64_t i = m * a.ldy + n;
+    if (a.vec && n + 4 <= a.N) {
+        if constexpr (YT == CHAM_T_F32) *(float4v*)((float*)a.Y + i) = p;
+        else *(uint2*)((uint16_t*)a.Y + i) = make_uint2(pack2<YT>(p[0], p[1]), pack2<YT>(p[2], p[3]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (n + j < a.N) store1<YT>(a.Y, i + j, p[j]);
+    }
+}
+template <int YT>
+CHAM_DEV void store8(const BlockArgs& a, int64_t m, int64_t n, float4v p, float4v q) {
+    const int64_t i = m * a.ldy + n;
+    if (a.vec && n + 8 <= a.N) {
+        if constexpr (YT == CHAM_T_F32) {
+            *(float4v*)((float*)a.Y + i) = p;
+            *(float4v*)((float*)a.Y + i + 4) = q;
+        } else {
+            *(uint4*)((uint16_t*)a.Y + i) = make_uint4(pack2<YT>(p[0], p[1]), pack2<YT>(p[2], p[3]), pack2<YT>(q[0], q[1]),
+                                                       pack2<YT>(q[2], q[3]));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (n + j < a.N) store1<YT>(a.Y, i + j, j < 4 ? p[j] : q[j - 4]);
+    }
+}
+
+// ------------------------------------------------------------------------------------
+// tiles through LDS
+// ------------------------------------------------------------------------------------
+// WM x WN wavefronts of (16 TM rows) x (16 TN channels).  A k-step's rows (128 bytes each) go
+// from memory to LDS directly (16 bytes a lane), two steps ahead: activations in two buffers (a
+// step's operands are in registers before its products begin, so its buffer takes the step after
+// next then), weights in three.  The 16-byte chunk c of LDS row r lies at c ^ key(r): the lanes
+// that read one chunk of 16 rows in one operand load then spread over all banks (no conflicts
+// counted).  The channel order inside a wavefront's block is chosen so that a lane's results of
+// two neighbouring operand blocks are 8 consecutive channels of Y.
+// bytes of LDS; the address space is part of the type, so that reads of it cannot become others
+typedef __attribute__((address_space(3))) uint8_t Lds;
+
+CHAM_DEV int key_x(int r) { return (r >> 1) & 7; }
+CHAM_DEV int key_w(int r) { return ((r >> 1) & 1) | ((r >> 3) & 3) << 1; }
+
+// channel (within a wavefront's 16 TN) of operand row rr of block t
+CHAM_DEV int chan(int t, int rr) { return (t >> 1) * 32 + (rr >> 2) * 8 + (t & 1) * 4 + (rr & 3); }
+
+// KS groups of WM x WN wavefronts: group q takes the k-steps q, q + KS, ... through buffers of its
+// own, and the groups' sums are added in their order at the end.
+template <int WM_, int WN_, int TM_, int TN_, int KS_>
+struct Tile {
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, KS = KS_;
+    static constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN, kWaves = WM * WN;
+    static constexpr int kLoadsX = BM / 8 / kWaves, kLoadsW = BN / 8 / kWaves;  // 1 KB each
+    static_assert(kWaves % 4 == 0 && TN % 2 == 0 && 128 % (16 * TN) == 0 && BN <= 256, "layout");
+    static_assert(KS == 1 || BM <= 64, "a group's sums fit its slices of two weight buffers");
+};
+
+
+// Workgroup -> tile.  Workgroups go round the 8 XCDs; each XCD takes a contiguous run of an
+// order that walks kGroup tile rows down before it steps to the next tile column, so that the
+// tiles an XCD works on at one time share their activation and weight rows in its L2.
+constexpr int kGroup = 8;
+CHAM_DEV void tile_of(const BlockArgs& a, int& bm, int& bn) {
+    const int n = a.tm * a.tn, b = blockIdx.x;
+    const int q = n >> 3, r = n & 7, x = b & 7;
+    const int i = x * q + min(x, r) + (b >> 3);
+    const int gsize = kGroup * a.tn, gi = i / gsize, rows = min(kGroup, a.tm - gi * kGroup), j = i - gi * gsize;
+    bn = j / rows;
+    bm = gi * kGroup + (j - bn * rows);
+}
+
+// Waits until at most N of this wavefront's memory loads (LDS writes among them) are in flight,
+// then for the other wavefronts; loads stay in flight across it.
+template <int N>
+CHAM_DEV void landed_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4 | 15 << 8);  // vmcnt(N)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+// Waits until this wavefront's LDS reads are in registers, then for the other wavefronts.
+CHAM_DEV void read_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <class T, int MODE, int YT>
+__global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockArgs a) {
+    constexpr int WM = T::WM, TM = T::TM, TN = T::TN, KS = T::KS;
+    using Scale = typename ScaleOf<byte_scales(MODE)>::type;
+    constexpr int kX = T::BM * BK, kW = T::BN * BK;  // bytes of a step
+    __shared__ __align__(16) uint8_t X0[KS * kX], X1[KS * kX];
+    __shared__ __align__(16) uint8_t W0[KS * kW], W1[KS * kW], W2[KS * kW];
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = KS > 1 ? all / T::kWaves : 0, wave = all - group * T::kWaves;
+    const int wm = wave % WM, wn = wave / WM;
+    int bm, bn;
+    tile_of(a, bm, bn);
+    const int64_t m0 = (int64_t)bm * T::BM, n0 = (int64_t)bn * T::BN;
+    const int K = a.K, nkb = a.nkb;
+
+    const int mrows = min((int64_t)T::BM, a.M - m0), nrows = min((int64_t)T::BN, a.N - n0);
+    const __amdgpu_buffer_rsrc_t rx =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(a.xc + m0 * K), (short)0, mrows * K, kBufferFlags);
+    const __amdgpu_buffer_rsrc_t rw =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(a.wc + n0 * K), (short)0, nrows * K, kBufferFlags);
+
+    // Load i of a wavefront: rows (i kWaves + wave) 8 .. + 7, lane l the slot l % 8 of row l / 8.
+    // The rows of two loads differ by a multiple of 32, so a lane's chunk is the same in all.
+    // Rows past the tile's last and chunks past K are outside the buffer: zeros.
+    const int r0 = wave * 8 + (lane >> 3);
+    const int cx0 = (lane & 7) ^ key_x(r0), cw0 = (lane & 7) ^ key_w(r0);
+    uint32_t offx = (uint32_t)r0 * K + cx0 * 16, offw = (uint32_t)r0 * K + cw0 * 16;
+    const bool lastx = (nkb - 1) * BK + cx0 * 16 >= K, lastw = (nkb - 1) * BK + cw0 * 16 >= K;
+    const uint32_t rstep = (uint32_t)T::kWaves * 8 * K;
+    auto issue = [&](const __amdgpu_buffer_rsrc_t& r, Lds* buf, int loads, uint32_t off, bool past, int kb) {
+        const uint32_t o = kb >= nkb || (kb == nkb - 1 && past) ? kOutside : off;
+#pragma unroll
+        for (int i = 0; i < loads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                r, (__attribute__((address_space(3))) void*)(buf + (i * T::kWaves + wave) * 1024), 16, o + i * rstep, kb * BK, 0, 0);
+    };
+    auto issue_x = [&](Lds* buf, int kb) { issue(rx, buf + group * kX, T::kLoadsX, offx, lastx, kb); };
+    auto issue_w = [&](Lds* buf, int kb) { issue(rw, buf + group * kW, T::kLoadsW, offw, lastw, kb); };
+
+    // scales of the lane's rows (one per 16-row block) and of the wavefront's channels
+    const int rr = lane & 15, g = lane >> 4;
+    const int64_t wblk = min((n0 + wn * 16 * TN) / 128, ((int64_t)a.N - 1) / 128) * nkb;
+    const Scale* const wsp = (const Scale*)a.ws + wblk;
+    struct Factors {
+        Scale x[TM], w;
+    };
+    Factors s0, s1;
+    auto scales = [&](Factors& s, int kb) {
+        const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(wsp + min(kb, nkb - 1)), (short)0, (int)sizeof(Scale), kBufferFlags);
+        // one block's scales from the tile's first row on; zeros past the last row
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)((const Scale*)a.xs + (int64_t)min(kb, nkb - 1) * a.M + m0), (short)0, mrows * (int)sizeof(Scale), kBufferFlags);
+        if constexpr (byte_scales(MODE)) s.w = __builtin_amdgcn_raw_buffer_load_b8(rb, 0, 0, 0);
+        else s.w = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, 0, 0, 0));
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+            const int o = (int)((wm * TM * 16 + rr) * sizeof(Scale) + t * 16 * sizeof(Scale));
+            if constexpr (byte_scales(MODE)) s.x[t] = __builtin_amdgcn_raw_buffer_load_b8(rs, o, 0, 0);
+            else s.x[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, 0));
+        }
+    };
+
+    float4v acc[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) acc[i][j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+
+    // byte offsets of the lane's two chunks: its key is the same in every 16-row block
+    const int x0 = group * kX + (wm * TM * 16 + rr) * BK, w0 = group * kW + (wn * 16 * TN + chan(0, rr)) * BK;
+    const int xlo = x0 + ((g ^ key_x(rr)) << 4), xhi = x0 + (((g + 4) ^ key_x(rr)) << 4);
+    const int wlo = w0 + ((g ^ key_w(chan(0, rr))) << 4), whi = w0 + (((g + 4) ^ key_w(chan(0, rr))) << 4);
+    auto operand = [&](const Lds* buf, int lo, int hi, int off) {
+        Codes o;
+        o.q[0] = *(const __attribute__((address_space(3))) int4v*)(buf + lo + off);
+        o.q[1] = *(const __attribute__((address_space(3))) int4v*)(buf + hi + off);
+        return o;
+    };
+
+    // The group's step j: X and W hold it, X and Wn take its step j + 2.
+    auto step = [&](Lds* X, const Lds* W, Lds* Wn, Factors& s, int j) {
+        const int next = __builtin_amdgcn_readfirstlane((j + 2) * KS + group);
+        landed_barrier<T::kLoadsX + T::kLoadsW + TM + 1>();  // step j is there; W of step j - 1 is free
+        float f[TM];
+        Scale cx[TM], cw = s.w;
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+            cx[t] = s.x[t];
+            if constexpr (MODE != kCodesPow2) f[t] = factor(cx[t]) * factor(cw);
+        }
+        Codes bc[TM];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) bc[t] = operand(X, xlo, xhi, t * 16 * BK);
+        Codes w[2];
+        w[0] = operand(W, wlo, whi, 0);
+        asm volatile("" : "+v"(offx), "+v"(offw));  // keeps the sums of issue() from living in registers
+        scales(s, next);
+        issue_w(Wn, next);
+        read_barrier();  // X is in registers everywhere
+        issue_x(X, next);
+        // Operand block i + 1 is read from LDS while block i is multiplied; a product waits kLag
+        // others before it is scaled and added, so that no instruction waits for the one before
+        // it.  The scheduling fences keep the compiler from gathering all reads in front (more
+        // registers than there are).
+        Operand<MODE> b[TM];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) b[t] = operand_as(bc[t], (const Operand<MODE>*)nullptr);
+        constexpr int kLag = exact(MODE) ? 0 : 3;
+        float4v d[exact(MODE) ? TM : 4];
+        auto add = [&](int j) {
+            const int i = j / TM, t = j % TM;
+            const float4v p = d[j % (exact(MODE) ? TM : 4)];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[i][t][q] = __builtin_fmaf(p[q], f[t], acc[i][t][q]);
+        };
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            if (i + 1 < TN) w[(i + 1) & 1] = operand(W, wlo, whi, chan(i + 1, 0) * BK);
+            const Operand<MODE> a = operand_as(w[i & 1], (const Operand<MODE>*)nullptr);
+            const int j = i * TM;
+            if constexpr (exact(MODE)) {
+                float4v* e = d;
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+#pragma unroll
+                    for (int t = 0; t < TM; ++t)
+                        e[t] = mfma_half(a.h[h], b[t].h[h], h == 0 ? float4v{0.0f, 0.0f, 0.0f, 0.0f} : e[t]);
+            }
+#pragma unroll
+            for (int t = 0; t < TM; ++t) {
+                if constexpr (MODE == kCodesPow2) {
+                    acc[i][t] = mfma_pow2(a, b[t], acc[i][t], cw, cx[t]);
+                } else {
+                    if constexpr (MODE == kCodes) d[(j + t) & 3] = mfma(a, b[t], float4v{0.0f, 0.0f, 0.0f, 0.0f});
+                    if (j + t >= kLag) add(j + t - kLag);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (MODE != kCodesPow2) {
+#pragma unroll
+            for (int j = TN * TM - kLag; j < TN * TM; ++j) add(j);
+        }
+    };
+
+    Lds *const x_0 = (Lds*)X0, *const x_1 = (Lds*)X1;
+    Lds *const w_0 = (Lds*)W0, *const w_1 = (Lds*)W1, *const w_2 = (Lds*)W2;
+    scales(s0, group);
+    issue_w(w_0, group);
+    issue_x(x_0, group);
+    scales(s1, KS + group);
+    issue_w(w_1, KS + group);
+    issue_x(x_1, KS + group);
+    const int steps = (nkb + KS - 1) / KS;  // the same for all groups: steps past the last block are zeros
+    for (int j = 0;; j += 6) {
+        step(x_0, w_0, w_2, s0, j);
+        if (j + 1 >= steps) break;
+        step(x_1, w_1, w_0, s1, j + 1);
+        if (j + 2 >= steps) break;
+        step(x_0, w_2, w_1, s0, j + 2);
+        if (j + 3 >= steps) break;
+        step(x_1, w_0, w_2, s1, j + 3);
+        if (j + 4 >= steps) break;
+        step(x_0, w_1, w_0, s0, j + 4);
+        if (j + 5 >= steps) break;
+        step(x_1, w_2, w_1, s1, j + 5);
+        if (j + 6 >= steps) break;
+    }
+    landed_barrier<0>();  // no write to LDS outlives the workgroup or meets the sums below
+
+    if constexpr (KS > 1) {
+        auto part = [&](int q, int i, int t) {  // block (i, t) of this wavefront's counterpart in group q
+            float4v* p = (float4v*)((i < TN / 2 ? W0 : W1) + q * kW);
+            return p + ((wave * (TN / 2) + i % (TN / 2)) * TM + t) * 64 + lane;
+        };
+        if (group > 0) {
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+#pragma unroll
+                for (int t = 0; t < TM; ++t) *part(group, i, t) = acc[i][t];
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int q = 1; q < KS; ++q)
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+#pragma unroll
+                for (int t = 0; t < TM; ++t) acc[i][t] += *part(q, i, t);
+    }
+
+#pragma unroll
+    for (int t = 0; t < TM; ++t) {
+        const int64_t m = m0 + (wm * TM + t) * 16 + rr;
+        if (m < a.M) {
+#pragma unroll
+            for (int i = 0; i < TN; i += 2)
+                store8<YT>(a, m, n0 + wn * 16 * TN + (i >> 1) * 32 + g * 8, acc[i][t], acc[i + 1][t]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------
+// few rows: operands straight from memory, k split over the workgroup's wavefronts
+// ------------------------------------------------------------------------------------
+// A workgroup makes 16 TM rows x 16 TN channels; wavefront v of NW takes the k-steps v, v + NW,
+// ...  With few rows every weight is read by few workgroups, so LDS would only stand in the way:
+// a lane loads its operands of the next step while it multiplies.  The partial sums meet in LDS
+// and are added in the order of the wavefronts (no second launch, no atomics).
+template <int TM, int TN, int NW, int MODE, int YT>
+__global__ __launch_bounds__(NW * 64) void few_rows_kernel(BlockArgs a) {
+    using Scale = typename ScaleOf<byte_scales(MODE)>::type;
+    __shared__ float4v part[NW][TN * TM][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rr = lane & 15, g = lane >> 4, K = a.K, nkb = a.nkb;
+    const int64_t m0 = (int64_t)(blockIdx.x % a.tm) * 16 * TM, n0 = (int64_t)(blockIdx.x / a.tm) * 16 * TN;
+    const uint8_t *px[TM], *pw[TN];
+    const Scale* ps[TM];
+#pragma unroll
+    for (int t = 0; t < TM; ++t) {
+        const int64_t m = min(m0 + t * 16 + rr, (int64_t)a.M - 1);  // past the last row: repeats of it, not written
+        px[t] = a.xc + m * K;
+        ps[t] = (const Scale*)a.xs + m;
+    }
+#pragma unroll
+    for (int i = 0; i < TN; ++i) pw[i] = a.wc + min(n0 + i * 16 + rr, (int64_t)a.N - 1) * K;
+    const Scale* const wsp = (const Scale*)a.ws + n0 / 128 * nkb;  // 16 TN divides 128
+
+    struct Step {
+        Codes x[TM], w[TN];
+        Scale sx[TM], sw;
+    };
+    auto load = [&](Step& s, int kb) {
+        const int k0 = kb * BK + g * 16, k1 = k0 + 64;  // the lane's two chunks
+        const int c0 = min(k0, K - 16), c1 = min(k1, K - 16);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            s.w[i].q[0] = *(const int4v*)(pw[i] + c0);
+            s.w[i].q[1] = *(const int4v*)(pw[i] + c1);
+        }
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+            s.x[t].q[0] = *(const int4v*)(px[t] + c0);
+            s.x[t].q[1] = *(const int4v*)(px[t] + c1);
+            s.sx[t] = ps[t][(int64_t)kb * a.M];
+        }
+        s.sw = wsp[kb];
+    };
+    float4v acc[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int t = 0; t < TM; ++t) acc[i][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    auto multiply = [&](Step& s, int kb) {
+        if (kb == nkb - 1 && K % BK != 0) {  // chunks past K: zeros in both operands
+            const int k0 = kb * BK + g * 16;
+            const int4v z = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+                if (k0 >= K) s.w[i].q[0] = z;
+                if (k0 + 64 >= K) s.w[i].q[1] = z;
+            }
+#pragma unroll
+            for (int t = 0; t < TM; ++t) {
+                if (k0 >= K) s.x[t].q[0] = z;
+                if (k0 + 64 >= K) s.x[t].q[1] = z;
+            }
+        }
+        Operand<MODE> b[TM];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) b[t] = operand_as(s.x[t], (const Operand<MODE>*)nullptr);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            const Operand<MODE> w = operand_as(s.w[i], (const Operand<MODE>*)nullptr);
+#pragma unroll
+            for (int t = 0; t < TM; ++t) {
+                if constexpr (MODE == kCodesPow2) {
+                    acc[i][t] = mfma_pow2(w, b[t], acc[i][t], s.sw, s.sx[t]);
+                } else {
+                    float4v d = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if constexpr (exact(MODE)) {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) d = mfma_half(w.h[h], b[t].h[h], d);
+                    } else {
+                        d = mfma(w, b[t], d);
+                    }
+                    const float f = factor(s.sx[t]) * factor(s.sw);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[i][t][q] = __builtin_fmaf(d[q], f, acc[i][t][q]);
+                }
+            }
+        }
+    };
+    Step s0, s1;
+    if (wave < nkb) load(s0, wave);
+    for (int kb = wave; kb < nkb; kb += 2 * NW) {
+        if (kb + NW < nkb) load(s1, kb + NW);
+        multiply(s0, kb);
+        if (kb + NW >= nkb) break;
+        if (kb + 2 * NW < nkb) load(s0, kb + 2 * NW);
+        multiply(s1, kb + NW);
+    }
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int t = 0; t < TM; ++t) part[wave][i * TM + t][lane] = acc[i][t];
+    __syncthreads();
+    for (int e = threadIdx.x; e < TN * TM * 64; e += NW * 64) {
+        const int j = e >> 6, l = e & 63;
+        float4v y = part[0][j][l];
+#pragma unroll
+        for (int v = 1; v < NW; ++v) y += part[v][j][l];
+        store4<YT>(a, m0 + (j % TM) * 16 + (l & 15), n0 + (j / TM) * 16 + (l >> 4) * 4, y);
+    }
+}
+
+// ------------------------------------------------------------------------------------
+// launches
+// ------------------------------------------------------------------------------------
+template <class T, int MODE, int YT>
+void launch_tile(BlockArgs a, hipStream_t s) {
+    a.tm = (a.M + T::BM - 1) / T::BM;
+    a.tn = (a.N + T::BN - 1) / T::BN;
+    hipLaunchKernelGGL((tile_kernel<T, MODE, YT>), dim3((unsigned)(a.tm * a.tn)), dim3(T::kWaves * T::KS * 64), 0, s, a);
+}
+template <int TM, int TN, int NW, int MODE, int YT>
+void launch_few(BlockArgs a, hipStream_t s) {
+    a.tm = (a.M + 16 * TM - 1) / (16 * TM);
+    a.tn = (a.N + 16 * TN - 1) / (16 * TN);
+    hipLaunchKernelGGL((few_rows_kernel<TM, TN, NW, MODE, YT>), dim3((unsigned)(a.tm * a.tn)), dim3(NW * 64), 0, s, a);
+}
+
+// Modeled time (us) of one tile shape: tiles on the busiest CU, each its k-steps and a fixed part
+// (first loads, output).  Fitted to forced launches over 20 shapes (M 1 - 8192, N 640 - 10240,
+// K 1152 - 8192) with inputs that rotate through the last-level cache.
+struct TileCost {
+    int bm, bn, ks;
+    double lone, step, fixed;  // us: a k-step alone on a CU, among others, and the fixed part
+};
+enum { kT256, kT128, kT64, kT64x2, kT32, kT32x2, kTWide, kTiles };
+// 8-bit matrix instructions
+constexpr TileCost kCostCodes[kTiles] = {{256, 256, 1, 1.96, 1.96, 3.0}, {128, 128, 1, 0.67, 0.55, 1.8},
+                                         {64, 64, 1, 0.28, 0.205, 0.35}, {64, 64, 2, 0.46, 0.50, 0.6},
+                                         {32, 64, 1, 0.25, 0.137, 0.2},  {32, 64, 2, 0.36, 0.38, 0.3},
+                                         {0, 0, 0, 0, 0, 0}};
+// f16 matrix instructions
+constexpr TileCost kCostHalf[kTiles] = {{0, 0, 0, 0, 0, 0},             {0, 0, 0, 0, 0, 0},
+                                        {64, 64, 1, 0.43, 0.314, 0.55}, {64, 64, 2, 0.70, 0.77, 0.8},
+                                        {32, 64, 1, 0.33, 0.195, 0.4},  {32, 64, 2, 0.50, 0.43, 0.5},
+                                        {64, 128, 1, 0.65, 0.57, 1.0}};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int plan_tile(const BlockArgs& a, const TileCost* costs) {
+    const int cus = cham_device_cus();
+    int best = -1;
+    double least = 0.0;
+    for (int i = 0; i < kTiles; ++i) {
+        const TileCost& c = costs[i];
+        if (c.bm == 0) continue;
+        const int64_t tiles = ceil_div(a.M, c.bm) * ceil_div(a.N, c.bn), k = ceil_div(tiles, cus);
+        const double t = (double)k * ((double)ceil_div(a.nkb, c.ks) * (k == 1 ? c.lone : c.step) + c.fixed);
+        if (best < 0 || t < least) { best = i; least = t; }
+    }
+    return best;
+}
+
+// Few rows go without LDS where the launch is at most one workgroup per CU, or where the
+// activations' repeated rows cost nothing: 1 x 10240 x 1280 4.5 us against 5.0 in tiles of 32 x 64
+// (f16 route 4.5 against 5.7), 32 x 1280 x 5120 6.9 against 8.8; but 16 x 10240 x 1280 5.7 against
+// 5.1 (f16 route 5.7 against 5.9).
+bool few_rows(const BlockArgs& a, bool half) {
+    return ceil_div(a.M, 16) * ceil_div(a.N, 16) <= cham_device_cus() || a.M <= (half ? 16 : 8);
+}
+
+template <int MODE, int YT>
+void launch_plan(const BlockArgs& a, hipStream_t s) {
+    if (few_rows(a, exact(MODE))) return launch_few<1, 1, 8, MODE, YT>(a, s);
+    const int tile = plan_tile(a, exact(MODE) ? kCostHalf : kCostCodes);
+    if constexpr (exact(MODE)) {
+        if (tile == kTWide) return launch_tile<Tile<2, 2, 2, 4, 1>, MODE, YT>(a, s);
+    } else {
+        if (tile == kT256) return launch_tile<Tile<4, 2, 4, 8, 1>, MODE, YT>(a, s);
+        if (tile == kT128) return launch_tile<Tile<2, 2, 4, 4, 1>, MODE, YT>(a, s);
+    }
+    if (tile == kT64) return launch_tile<Tile<2, 2, 2, 2, 1>, MODE, YT>(a, s);
+    if (tile == kT64x2) return launch_tile<Tile<2, 2, 2, 2, 2>, MODE, YT>(a, s);
+    if (tile == kT32) return launch_tile<Tile<2, 2, 1, 2, 1>, MODE, YT>(a, s);
+    return launch_tile<Tile<2, 2, 1, 2, 2>, MODE, YT>(a, s);
+}
+
+int block_check(const cham_bq* x, const cham_bw* w) {
+    if (!x || !w || x->M < 0 || w->N < 1 || x->K < 1 || x->K != w->K) return CHAM_EINVAL;
+    if (x->K % 32 != 0 || x->K > (1 << 20) || x->M >= (int64_t)1 << 31 || w->N >= (int64_t)1 << 31) return CHAM_ESHAPE;
+    if (ceil_div(x->M, 32) * ceil_div(w->N, 16) >= (int64_t)1 << 31) return CHAM_ESHAPE;  // workgroups of any plan
+    if ((x->M > 0 && (!x->codes || !x->scale)) || !w->codes || !w->scale) return CHAM_EINVAL;
+    if (((uintptr_t)x->codes & 15u) || ((uintptr_t)w->codes & 15u)) return CHAM_EINVAL;
+    if ((!x->pow2 && ((uintptr_t)x->scale & 3u)) || (!w->pow2 && ((uintptr_t)w->scale & 3u))) return CHAM_EINVAL;
+    if ((x->pow2 != 0 && x->pow2 != 1) || x->pow2 != w->pow2) return CHAM_EINVAL;
+    return CHAM_OK;
+}
+
+}  // namespace
+}  // namespace cham
+
+using namespace cham;
+
+extern "C" int cham_block_linear(const cham_bq* x, const cham_bw* w, void* Y, int32_t y_type, int64_t ldy,
+                                 void* stream) {
+    const int rc = block_check(x, w);
+    if (rc != CHAM_OK) return rc;
+    if (y_type < 0 || y_type >= CHAM_T_N) return CHAM_EFORMAT;
+    const int size = y_type == CHAM_T_F32 ? 4 : 2;
+    if (x->M == 0) return CHAM_OK;
+    if (!Y || ldy < w->N || (uintptr_t)Y % size) return CHAM_EINVAL;
+    BlockArgs a{};
+    a.xc = x->codes;
+    a.xs = x->scale;
+    a.wc = w->codes;
+    a.ws = w->scale;
+    a.Y = Y;
+    a.ldy = ldy;
+    a.M = (int)x->M;
+    a.N = (int)w->N;
+    a.K = (int)x->K;
+    a.nkb = (a.K + BK - 1) / BK;
+    a.vec = ((uintptr_t)Y & 15u) == 0 && ldy * size % 16 == 0;
+    const hipStream_t s = (hipStream_t)stream;
+    if (y_type == CHAM_T_F32) {
+        if (x->pow2) launch_plan<kHalfPow2, CHAM_T_F32>(a, s);
+        else launch_plan<kHalf, CHAM_T_F32>(a, s);
+    } else if (y_type == CHAM_T_F16) {
+        if (x->pow2) launch_plan<kCodesPow2, CHAM_T_F16>(a, s);
+        else launch_plan<kCodes, CHAM_T_F16>(a, s);
+    } else {
+        if (x->pow2) launch_plan<kCodesPow2, CHAM_T_BF16>(a, s);
+        else launch_plan<kCodes, CHAM_T_BF16>(a, s);
+    }
+    CHAM_CHECK_LAUNCH();
+    return CHAM_OK;
+}
+
+extern "C" int cham_block_linear_plan(int64_t M, int64_t N, int64_t K, int32_t y_type, int32_t* out, int32_t out_len) {
+    if (!out || out_len < 3 || M < 1 || N < 1 || K < 1) return CHAM_EINVAL;
+    if (y_type < 0 || y_type >= CHAM_T_N) return CHAM_EFORMAT;
+    if (K % 32 != 0 || K > (1 << 20) || M >= (int64_t)1 << 31 || N >= (int64_t)1 << 31) return CHAM_ESHAPE;
+    BlockArgs a{};
+    a.M = (int)M;
+    a.N = (int)N;
+    a.K = (int)K;
+    a.nkb = (a.K + BK - 1) / BK;
+    const bool half = y_type == CHAM_T_F32;
+    if (few_rows(a, half)) {
+        out[0] = out[1] = 16;
+        out[2] = 8;
+        return CHAM_OK;
+    }
+    const TileCost& c = (half ? kCostHalf : kCostCodes)[plan_tile(a, half ? kCostHalf : kCostCodes)];
+    out[0] = c.bm;
+    out[1] = c.bn;
+    out[2] = c.ks;
+    return CHAM_OK;
+}

@@ -302,6 +302,7 @@ CHAM_DEV uint32_t act_codes4_mx(const float4& t, int* Eout) {
 }  // namespace cham
 
 // host-side helpers shared by the entry points
+int cham_device_cus();  // compute units of the current device (256 if none is visible)
 #define CHAM_CHECK_LAUNCH()                                     \
     do {                                                        \
         if (hipGetLastError() != hipSuccess) return CHAM_EHIP; \

@@ -44,7 +44,6 @@
 //
 // The MFMA contracts over k in any order as long as both operands agree: lane half h of a
 // k-step takes k = 32h .. 32h+31, sub-step s the 8 k at 32h + 8s.
-#include <atomic>
 #include <cmath>
 #include <vector>
 
@@ -902,20 +901,6 @@ __global__ __launch_bounds__(256) void reduce_kernel(const float* __restrict__ p
 
 // ---- launch plan: one launch of one tile shape, optionally split along k into partial
 // outputs that reduce_kernel sums (for layers with too few output tiles to fill the CUs).
-// CU count of the current device, queried once per device (every thread that races to
-// fill the cache stores the same value, so relaxed atomics suffice)
-int cu_count() {
-    static std::atomic<int> cached[64];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-    int n = cached[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
-        cached[dev].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
-
 // Modeled time (us) of a launch of one tile shape: a fixed cost (prologue, tail), plus the
 // k-steps of the rounds of workgroups, each at the k-step time of as many workgroups per CU as
 // the round puts there -- the workgroups of later rounds start while earlier ones finish --
@@ -965,7 +950,7 @@ double output_cost(int64_t M, int64_t N, int splits) {
 }
 
 Plan plan_gemm(int M, int N, int K) {
-    const int P = cu_count();
+    const int P = cham_device_cus();
     const int nsteps = K / BK;
     double best = 1e300;
     Plan plan{0, 1};

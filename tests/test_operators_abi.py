@@ -1,0 +1,165 @@
+"""CPU checks of the operators around 8-bit linear layers: their argument errors (no kernel is
+launched by these calls), the binding's refusals, and the product's launch plans."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2609_33496_amd import cham
+
+P = ctypes.c_void_p
+NAN, INF = float("nan"), float("inf")
+
+
+def _norm(**kw):
+    d = dict(M=4, K=64, x=64, ldx=64, r=128, ldr=64, h=256, ldh=64, g=512, x_type=2, r_type=2, g_type=0, eps=1e-6)
+    d.update(kw)
+    return cham._Norm(*[d[k] for k, _ in cham._Norm._fields_])
+
+
+def _gate(**kw):
+    d = dict(M=4, K=64, x=64, ldx=64, u=128, ldu=64, type=1, act=1)
+    d.update(kw)
+    return cham._Gate(*[d[k] for k, _ in cham._Gate._fields_])
+
+
+def _bq(**kw):
+    d = dict(M=4, K=64, pow2=0, codes=64, scale=64)
+    d.update(kw)
+    return cham._BQ(*[d[k] for k, _ in cham._BQ._fields_])
+
+
+def _bw(**kw):
+    d = dict(N=4, K=64, pow2=0, codes=64, scale=64)
+    d.update(kw)
+    return cham._BW(*[d[k] for k, _ in cham._BW._fields_])
+
+
+def _aq(**kw):
+    d = dict(M=4, K=64, fmt=0, nsamples=4, codes=64, e8m0=64, scale=64, zero=64)
+    d.update(kw)
+    return cham._AQ(*[d[k] for k, _ in cham._AQ._fields_])
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(M=-1), cham.EINVAL), (dict(K=0), cham.EINVAL), (dict(K=48), cham.ESHAPE), (dict(K=32800), cham.ESHAPE),
+    (dict(M=1 << 31), cham.ESHAPE), (dict(x=None), cham.EINVAL), (dict(x=68), cham.EINVAL), (dict(ldx=63), cham.EINVAL),
+    (dict(ldx=68), cham.EINVAL),                       # a row of 136 bytes: not 16-byte aligned
+    (dict(x_type=3), cham.EFORMAT), (dict(r_type=1), cham.EFORMAT), (dict(g_type=7), cham.EFORMAT),
+    (dict(ldr=32), cham.EINVAL), (dict(r=None), cham.EINVAL),  # h without a residual
+    (dict(h=136), cham.EINVAL), (dict(h=128, ldh=72), cham.EINVAL),  # in place with another stride
+    (dict(g=520), cham.EINVAL), (dict(eps=-1.0), cham.EINVAL), (dict(eps=NAN), cham.EINVAL), (dict(eps=INF), cham.EINVAL),
+])
+def test_norm_refusals(kw, status):
+    L = cham.lib()
+    n = _norm(**kw)
+    K, M = max(0, n.K), max(0, n.M)
+    assert L.cham_rms_norm_quantize_block(ctypes.byref(n), ctypes.byref(_bq(M=n.M, K=n.K)), None) == status
+    assert L.cham_rms_norm_quantize(ctypes.byref(n), 1, ctypes.byref(_aq(M=n.M, K=n.K, nsamples=min(M, 100))), None) == status
+    assert K >= 0
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(M=5), cham.EINVAL), (dict(K=96), cham.EINVAL), (dict(codes=None), cham.EINVAL), (dict(codes=72), cham.EINVAL),
+    (dict(scale=None), cham.EINVAL), (dict(scale=66), cham.EINVAL), (dict(pow2=2), cham.EINVAL),
+])
+def test_block_output_refusals(kw, status):
+    L = cham.lib()
+    q = _bq(**kw)
+    assert L.cham_rms_norm_quantize_block(ctypes.byref(_norm()), ctypes.byref(q), None) == status
+    assert L.cham_gated_quantize_block(ctypes.byref(_gate()), ctypes.byref(q), None) == status
+    assert L.cham_rms_norm_quantize_block(ctypes.byref(_norm()), None, None) == cham.EINVAL
+    assert L.cham_rms_norm_quantize_block(None, ctypes.byref(_bq()), None) == cham.EINVAL
+
+
+@pytest.mark.parametrize("fmt,kw,status", [
+    (1, dict(nsamples=1), cham.EINVAL), (1, dict(codes=68), cham.EINVAL), (1, dict(zero=None), cham.EINVAL),
+    (1, dict(scale=None), cham.EINVAL), (3, dict(e8m0=None), cham.EINVAL), (5, dict(), cham.EFORMAT),
+    (-1, dict(), cham.EFORMAT), (16, dict(), cham.EFORMAT), (0, dict(K=96), cham.EINVAL),
+])
+def test_token_output_refusals(fmt, kw, status):
+    L = cham.lib()
+    q = _aq(**kw)
+    assert L.cham_rms_norm_quantize(ctypes.byref(_norm()), fmt, ctypes.byref(q), None) == status
+    assert L.cham_gated_quantize(ctypes.byref(_gate()), fmt, ctypes.byref(q), None) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(M=-1), cham.EINVAL), (dict(K=40), cham.ESHAPE), (dict(type=3), cham.EFORMAT), (dict(act=4), cham.EFORMAT),
+    (dict(act=-1), cham.EFORMAT), (dict(x=None), cham.EINVAL), (dict(u=132), cham.EINVAL), (dict(ldu=60), cham.EINVAL),
+    (dict(ldx=65), cham.EINVAL),
+])
+def test_gate_refusals(kw, status):
+    g = _gate(**kw)
+    assert cham.lib().cham_gated_quantize_block(ctypes.byref(g), ctypes.byref(_bq(M=g.M, K=g.K)), None) == status
+
+
+def test_long_rows_only_where_a_row_is_not_held():
+    """A scale per token needs the whole row in registers; the block and MX formats do not."""
+    L = cham.lib()
+    g = _gate(M=0, K=65536, ldx=65536, ldu=65536)
+    assert L.cham_gated_quantize(ctypes.byref(g), 1, ctypes.byref(_aq(M=0, K=65536, nsamples=0)), None) == cham.ESHAPE
+    assert L.cham_gated_quantize(ctypes.byref(g), 3, ctypes.byref(_aq(M=0, K=65536, nsamples=0)), None) == cham.OK
+    assert L.cham_gated_quantize_block(ctypes.byref(g), ctypes.byref(_bq(M=0, K=65536)), None) == cham.OK
+
+
+@pytest.mark.parametrize("kw,ty,ldw,status", [
+    (dict(N=0), 0, 64, cham.EINVAL), (dict(K=48), 0, 64, cham.ESHAPE), (dict(), 3, 64, cham.EFORMAT),
+    (dict(), 0, 62, cham.EINVAL), (dict(), 0, 66, cham.EINVAL), (dict(codes=None), 0, 64, cham.EINVAL),
+    (dict(scale=65), 0, 64, cham.EINVAL), (dict(pow2=3), 0, 64, cham.EINVAL),
+])
+def test_weights_refusals(kw, ty, ldw, status):
+    L = cham.lib()
+    assert L.cham_block_quantize_weights(P(64), ty, ldw, ctypes.byref(_bw(**kw)), None) == status
+    assert L.cham_block_quantize_weights(None, 0, 64, ctypes.byref(_bw()), None) == cham.EINVAL
+    assert L.cham_block_quantize_weights(P(64), 0, 64, None, None) == cham.EINVAL
+
+
+@pytest.mark.parametrize("x,w,Y,ty,ldy,status", [
+    (dict(M=-1), {}, 64, 0, 4, cham.EINVAL), ({}, dict(N=0), 64, 0, 4, cham.EINVAL), (dict(K=128), {}, 64, 0, 4, cham.EINVAL),
+    (dict(K=48), dict(K=48), 64, 0, 4, cham.ESHAPE), (dict(K=(1 << 20) + 32), dict(K=(1 << 20) + 32), 64, 0, 4, cham.ESHAPE),
+    (dict(pow2=1), {}, 64, 0, 4, cham.EINVAL),        # the two kinds of scales are not mixed
+    (dict(pow2=2), dict(pow2=2), 64, 0, 4, cham.EINVAL), (dict(codes=72), {}, 64, 0, 4, cham.EINVAL),
+    ({}, dict(codes=72), 64, 0, 4, cham.EINVAL), (dict(scale=None), {}, 64, 0, 4, cham.EINVAL),
+    ({}, dict(scale=66), 64, 0, 4, cham.EINVAL), ({}, {}, 64, 3, 4, cham.EFORMAT), ({}, {}, None, 0, 4, cham.EINVAL),
+    ({}, {}, 66, 0, 4, cham.EINVAL), ({}, {}, 65, 1, 4, cham.EINVAL), ({}, {}, 64, 0, 3, cham.EINVAL),
+    (dict(M=0), {}, None, 0, 4, cham.OK),
+])
+def test_linear_refusals(x, w, Y, ty, ldy, status):
+    L = cham.lib()
+    assert L.cham_block_linear(ctypes.byref(_bq(**x)), ctypes.byref(_bw(**w)), P(Y), ty, ldy, None) == status
+    assert L.cham_block_linear(None, ctypes.byref(_bw()), P(64), 0, 4, None) == cham.EINVAL
+    assert L.cham_block_linear(ctypes.byref(_bq()), None, P(64), 0, 4, None) == cham.EINVAL
+
+
+def test_binding_refuses_host_tensors_and_wrong_shapes():
+    x = torch.zeros(4, 64)
+    for call in (lambda: cham.rms_norm_quantize(x), lambda: cham.gated_quantize(x), lambda: cham.block_quantize_weights(x)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    with pytest.raises(ValueError, match="float32, float16 or bfloat16"):
+        cham.gated_quantize(x.double())
+    with pytest.raises(ValueError, match="codes"):
+        cham.BQ(4, 64, torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(1, 4)).struct()
+
+
+def test_every_plan_has_a_kernel_and_covers_the_chip():
+    """Plans over a grid of sizes: one of the tiles that exist for the output's type; never the
+    largest tile where it would leave most of the chip idle."""
+    kinds = {torch.bfloat16: {(16, 16, 8), (256, 256, 1), (128, 128, 1), (64, 64, 1), (64, 64, 2), (32, 64, 1), (32, 64, 2)},
+             torch.float32: {(16, 16, 8), (64, 128, 1), (64, 64, 1), (64, 64, 2), (32, 64, 1), (32, 64, 2)}}
+    for dt, known in kinds.items():
+        seen = set()
+        for M in (1, 8, 16, 17, 64, 240, 512, 1000, 2048, 8192, 16384):
+            for N in (1, 64, 640, 1152, 1280, 4608, 10240, 16384):
+                for K in (32, 96, 640, 1280, 5120, 16384):
+                    p = cham.block_linear_plan(M, N, K, dt)
+                    assert p in known, (M, N, K, dt, p)
+                    if p[0] == 256:
+                        assert M * N >= 64 * 65536, (M, N, K)
+                    seen.add(p)
+        assert seen == known, known - seen
+    assert cham.block_linear_plan(512, 640, 640, torch.float16) == cham.block_linear_plan(512, 640, 640, torch.bfloat16)
+    for bad in ((0, 64, 64), (64, 64, 48)):
+        with pytest.raises(cham.ChamError):
+            cham.block_linear_plan(*bad)
