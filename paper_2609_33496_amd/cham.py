@@ -741,24 +741,28 @@ def _cdiv(a: int, b: int) -> int:
 
 def _scales(scale, rows, cols, codes, n, k) -> int:
     """Check a block-format pair of tensors; whether its scales are powers of two."""
-    if codes.dtype != torch.uint8 or codes.shape != (n, k) or not codes.is_contiguous() or not codes.is_cuda:
+    if codes.dtype is not torch.uint8 or codes.shape != (n, k) or not codes.is_contiguous() or not codes.is_cuda:
         raise ValueError(f"codes must be a contiguous device uint8 [{n}, {k}]")
-    pow2 = scale.dtype == torch.uint8
-    if (not pow2 and scale.dtype != torch.float32) or scale.shape != (rows, cols) or not scale.is_contiguous():
+    pow2 = scale.dtype is torch.uint8
+    if (not pow2 and scale.dtype is not torch.float32) or scale.shape != (rows, cols) or not scale.is_contiguous():
         raise ValueError(f"scale must be a contiguous float32 or uint8 [{rows}, {cols}]")
     if scale.device != codes.device:
         raise ValueError("codes and scale must be on one device")
     return int(pow2)
 
 
+def _scale_type(pow2):
+    return torch.uint8 if pow2 else torch.float32
+
+
 def alloc_bq(M: int, K: int, device="cuda", pow2: bool = False) -> BQ:
     return BQ(M, K, torch.empty((M, K), dtype=torch.uint8, device=device),
-              torch.empty((_cdiv(K, BLOCK), M), dtype=torch.uint8 if pow2 else torch.float32, device=device))
+              torch.empty((_cdiv(K, BLOCK), M), dtype=_scale_type(pow2), device=device))
 
 
 def alloc_bw(N: int, K: int, device="cuda", pow2: bool = False) -> BW:
     return BW(N, K, torch.empty((N, K), dtype=torch.uint8, device=device),
-              torch.empty((_cdiv(N, BLOCK), _cdiv(K, BLOCK)), dtype=torch.uint8 if pow2 else torch.float32, device=device))
+              torch.empty((_cdiv(N, BLOCK), _cdiv(K, BLOCK)), dtype=_scale_type(pow2), device=device))
 
 
 def _matrix(t: torch.Tensor, name: str, shape=None, device=None) -> int:
@@ -780,60 +784,57 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-class _On:
-    """The launch stream, with its device current.  What a call allocates comes from that
-    stream's pool: memory of another stream's pool may still be in use there."""
-    __slots__ = ("device", "stream", "prev")
-
-    def __init__(self, device, stream):
-        if stream is not None and stream.device != device:
-            raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
-        self.device, self.stream, self.prev = device, stream, None
-
-    def __enter__(self):
-        if self.device.index != torch.cuda.current_device():
-            self.prev = torch.cuda.current_device()
-            torch.cuda.set_device(self.device)
-        return (self.stream or torch.cuda.current_stream(self.device)).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.prev is not None:
-            torch.cuda.set_device(self.prev)
-
-    def alloc(self, make, *args, **kw):
-        if self.stream is None:
-            return make(*args, **kw)
-        with torch.cuda.stream(self.stream):
-            return make(*args, **kw)
+# the current device and its current stream's handle, without the stream object that
+# torch.cuda.current_stream makes (2 us of the host's time in front of a 3 us launch)
+_device_now = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_stream_now = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
-def _out_of(out, fmt, M, K, device, pow2, on):
-    """The output descriptor of a row pass: the caller's, else a new one."""
-    block = fmt == A_BLOCK128
+def _on_device(dev, stream, call, *args):
+    """call(*args, stream handle) with the tensors' device current."""
+    if stream is None and dev.index == _device_now():
+        return call(*args, _stream_now(dev.index))
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"stream is on {stream.device}, the tensors on {dev}")
+    with torch.cuda.device(dev):
+        return call(*args, _stream_now(dev.index) if stream is None else stream.cuda_stream)
+
+
+def _empty(shape, dtype, dev, stream):
+    """Memory of the launch stream's pool: that of another stream's may still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _row_out(out, fmt, M, K, dev, pow2, stream):
+    """The output of a row pass (the caller's, else a new one) and its C descriptor."""
+    if fmt == A_BLOCK128:
+        if out is None:
+            out = BQ(M, K, _empty((M, K), torch.uint8, dev, stream), _empty((_cdiv(K, BLOCK), M), _scale_type(pow2), dev, stream))
+            return out, _BQ(M, K, int(bool(pow2)), out.codes.data_ptr(), out.scale.data_ptr())
+        if not isinstance(out, BQ) or (out.M, out.K) != (M, K) or out.codes.device != dev:
+            raise ValueError(f"out must be a BQ of shape ({M}, {K}) on {dev}")
+        if (out.scale.dtype is torch.uint8) != bool(pow2):
+            raise ValueError("out's scales are not of the kind pow2 asks for")
+        return out, out.struct()
+    mx = fmt in (A_MXFP8, A_MXINT8)
     if out is None:
-        if block:
-            out = on.alloc(alloc_bq, M, K, device, pow2)
-        else:
-            out = on.alloc(alloc_aq, M, K, device, with_e8m0=fmt in (A_MXFP8, A_MXINT8), nsamples=M)
-    elif isinstance(out, BQ) != block or (out.M, out.K) != (M, K) or out.codes.device != device:
-        raise ValueError("out must be a %s of shape (%d, %d) on %s" % ("BQ" if block else "AQ", M, K, device))
-    elif block and (out.scale.dtype == torch.uint8) != bool(pow2):
-        raise ValueError("out's scales are not of the kind pow2 asks for")
-    elif not block:
-        _check_token_aq(out, fmt)
-    return out, block
-
-
-def _check_token_aq(out, fmt):
-    M, K = out.M, out.K
-    if out.codes.shape != (M, K) or out.codes.dtype != torch.uint8 or not out.codes.is_contiguous():
+        out = AQ(M, K, fmt, _empty((M, K), torch.uint8, dev, stream), _empty((M, K // 32), torch.uint8, dev, stream) if mx else None,
+                 _empty(M, torch.float32, dev, stream), _empty(M, torch.float32, dev, stream), M)
+        return out, out.struct()
+    if not isinstance(out, AQ) or (out.M, out.K) != (M, K) or out.codes.device != dev:
+        raise ValueError(f"out must be an AQ of shape ({M}, {K}) on {dev}")
+    if out.codes.shape != (M, K) or out.codes.dtype is not torch.uint8 or not out.codes.is_contiguous():
         raise ValueError(f"out.codes must be a contiguous uint8 [{M}, {K}]")
     for t in (out.scale, out.zero):
-        if t.shape != (M,) or t.dtype != torch.float32 or not t.is_contiguous():
+        if t.shape != (M,) or t.dtype is not torch.float32 or not t.is_contiguous() or t.device != dev:
             raise ValueError(f"out.scale and out.zero must be contiguous float32 [{M}] (one scale per token)")
-    if fmt in (A_MXFP8, A_MXINT8) and (out.e8m0 is None or out.e8m0.shape != (M, K // 32) or
-                                       out.e8m0.dtype != torch.uint8 or not out.e8m0.is_contiguous()):
+    if mx and (out.e8m0 is None or out.e8m0.shape != (M, K // 32) or out.e8m0.dtype is not torch.uint8 or
+               not out.e8m0.is_contiguous() or out.e8m0.device != dev):
         raise ValueError(f"out.e8m0 must be a contiguous uint8 [{M}, {K // 32}]")
+    return out, out.struct()
 
 
 def rms_norm_quantize(X: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6, *,
@@ -846,34 +847,34 @@ def rms_norm_quantize(X: torch.Tensor, weight: Optional[torch.Tensor] = None, ep
     xt = _matrix(X, "X")
     M, K = X.shape
     dev = X.device
-    on = _On(dev, stream)
-    rt = r_ptr = ldr = h_ptr = ldh = 0
+    rt = r_ptr = ldr = h_ptr = ldh = gt = g_ptr = 0
     if residual is not None:
         rt = _matrix(residual, "residual", X.shape, dev)
         r_ptr, ldr = residual.data_ptr(), _ld(residual)
         if residual_out is None:
-            residual_out = on.alloc(torch.empty, (M, K), dtype=residual.dtype, device=dev)
+            residual_out = _empty((M, K), residual.dtype, dev, stream)
+            ldh = K
         elif _matrix(residual_out, "residual_out", X.shape, dev) != rt:
             raise ValueError("residual_out must have the residual's type")
-        h_ptr, ldh = residual_out.data_ptr(), _ld(residual_out)
+        else:
+            ldh = _ld(residual_out)
+        h_ptr = residual_out.data_ptr()
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
-    gt = g_ptr = 0
     if weight is not None:
         gt = _TYPES.get(weight.dtype, -1)
         if gt < 0 or weight.shape != (K,) or weight.device != dev or not weight.is_contiguous():
             raise ValueError(f"weight must be a contiguous float32, float16 or bfloat16 [{K}] on {dev}")
         g_ptr = weight.data_ptr()
-    out, block = _out_of(out, fmt, M, K, dev, pow2, on)
+    out, st = _row_out(out, fmt, M, K, dev, pow2, stream)
     n = _Norm(M, K, X.data_ptr(), _ld(X), r_ptr, ldr, h_ptr, ldh, g_ptr, xt, rt, gt, eps)
-    st = out.struct()
-    with on as s:
-        if block:
-            rc = lib().cham_rms_norm_quantize_block(ctypes.byref(n), ctypes.byref(st), s)
-        else:
-            rc = lib().cham_rms_norm_quantize(ctypes.byref(n), fmt, ctypes.byref(st), s)
-            out.fmt = fmt
+    if fmt == A_BLOCK128:
+        rc = _on_device(dev, stream, lib().cham_rms_norm_quantize_block, ctypes.byref(n), ctypes.byref(st))
+    else:
+        rc = _on_device(dev, stream, lib().cham_rms_norm_quantize, ctypes.byref(n), fmt, ctypes.byref(st))
     _check(rc, "rms_norm_quantize")
+    if fmt != A_BLOCK128:
+        out.fmt, out.nsamples = fmt, M
     return out, residual_out
 
 
@@ -884,22 +885,20 @@ def gated_quantize(X: torch.Tensor, up: Optional[torch.Tensor] = None, act: int 
     xt = _matrix(X, "X")
     M, K = X.shape
     dev = X.device
-    on = _On(dev, stream)
     u_ptr = ldu = 0
     if up is not None:
         if _matrix(up, "up", X.shape, dev) != xt:
             raise ValueError("X and up must have one type")
         u_ptr, ldu = up.data_ptr(), _ld(up)
-    out, block = _out_of(out, fmt, M, K, dev, pow2, on)
+    out, st = _row_out(out, fmt, M, K, dev, pow2, stream)
     g = _Gate(M, K, X.data_ptr(), _ld(X), u_ptr, ldu, xt, act)
-    st = out.struct()
-    with on as s:
-        if block:
-            rc = lib().cham_gated_quantize_block(ctypes.byref(g), ctypes.byref(st), s)
-        else:
-            rc = lib().cham_gated_quantize(ctypes.byref(g), fmt, ctypes.byref(st), s)
-            out.fmt = fmt
+    if fmt == A_BLOCK128:
+        rc = _on_device(dev, stream, lib().cham_gated_quantize_block, ctypes.byref(g), ctypes.byref(st))
+    else:
+        rc = _on_device(dev, stream, lib().cham_gated_quantize, ctypes.byref(g), fmt, ctypes.byref(st))
     _check(rc, "gated_quantize")
+    if fmt != A_BLOCK128:
+        out.fmt, out.nsamples = fmt, M
     return out
 
 
@@ -907,14 +906,16 @@ def block_quantize_weights(W: torch.Tensor, pow2: bool = False, out: Optional[BW
     """W [N, K] (rows may be strided) in the block format: a scale for each 128 x 128 block."""
     ty = _matrix(W, "W")
     N, K = W.shape
-    on = _On(W.device, stream)
+    dev = W.device
     if out is None:
-        out = on.alloc(alloc_bw, N, K, W.device, pow2)
-    elif (out.N, out.K) != (N, K) or out.codes.device != W.device or (out.scale.dtype == torch.uint8) != bool(pow2):
+        out = BW(N, K, _empty((N, K), torch.uint8, dev, stream),
+                 _empty((_cdiv(N, BLOCK), _cdiv(K, BLOCK)), _scale_type(pow2), dev, stream))
+        st = _BW(N, K, int(bool(pow2)), out.codes.data_ptr(), out.scale.data_ptr())
+    elif (out.N, out.K) != (N, K) or out.codes.device != dev or (out.scale.dtype is torch.uint8) != bool(pow2):
         raise ValueError("out does not fit W and pow2")
-    st = out.struct()
-    with on as s:
-        rc = lib().cham_block_quantize_weights(W.data_ptr(), ty, _ld(W), ctypes.byref(st), s)
+    else:
+        st = out.struct()
+    rc = _on_device(dev, stream, lib().cham_block_quantize_weights, W.data_ptr(), ty, _ld(W), ctypes.byref(st))
     _check(rc, "block_quantize_weights")
     return out
 
@@ -924,15 +925,17 @@ def block_linear(xb: BQ, wb: BW, Y: Optional[torch.Tensor] = None, dtype: torch.
     """Y [M, N] = activations times weights^T, both in the block format; Y (rows may be strided)
     decides the type where it is given, else dtype."""
     dev = xb.codes.device
+    a, w = xb.struct(), wb.struct()
     if wb.codes.device != dev:
         raise ValueError(f"the weights must be on {dev}")
-    on = _On(dev, stream)
     if Y is None:
-        Y = on.alloc(torch.empty, (xb.M, wb.N), dtype=dtype, device=dev)
-    ty = _matrix(Y, "Y", (xb.M, wb.N), dev)
-    a, w = xb.struct(), wb.struct()
-    with on as s:
-        rc = lib().cham_block_linear(ctypes.byref(a), ctypes.byref(w), Y.data_ptr(), ty, _ld(Y), s)
+        ty, ld = _TYPES.get(dtype), wb.N
+        if ty is None:
+            raise ValueError("dtype must be float32, float16 or bfloat16")
+        Y = _empty((xb.M, ld), dtype, dev, stream)
+    else:
+        ty, ld = _matrix(Y, "Y", (xb.M, wb.N), dev), _ld(Y)
+    rc = _on_device(dev, stream, lib().cham_block_linear, ctypes.byref(a), ctypes.byref(w), Y.data_ptr(), ty, ld)
     _check(rc, "block_linear")
     return Y
 
