@@ -96,26 +96,11 @@ CHAM_DEV float4v mfma_half(half8v a, half8v b, float4v c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-CHAM_DEV uint32_t bf16_bits(float x) {
-    const uint32_t u = __float_as_uint(x);
-    return (u & 0x7fffffffu) > 0x7f800000u ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
-}
-
 template <int YT>
 CHAM_DEV void store1(void* Y, int64_t i, float v) {
     if constexpr (YT == CHAM_T_F32) ((float*)Y)[i] = v;
     else if constexpr (YT == CHAM_T_F16) ((_Float16*)Y)[i] = (_Float16)v;
-    else ((uint16_t*)Y)[i] = (uint16_t)bf16_bits(v);
-}
-
-template <int YT>
-CHAM_DEV uint32_t pack2(float a, float b) {
-    if constexpr (YT == CHAM_T_F16) {
-        const half2v h = {(_Float16)a, (_Float16)b};
-        return __builtin_bit_cast(uint32_t, h);
-    } else {
-        return bf16_bits(a) | bf16_bits(b) << 16;
-    }
+    else ((__bf16*)Y)[i] = (__bf16)v;
 }
 
 // 4 and 8 consecutive channels of one row of Y
@@ -125,7 +110,7 @@ CHAM_DEV void store4(const BlockArgs& a, int64_t m, int64_t n, float4v p) {
     const int64_t i = m * a.ldy + n;
     if (a.vec && n + 4 <= a.N) {
         if constexpr (YT == CHAM_T_F32) *(float4v*)((float*)a.Y + i) = p;
-        else *(uint2*)((uint16_t*)a.Y + i) = make_uint2(pack2<YT>(p[0], p[1]), pack2<YT>(p[2], p[3]));
+        else *(uint2*)((uint16_t*)a.Y + i) = make_uint2(narrow<YT>(p[0], p[1]), narrow<YT>(p[2], p[3]));
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -140,8 +125,8 @@ CHAM_DEV void store8(const BlockArgs& a, int64_t m, int64_t n, float4v p, float4
             *(float4v*)((float*)a.Y + i) = p;
             *(float4v*)((float*)a.Y + i + 4) = q;
         } else {
-            *(uint4*)((uint16_t*)a.Y + i) = make_uint4(pack2<YT>(p[0], p[1]), pack2<YT>(p[2], p[3]), pack2<YT>(q[0], q[1]),
-                                                       pack2<YT>(q[2], q[3]));
+            *(uint4*)((uint16_t*)a.Y + i) = make_uint4(narrow<YT>(p[0], p[1]), narrow<YT>(p[2], p[3]), narrow<YT>(q[0], q[1]),
+                                                       narrow<YT>(q[2], q[3]));
         }
     } else {
 #pragma unroll
@@ -176,6 +161,8 @@ struct Tile {
     static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, KS = KS_;
     static constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN, kWaves = WM * WN;
     static constexpr int kLoadsX = BM / 8 / kWaves, kLoadsW = BN / 8 / kWaves;  // 1 KB each
+    static constexpr int kLoads = kLoadsX + kLoadsW;
+    static constexpr bool kSpread = TM * TN >= 16;  // loads of a step spread over its products
     static_assert(kWaves % 4 == 0 && TN % 2 == 0 && 128 % (16 * TN) == 0 && BN <= 256, "layout");
     static_assert(KS == 1 || BM <= 64, "a group's sums fit its slices of two weight buffers");
 };
@@ -240,15 +227,18 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
     uint32_t offx = (uint32_t)r0 * K + cx0 * 16, offw = (uint32_t)r0 * K + cw0 * 16;
     const bool lastx = (nkb - 1) * BK + cx0 * 16 >= K, lastw = (nkb - 1) * BK + cw0 * 16 >= K;
     const uint32_t rstep = (uint32_t)T::kWaves * 8 * K;
-    auto issue = [&](const __amdgpu_buffer_rsrc_t& r, Lds* buf, int loads, uint32_t off, bool past, int kb) {
-        const uint32_t o = kb >= nkb || (kb == nkb - 1 && past) ? kOutside : off;
-#pragma unroll
-        for (int i = 0; i < loads; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                r, (__attribute__((address_space(3))) void*)(buf + (i * T::kWaves + wave) * 1024), 16, o + i * rstep, kb * BK, 0, 0);
+    // load i of a step: its weights first, then its activations
+    auto issue = [&](Lds* x, Lds* w, int i, int kb) {
+        const bool isx = i >= T::kLoadsW, past = kb >= nkb || (kb == nkb - 1 && (isx ? lastx : lastw));
+        const int j = isx ? i - T::kLoadsW : i;
+        Lds* const to = (isx ? x + group * kX : w + group * kW) + (j * T::kWaves + wave) * 1024;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(isx ? rx : rw, (__attribute__((address_space(3))) void*)to, 16,
+                                                 (past ? kOutside : isx ? offx : offw) + j * rstep, kb * BK, 0, 0);
     };
-    auto issue_x = [&](Lds* buf, int kb) { issue(rx, buf + group * kX, T::kLoadsX, offx, lastx, kb); };
-    auto issue_w = [&](Lds* buf, int kb) { issue(rw, buf + group * kW, T::kLoadsW, offw, lastw, kb); };
+    auto issue_all = [&](Lds* x, Lds* w, int kb) {
+#pragma unroll
+        for (int i = 0; i < T::kLoads; ++i) issue(x, w, i, kb);
+    };
 
     // scales of the lane's rows (one per 16-row block) and of the wavefront's channels
     const int rr = lane & 15, g = lane >> 4;
@@ -294,7 +284,7 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
     // The group's step j: X and W hold it, X and Wn take its step j + 2.
     auto step = [&](Lds* X, const Lds* W, Lds* Wn, Factors& s, int j) {
         const int next = __builtin_amdgcn_readfirstlane((j + 2) * KS + group);
-        landed_barrier<T::kLoadsX + T::kLoadsW + TM + 1>();  // step j is there; W of step j - 1 is free
+        landed_barrier<T::kLoads + TM + 1>();  // step j is there; W of step j - 1 is free
         float f[TM];
         Scale cx[TM], cw = s.w;
 #pragma unroll
@@ -302,69 +292,100 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
             cx[t] = s.x[t];
             if constexpr (MODE != kCodesPow2) f[t] = factor(cx[t]) * factor(cw);
         }
-        Codes bc[TM];
+        Codes b[TM];
 #pragma unroll
-        for (int t = 0; t < TM; ++t) bc[t] = operand(X, xlo, xhi, t * 16 * BK);
+        for (int t = 0; t < TM; ++t) b[t] = operand(X, xlo, xhi, t * 16 * BK);
         Codes w[2];
         w[0] = operand(W, wlo, whi, 0);
         asm volatile("" : "+v"(offx), "+v"(offw));  // keeps the sums of issue() from living in registers
         scales(s, next);
-        issue_w(Wn, next);
-        read_barrier();  // X is in registers everywhere
-        issue_x(X, next);
-        // Operand block i + 1 is read from LDS while block i is multiplied; a product waits kLag
-        // others before it is scaled and added, so that no instruction waits for the one before
-        // it.  The scheduling fences keep the compiler from gathering all reads in front (more
-        // registers than there are).
-        Operand<MODE> b[TM];
+        if constexpr (!T::kSpread) {
 #pragma unroll
-        for (int t = 0; t < TM; ++t) b[t] = operand_as(bc[t], (const Operand<MODE>*)nullptr);
-        constexpr int kLag = exact(MODE) ? 0 : 3;
-        float4v d[exact(MODE) ? TM : 4];
-        auto add = [&](int j) {
-            const int i = j / TM, t = j % TM;
-            const float4v p = d[j % (exact(MODE) ? TM : 4)];
+            for (int l = 0; l < T::kLoads; ++l) {
+                if (l == T::kLoadsW) read_barrier();
+                issue(X, Wn, l, next);
+            }
+        }
+        // Operand block i + 1 is read from LDS while block i is multiplied, and 8-bit products are
+        // scaled and added behind later ones, so that no instruction waits for the one before it.  The scheduling groups interleave matrix and
+        // vector instructions evenly (16 additions behind 4 products left the matrix cores idle
+        // in between: 8192 x 8192 x 8192 in 256 x 256 tiles 476 us -> 455); the fences keep the
+        // compiler from gathering all reads in front (more registers than there are).
+        auto add = [&](int i, int t, const float4v& p) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) acc[i][t][q] = __builtin_fmaf(p[q], f[t], acc[i][t][q]);
         };
+        // The loads of step j + 2 go out between the products, a few at a time: all at once they
+        // hold up the wavefront until the memory pipe has taken them (1 KB each, 16 cycles or
+        // more; the same product 502 us -> 476).
+        auto spread = [&](int i) {
+            if constexpr (T::kSpread) {
 #pragma unroll
-        for (int i = 0; i < TN; ++i) {
-            if (i + 1 < TN) w[(i + 1) & 1] = operand(W, wlo, whi, chan(i + 1, 0) * BK);
-            const Operand<MODE> a = operand_as(w[i & 1], (const Operand<MODE>*)nullptr);
-            const int j = i * TM;
-            if constexpr (exact(MODE)) {
-                float4v* e = d;
+                for (int l = i * T::kLoads / TN; l < (i + 1) * T::kLoads / TN; ++l) {
+                    if (l == T::kLoadsW) read_barrier();  // X is in registers everywhere
+                    issue(X, Wn, l, next);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        const float4v zero = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (exact(MODE)) {
+            Halves hb[TM];
+#pragma unroll
+            for (int t = 0; t < TM; ++t) hb[t] = to_half(b[t]);
+            float4v d[TM];
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+                if (i + 1 < TN) w[(i + 1) & 1] = operand(W, wlo, whi, chan(i + 1, 0) * BK);
+                const Halves hw = to_half(w[i & 1]);
 #pragma unroll
                 for (int h = 0; h < 4; ++h)
 #pragma unroll
-                    for (int t = 0; t < TM; ++t)
-                        e[t] = mfma_half(a.h[h], b[t].h[h], h == 0 ? float4v{0.0f, 0.0f, 0.0f, 0.0f} : e[t]);
-            }
+                    for (int t = 0; t < TM; ++t) d[t] = mfma_half(hw.h[h], hb[t].h[h], h == 0 ? zero : d[t]);
 #pragma unroll
-            for (int t = 0; t < TM; ++t) {
-                if constexpr (MODE == kCodesPow2) {
-                    acc[i][t] = mfma_pow2(a, b[t], acc[i][t], cw, cx[t]);
-                } else {
-                    if constexpr (MODE == kCodes) d[(j + t) & 3] = mfma(a, b[t], float4v{0.0f, 0.0f, 0.0f, 0.0f});
-                    if (j + t >= kLag) add(j + t - kLag);
+                for (int t = 0; t < TM; ++t) add(i, t, d[t]);
+                __builtin_amdgcn_sched_barrier(0);
+                spread(i);
+            }
+        } else {
+            constexpr int kLag = 3;  // products between one and its addition
+            float4v d[kLag + 1];
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+                if (i + 1 < TN) w[(i + 1) & 1] = operand(W, wlo, whi, chan(i + 1, 0) * BK);
+#pragma unroll
+                for (int t = 0; t < TM; ++t) {
+                    const int j = i * TM + t, k = j - kLag;
+                    if constexpr (MODE == kCodesPow2) {
+                        acc[i][t] = mfma_pow2(w[i & 1], b[t], acc[i][t], cw, cx[t]);
+                    } else {
+                        d[j & kLag] = mfma(w[i & 1], b[t], zero);
+                        if (k >= 0) add(k / TM, k % TM, d[k & kLag]);
+                    }
                 }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if constexpr (MODE != kCodesPow2) {
+                if constexpr (MODE == kCodes) {
 #pragma unroll
-            for (int j = TN * TM - kLag; j < TN * TM; ++j) add(j);
+                    for (int t = 0; t < TM; ++t) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                spread(i);
+            }
+            if constexpr (MODE == kCodes) {
+#pragma unroll
+                for (int k = TN * TM - kLag; k < TN * TM; ++k) add(k / TM, k % TM, d[k & kLag]);
+            }
         }
     };
 
     Lds *const x_0 = (Lds*)X0, *const x_1 = (Lds*)X1;
     Lds *const w_0 = (Lds*)W0, *const w_1 = (Lds*)W1, *const w_2 = (Lds*)W2;
     scales(s0, group);
-    issue_w(w_0, group);
-    issue_x(x_0, group);
+    issue_all(x_0, w_0, group);
     scales(s1, KS + group);
-    issue_w(w_1, KS + group);
-    issue_x(x_1, KS + group);
+    issue_all(x_1, w_1, KS + group);
     const int steps = (nkb + KS - 1) / KS;  // the same for all groups: steps past the last block are zeros
     for (int j = 0;; j += 6) {
         step(x_0, w_0, w_2, s0, j);
@@ -544,24 +565,25 @@ void launch_few(BlockArgs a, hipStream_t s) {
     hipLaunchKernelGGL((few_rows_kernel<TM, TN, NW, MODE, YT>), dim3((unsigned)(a.tm * a.tn)), dim3(NW * 64), 0, s, a);
 }
 
-// Modeled time (us) of one tile shape: tiles on the busiest CU, each its k-steps and a fixed part
-// (first loads, output).  Fitted to forced launches over 20 shapes (M 1 - 8192, N 640 - 10240,
-// K 1152 - 8192) with inputs that rotate through the last-level cache.
+// Modeled time (us) of one tile shape: the tiles of the busiest CU, each its k-steps and a fixed
+// part (first loads, output).  Fitted to 286 forced launches over 26 shapes (M 32 - 16384,
+// N 640 - 16384, K 320 - 8192; 3 sets of operands in turn); there the choice takes 0.6 % longer
+// than the best tile on average and 13 % at worst (8192 x 640 x 1920: 20.5 us against 18.1).
 struct TileCost {
     int bm, bn, ks;
     double lone, step, fixed;  // us: a k-step alone on a CU, among others, and the fixed part
 };
 enum { kT256, kT128, kT64, kT64x2, kT32, kT32x2, kTWide, kTiles };
 // 8-bit matrix instructions
-constexpr TileCost kCostCodes[kTiles] = {{256, 256, 1, 1.96, 1.96, 3.0}, {128, 128, 1, 0.67, 0.55, 1.8},
-                                         {64, 64, 1, 0.28, 0.205, 0.35}, {64, 64, 2, 0.46, 0.50, 0.6},
-                                         {32, 64, 1, 0.25, 0.137, 0.2},  {32, 64, 2, 0.36, 0.38, 0.3},
+constexpr TileCost kCostCodes[kTiles] = {{256, 256, 1, 1.13, 1.62, 6.0}, {128, 128, 1, 0.535, 0.492, 1.7},
+                                         {64, 64, 1, 0.28, 0.20, 0.44},  {64, 64, 2, 0.375, 0.437, 1.33},
+                                         {32, 64, 1, 0.24, 0.138, 0.30}, {32, 64, 2, 0.318, 0.267, 0.82},
                                          {0, 0, 0, 0, 0, 0}};
 // f16 matrix instructions
-constexpr TileCost kCostHalf[kTiles] = {{0, 0, 0, 0, 0, 0},             {0, 0, 0, 0, 0, 0},
-                                        {64, 64, 1, 0.43, 0.314, 0.55}, {64, 64, 2, 0.70, 0.77, 0.8},
-                                        {32, 64, 1, 0.33, 0.195, 0.4},  {32, 64, 2, 0.50, 0.43, 0.5},
-                                        {64, 128, 1, 0.65, 0.57, 1.0}};
+constexpr TileCost kCostHalf[kTiles] = {{0, 0, 0, 0, 0, 0},              {0, 0, 0, 0, 0, 0},
+                                        {64, 64, 1, 0.43, 0.306, 0.82},  {64, 64, 2, 0.666, 0.727, 1.66},
+                                        {32, 64, 1, 0.33, 0.20, 0.40},   {32, 64, 2, 0.493, 0.397, 0.98},
+                                        {64, 128, 1, 0.64, 0.551, 1.66}};
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 

@@ -299,6 +299,22 @@ CHAM_DEV uint32_t act_codes4_mx(const float4& t, int* Eout) {
     return w;
 }
 
+// ------------------------------------------------------------------------------------
+// 16-bit element types: two binary32 values rounded to nearest even (NaN stays NaN)
+// ------------------------------------------------------------------------------------
+template <int T>
+CHAM_DEV uint32_t narrow(float a, float b) {
+    if constexpr (T == CHAM_T_F16) {
+        typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+        const half2v h = {(_Float16)a, (_Float16)b};
+        return __builtin_bit_cast(uint32_t, h);
+    } else {
+        typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
+        const bf2v h = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(uint32_t, h);
+    }
+}
+
 }  // namespace cham
 
 // host-side helpers shared by the entry points

@@ -62,29 +62,19 @@ CHAM_DEV void widen(const Raw<T>& r, float (&v)[kChunk]) {
     }
 }
 
-// Rounded to nearest even; a NaN stays one (its mantissa's high bits, quiet).
-CHAM_DEV uint32_t bf16_bits(float x) {
-    const uint32_t u = __float_as_uint(x);
-    return (u & 0x7fffffffu) > 0x7f800000u ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
-}
-template <int T>
-CHAM_DEV uint32_t narrow2(float a, float b) {
-    if constexpr (T == CHAM_T_F16) {
-        const half2v h = {(_Float16)a, (_Float16)b};
-        return __builtin_bit_cast(uint32_t, h);
-    } else {
-        return bf16_bits(a) | bf16_bits(b) << 16;
-    }
-}
-
+// Stored past the caches: the residual is not read before the block's end, and its lines would
+// push out the codes that the next product reads (8192 x 1152, bfloat16 with a binary32 residual:
+// 25.9 us -> 21.8; the codes stored the same way too: 19.9, but the block of four operators
+// 172 -> 176).
 template <int T>
 CHAM_DEV void store8(void* p, int64_t i, const float (&v)[kChunk]) {
-    uint4* q = const_cast<uint4*>(at8<T>(p, i));
+    typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+    uint4v* q = (uint4v*)at8<T>(p, i);
     if constexpr (T == CHAM_T_F32) {
-        q[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        q[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        __builtin_nontemporal_store(uint4v{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, q);
+        __builtin_nontemporal_store(uint4v{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])}, q + 1);
     } else {
-        q[0] = make_uint4(narrow2<T>(v[0], v[1]), narrow2<T>(v[2], v[3]), narrow2<T>(v[4], v[5]), narrow2<T>(v[6], v[7]));
+        __builtin_nontemporal_store(uint4v{narrow<T>(v[0], v[1]), narrow<T>(v[2], v[3]), narrow<T>(v[4], v[5]), narrow<T>(v[6], v[7])}, q);
     }
 }
 
@@ -118,16 +108,26 @@ CHAM_DEV float gelu(float x) {
     return __builtin_fmaf(-z, q, fmaxf(x, 0.0f));
 }
 
-CHAM_DEV float activate(float x, int act) {
-    if (act == CHAM_ACT_NONE) return x;
-    if (act == CHAM_ACT_SILU) return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x));
-    if (act == CHAM_ACT_GELU) {
-        const float y = gelu(x);
-        return fabsf(x) < INFINITY ? y : x;  // NaN and infinities as they are
-    }
-    const float c = -2.0f * 0.79788456f * kLog2e;  // 2 sqrt(2/pi) log2(e)
-    const float w = c * __builtin_fmaf(0.044715f * x, x * x, x);
+CHAM_DEV float silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
+
+CHAM_DEV float gelu_tanh(float x) {
+    constexpr float c = -2.0f * 0.79788456f * kLog2e;  // 2 sqrt(2/pi) log2(e)
+    const float w = x * __builtin_fmaf(x * x, 0.044715f * c, c);
     return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w));
+}
+
+// one branch per chunk (a branch per element: 8192 x 4608 with GELU's tanh form 30.3 us)
+CHAM_DEV void activate(float (&y)[kChunk], int act) {
+    if (act == CHAM_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) y[j] = silu(y[j]);
+    } else if (act == CHAM_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) y[j] = gelu(y[j]);
+    } else if (act == CHAM_ACT_GELU_TANH) {
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) y[j] = gelu_tanh(y[j]);
+    }
 }
 
 // ------------------------------------------------------------------------------------
@@ -155,9 +155,19 @@ CHAM_DEV uint32_t max4(uint32_t v) { return dpp_maxu<0x4E>(dpp_maxu<0xB1>(v)); }
 
 constexpr uint32_t kInfBits = 0x7f800000u;
 
-// The scale of a block of maximum m (bits): its reciprocal, and the value that is stored.
+// a / 448, correctly rounded: the product with the reciprocal and one correction from the exact
+// remainder (equal to the IEEE quotient for every mantissa, checked exhaustively; a tenth of the
+// division's instructions).
+CHAM_DEV float div448(float a) {
+    constexpr float c = 1.0f / 448.0f;
+    const float q = a * c;
+    return __builtin_fmaf(__builtin_fmaf(-448.0f, q, a), c, q);
+}
+
+// The scale of a block of maximum m (bits): its reciprocal, and the value that is stored.  A
+// finite scale lies in [2^-126, 2^120), where the corrected estimate is the IEEE reciprocal.
 CHAM_DEV float block_scale(uint32_t m, bool pow2, uint32_t* stored) {
-    float s = floor_scale(__uint_as_float(m) / 448.0f);
+    float s = floor_scale(div448(__uint_as_float(m)));
     uint32_t u = __float_as_uint(s);
     if (pow2) {  // the exponent goes up where the mantissa is not zero
         u = (u + 0x7fffffu) & 0x7f800000u;
@@ -166,13 +176,21 @@ CHAM_DEV float block_scale(uint32_t m, bool pow2, uint32_t* stored) {
     }
     const bool bad = m >= kInfBits;
     *stored = bad ? (pow2 ? 255u : 0x7fc00000u) : u;
-    return rcp_rn(s);
+    const float r = __builtin_amdgcn_rcpf(s);
+    return __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r);
 }
 
 template <int FMT>
 CHAM_DEV uint2 codes8(const float (&y)[kChunk], float r, float z) {
     return make_uint2(act_codes4<FMT>(make_float4(y[0], y[1], y[2], y[3]), r, z),
                       act_codes4<FMT>(make_float4(y[4], y[5], y[6], y[7]), r, z));
+}
+
+// E4M3 codes of y r.  No clamp is needed: r is the rounded reciprocal of amax / 448 rounded, so
+// |y r| <= 448 (1 + 2^-22), which rounds to 448 (the next value of the grid would be 480).
+CHAM_DEV uint2 codes8_e4m3(const float (&y)[kChunk], float r) {
+    return make_uint2(pack_codes<CHAM_A_FP8_E4M3>(y[0] * r, y[1] * r, y[2] * r, y[3] * r, 0.0f),
+                      pack_codes<CHAM_A_FP8_E4M3>(y[4] * r, y[5] * r, y[6] * r, y[7] * r, 0.0f));
 }
 
 // Where a row pass writes
@@ -192,11 +210,12 @@ CHAM_DEV void put_codes(const Out& o, int64_t row, int c, uint2 w) {
     *(uint2*)(o.codes + row * o.K + (int64_t)c * kChunk) = w;
 }
 
-// A chunk of a block-format row; the 16 lanes of a block all come here (in: the chunk exists).
+// A chunk of a block-format row; the 16 lanes of a block all come here (in: the chunk exists and
+// is written; others take no part in the maximum).
 CHAM_DEV void emit_block(const Out& o, int64_t row, int c, bool in, const float (&y)[kChunk]) {
     uint32_t stored;
-    const float r = block_scale(max16(chunk_amax(y)), o.pow2 != 0, &stored);
-    const uint2 w = codes8<CHAM_A_FP8_E4M3>(y, r, 0.0f);
+    const float r = block_scale(max16(in ? chunk_amax(y) : 0u), o.pow2 != 0, &stored);
+    const uint2 w = codes8_e4m3(y, r);
     if (in) {
         put_codes(o, row, c, w);
         if ((c & 15) == 0) {
@@ -248,13 +267,6 @@ CHAM_DEV V team_reduce(V v, V* sh, F f) {
     return v;
 }
 
-// Workgroup -> group of consecutive rows: each XCD (workgroups go round the 8 XCDs) takes a
-// contiguous run, so that the block-major scales of neighbouring rows meet in one L2.
-CHAM_DEV int64_t xcd_run(int64_t b, int64_t n) {
-    const int64_t q = n >> 3, r = n & 7, x = b & 7, i = b >> 3;
-    return x * q + (x < r ? x : r) + i;
-}
-
 // Lanes per row T, chunks per lane V: rows of up to T V 8 elements.
 template <int T>
 constexpr int rows_per_wg() { return T == kWave ? 4 : 1; }
@@ -271,9 +283,9 @@ CHAM_DEV void emit_row(const Out& o, int64_t row, bool live, int lane, int nch, 
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
         if (v * T < nch) {
-            const uint32_t a = chunk_amax(y[v]);
-            m = m > a ? m : a;
             if (v * T + lane < nch) {
+                const uint32_t a = chunk_amax(y[v]);
+                m = m > a ? m : a;
 #pragma unroll
                 for (int j = 0; j < kChunk; ++j) {
                     lo = fminf(lo, y[v][j]);
@@ -302,7 +314,7 @@ CHAM_DEV void emit_row(const Out& o, int64_t row, bool live, int lane, int nch, 
         const int c = v * T + lane;
         if (live && c < nch) {
             if (o.fmt == CHAM_A_INT8_ASYM) put_codes(o, row, c, codes8<CHAM_A_INT8_ASYM>(y[v], r, z));
-            else if (o.fmt == CHAM_A_FP8_E4M3) put_codes(o, row, c, codes8<CHAM_A_FP8_E4M3>(y[v], r, z));
+            else if (o.fmt == CHAM_A_FP8_E4M3) put_codes(o, row, c, codes8_e4m3(y[v], r));
             else put_codes(o, row, c, codes8<CHAM_A_FP8_E5M2>(y[v], r, z));
         }
     }
@@ -345,9 +357,9 @@ struct NormArgs {
 // RT: type of the residual, or -1 for none
 template <int XT, int RT, int T, int OUT>
 __global__ __launch_bounds__(wg_threads<T>()) void norm_kernel(NormArgs a) {
-    __shared__ float sh[T > kWave ? T / kWave : 1];
+    __shared__ double sh[T > kWave ? T / kWave : 1];
     const int lane = threadIdx.x & (T - 1), nch = a.o.K / kChunk;
-    int64_t row = xcd_run(blockIdx.x, gridDim.x) * rows_per_wg<T>() + (T == kWave ? threadIdx.x / T : 0);
+    int64_t row = (int64_t)blockIdx.x * rows_per_wg<T>() + (T == kWave ? threadIdx.x / T : 0);
     const bool live = row < a.o.M;
     if (!live) row = a.o.M - 1;  // a repeat of the last row, not written
     constexpr int RR = RT < 0 ? XT : RT;
@@ -361,11 +373,10 @@ __global__ __launch_bounds__(wg_threads<T>()) void norm_kernel(NormArgs a) {
             if (RT >= 0) r[v] = load8<RR>(a.r, row * a.ldr + i);
         }
     }
-    float h[kV][kChunk], ss = 0.0f;
+    float h[kV][kChunk];
+    double ss = 0.0;
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) h[v][j] = 0.0f;
         if (v * T < nch && v * T + lane < nch) {
             widen<XT>(x[v], h[v]);
             if (RT >= 0) {
@@ -376,11 +387,12 @@ __global__ __launch_bounds__(wg_threads<T>()) void norm_kernel(NormArgs a) {
                 if (a.h && live) store8<RR>(a.h, row * a.ldh + (int64_t)(v * T + lane) * kChunk, h[v]);
             }
 #pragma unroll
-            for (int j = 0; j < kChunk; ++j) ss = __builtin_fmaf(h[v][j], h[v][j], ss);
+            for (int j = 0; j < kChunk; j += 4)  // pairs of pairs: a chunk's sum carries three roundings
+                ss += (double)((h[v][j] * h[v][j] + h[v][j + 1] * h[v][j + 1]) + (h[v][j + 2] * h[v][j + 2] + h[v][j + 3] * h[v][j + 3]));
         }
     }
-    ss = team_reduce<T>(ss, sh, [](float p, float q) { return p + q; });
-    const float rstd = 1.0f / sqrtf(ss / (float)a.o.K + a.eps);
+    ss = team_reduce<T>(ss, sh, [](double p, double q) { return p + q; });
+    const float rstd = (float)(1.0 / sqrt(ss / (double)a.o.K + (double)a.eps));
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
         const int c = v * T + lane;
@@ -408,8 +420,7 @@ struct GateArgs {
 template <int XT>
 CHAM_DEV void gate_chunk(const Raw<XT>& x, const Raw<XT>& u, bool gated, int act, float (&y)[kChunk]) {
     widen<XT>(x, y);
-#pragma unroll
-    for (int j = 0; j < kChunk; ++j) y[j] = activate(y[j], act);
+    activate(y, act);
     if (gated) {
         float t[kChunk];
         widen<XT>(u, t);
@@ -423,60 +434,65 @@ template <int XT, int T>
 __global__ __launch_bounds__(wg_threads<T>()) void gate_row_kernel(GateArgs a) {
     __shared__ float sh[T > kWave ? T / kWave : 1];
     const int lane = threadIdx.x & (T - 1), nch = a.o.K / kChunk;
-    int64_t row = xcd_run(blockIdx.x, gridDim.x) * rows_per_wg<T>() + (T == kWave ? threadIdx.x / T : 0);
+    int64_t row = (int64_t)blockIdx.x * rows_per_wg<T>() + (T == kWave ? threadIdx.x / T : 0);
     const bool live = row < a.o.M;
     if (!live) row = a.o.M - 1;
+    // binary32 rows of 1024 lanes: the second factor is loaded after the first is used up (both
+    // at once would not fit the 128 registers that 1024 lanes leave each)
+    constexpr bool kLate = XT == CHAM_T_F32 && T == 1024;
     Raw<XT> x[kV], u[kV];
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
         if (v * T < nch) {
             const int64_t i = (int64_t)min(v * T + lane, nch - 1) * kChunk;
             x[v] = load8<XT>(a.x, row * a.ldx + i);
-            if (a.u) u[v] = load8<XT>(a.u, row * a.ldu + i);
+            if (!kLate && a.u) u[v] = load8<XT>(a.u, row * a.ldu + i);
         }
     }
     float y[kV][kChunk];
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) y[v][j] = 0.0f;
-        if (v * T < nch && v * T + lane < nch) gate_chunk<XT>(x[v], u[v], a.u != nullptr, a.act, y[v]);
+        const int64_t c = v * T + lane;
+        if (v * T < nch && c < nch) {
+            if (kLate && a.u) u[v] = load8<XT>(a.u, row * a.ldu + c * kChunk);
+            gate_chunk<XT>(x[v], u[v], a.u != nullptr, a.act, y[v]);
+        }
     }
     emit<T, kOutRow>(a.o, row, live, lane, nch, y, sh);
 }
 
 // Block and MX formats need no more than 16 neighbouring lanes: the tensor is a list of blocks
-// of 128 (those of a row's ragged end are short), 16 lanes a block, any K.
+// of 128 (those of a row's ragged end are short), 16 lanes a block, any K.  A workgroup takes 32
+// consecutive blocks; where its first one lies is found once, in scalar registers.
 constexpr int kGateThreads = 256;
 constexpr int kGateBlocks = 2;  // blocks per 16 lanes, their loads in flight together
+constexpr int kGatePer = kGateThreads / 16 * kGateBlocks;
 
 template <int XT, int OUT>
 __global__ __launch_bounds__(kGateThreads) void gate_block_kernel(GateArgs a) {
     const int nch = a.o.K / kChunk, nb = (nch + 15) >> 4;
-    const int64_t all = a.o.M * nb;
-    const int64_t first = (xcd_run(blockIdx.x, gridDim.x) * kGateThreads + threadIdx.x) / 16 * kGateBlocks;
+    const int64_t b0 = (int64_t)blockIdx.x * kGatePer, row0 = b0 / nb;
+    const int c0 = (int)(b0 - row0 * nb);
+    const int recip = 65536 / min(nb, 65536) + 1;  // of nb < 32
     Raw<XT> x[kGateBlocks], u[kGateBlocks];
     int64_t row[kGateBlocks];
     int c[kGateBlocks];
     bool in[kGateBlocks];
 #pragma unroll
     for (int v = 0; v < kGateBlocks; ++v) {
-        const int64_t b = min(first + v, all - 1);
-        row[v] = b / nb;
-        c[v] = (int)(b - row[v] * nb) * 16 + (threadIdx.x & 15);
-        in[v] = first + v < all && c[v] < nch;
-        const int64_t i = (int64_t)min(c[v], nch - 1) * kChunk;
-        x[v] = load8<XT>(a.x, row[v] * a.ldx + i);
-        if (a.u) u[v] = load8<XT>(a.u, row[v] * a.ldu + i);
+        const int i = c0 + v * (kGateThreads / 16) + (int)threadIdx.x / 16;  // blocks from row0's start, < nb + 32
+        const int q = nb >= kGatePer ? (i >= nb ? 1 : 0) : (i * recip) >> 16;  // i / nb (i < 64 where nb < 32)
+        row[v] = row0 + q;
+        c[v] = (i - q * nb) * 16 + (threadIdx.x & 15);
+        in[v] = row[v] < a.o.M && c[v] < nch;
+        const int64_t r = min(row[v], a.o.M - 1), e = (int64_t)min(c[v], nch - 1) * kChunk;
+        x[v] = load8<XT>(a.x, r * a.ldx + e);
+        if (a.u) u[v] = load8<XT>(a.u, r * a.ldu + e);
     }
 #pragma unroll
     for (int v = 0; v < kGateBlocks; ++v) {
         float y[kChunk];
         gate_chunk<XT>(x[v], u[v], a.u != nullptr, a.act, y);
-        if (!in[v]) {
-#pragma unroll
-            for (int j = 0; j < kChunk; ++j) y[j] = 0.0f;
-        }
         if (OUT == kOutBlock) {
             emit_block(a.o, row[v], c[v], in[v], y);
         } else {
@@ -526,7 +542,7 @@ __global__ __launch_bounds__(kWThreads) void weights_block_kernel(const void* W,
 #pragma unroll
     for (int v = 0; v < kWSteps; ++v) {
         const int64_t n = n0 + v * kWRows;
-        if (n < N && c < nch) *(uint2*)(codes + n * K + (int64_t)c * kChunk) = codes8<CHAM_A_FP8_E4M3>(y[v], r, 0.0f);
+        if (n < N && c < nch) *(uint2*)(codes + n * K + (int64_t)c * kChunk) = codes8_e4m3(y[v], r);
     }
 }
 
@@ -642,7 +658,7 @@ void launch_gate_t(const GateArgs& a, int out, hipStream_t s) {
         else hipLaunchKernelGGL((gate_row_kernel<XT, 1024>), grid, dim3(1024), 0, s, a);
         return;
     }
-    const int64_t blocks = a.o.M * ((a.o.K + 127) / 128), per = kGateThreads / 16 * kGateBlocks;
+    const int64_t blocks = a.o.M * ((a.o.K + 127) / 128), per = kGatePer;
     const dim3 grid((unsigned)((blocks + per - 1) / per));
     if (out == kOutBlock) hipLaunchKernelGGL((gate_block_kernel<XT, kOutBlock>), grid, dim3(kGateThreads), 0, s, a);
     else hipLaunchKernelGGL((gate_block_kernel<XT, kOutMx>), grid, dim3(kGateThreads), 0, s, a);

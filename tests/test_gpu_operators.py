@@ -427,6 +427,28 @@ def test_product_of_small_integers_is_exact(M, N, K, pow2):
 
 
 @pytest.mark.parametrize("dt", DTS)
+@pytest.mark.parametrize("pow2", [False, True])
+@pytest.mark.parametrize("other", [3, 40, 300, 5000])
+def test_product_of_single_codes(dt, pow2, other):
+    """Every finite E4M3 code, alone in its row, against ones: Y is the code's value exactly,
+    subnormal codes among them, as activation and as weight, in small and large tiles."""
+    case(f"single codes {dt} pow2={pow2} other={other}")
+    codes = torch.tensor([c for c in range(256) if c & 127 != 127], dtype=torch.uint8)
+    n, K = codes.numel(), 160
+    a = torch.zeros(n, K, dtype=torch.uint8)
+    a[torch.arange(n), (torch.arange(n) * 7) % K] = codes
+    one = torch.full((other, K), 0x38, dtype=torch.uint8)
+
+    def scale(*shape):
+        return (torch.full(shape, 127, dtype=torch.uint8) if pow2 else torch.ones(shape)).to(DEV)
+    v = _e4m3(codes).to(dt)
+    Y = cham.block_linear(cham.BQ(n, K, a.to(DEV), scale(2, n)), cham.BW(other, K, one.to(DEV), scale(-(-other // 128), 2)), dtype=dt)
+    assert torch.equal(Y.cpu(), v[:, None].expand(n, other))
+    Y = cham.block_linear(cham.BQ(other, K, one.to(DEV), scale(2, other)), cham.BW(n, K, a.to(DEV), scale(2, 2)), dtype=dt)
+    assert torch.equal(Y.cpu(), v[None, :].expand(other, n))
+
+
+@pytest.mark.parametrize("dt", DTS)
 @pytest.mark.parametrize("pad,off", [(0, 0), (1, 0), (8, 0), (3, 1)])
 def test_product_into_strided_and_unaligned_rows(dt, pad, off):
     for M, N, K in ((7, 45, 160), (150, 333, 256), (600, 2001, 384)):
