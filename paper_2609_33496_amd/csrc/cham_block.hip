@@ -163,8 +163,6 @@ struct Tile {
     static constexpr int kLoadsX = BM / 8 / kWaves, kLoadsW = BN / 8 / kWaves;  // 1 KB each
     static constexpr int kLoads = kLoadsX + kLoadsW;
     static constexpr bool kSpread = TM * TN >= 16;  // loads of a step spread over its products
-    static constexpr int kLds = KS * BK * (2 * BM + 3 * BN);
-    static constexpr int kPerCu = 163840 / kLds < 4 ? 163840 / kLds : 4;  // resident workgroups of a CU
     static constexpr bool kFence = TM * TN >= 8;
     static_assert(kWaves % 4 == 0 && TN % 2 == 0 && 128 % (16 * TN) == 0 && BN <= 256, "layout");
     static_assert(KS == 1 || BM <= 64, "a group's sums fit its slices of two weight buffers");
@@ -175,8 +173,8 @@ struct Tile {
 // order that walks kGroup tile rows down before it steps to the next tile column, so that the
 // tiles an XCD works on at one time share their activation and weight rows in its L2.
 constexpr int kGroup = 8;
-CHAM_DEV void tile_of(const BlockArgs& a, int b, int& bm, int& bn) {
-    const int n = a.tm * a.tn;
+CHAM_DEV void tile_of(const BlockArgs& a, int& bm, int& bn) {
+    const int n = a.tm * a.tn, b = blockIdx.x;
     const int q = n >> 3, r = n & 7, x = b & 7;
     const int i = x * q + min(x, r) + (b >> 3);
     const int gsize = kGroup * a.tn, gi = i / gsize, rows = min(kGroup, a.tm - gi * kGroup), j = i - gi * gsize;
@@ -216,13 +214,6 @@ CHAM_DEV void read_barrier() {
     order_loads();
 }
 
-// Whether a workgroup makes several tiles: the large ones of the 8-bit instructions (the f16
-// route's registers do not hold a second tile's addresses; k groups take the buffers of the next
-// tile's loads for their sums; small tiles gain nothing, 8192 x 8192 x 8192 in 64 x 64 tiles 879
-// us against 912).  2048 x 10240 x 1280 35.3 us -> 32.8, 8192 x 4608 x 1152 58.4 -> 55.2.
-template <class T>
-constexpr bool many_rounds(int mode) { return T::kSpread && T::KS == 1 && !exact(mode); }
-
 template <class T, int MODE, int YT>
 __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockArgs a) {
     constexpr int WM = T::WM, TM = T::TM, TN = T::TN, KS = T::KS;
@@ -233,23 +224,16 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
     const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = KS > 1 ? all / T::kWaves : 0, wave = all - group * T::kWaves;
     const int wm = wave % WM, wn = wave / WM;
+    int bm, bn;
+    tile_of(a, bm, bn);
+    const int64_t m0 = (int64_t)bm * T::BM, n0 = (int64_t)bn * T::BN;
     const int K = a.K, nkb = a.nkb;
 
-    // the tile whose operands are loaded
-    int64_t m0, n0;
-    int mrows;
-    __amdgpu_buffer_rsrc_t rx, rw;
-    const Scale* wsp;
-    auto take_tile = [&](int id) {
-        int bm, bn;
-        tile_of(a, id, bm, bn);
-        m0 = (int64_t)bm * T::BM;
-        n0 = (int64_t)bn * T::BN;
-        mrows = min((int64_t)T::BM, a.M - m0);
-        rx = __builtin_amdgcn_make_buffer_rsrc((void*)(a.xc + m0 * K), (short)0, mrows * K, kBufferFlags);
-        rw = __builtin_amdgcn_make_buffer_rsrc((void*)(a.wc + n0 * K), (short)0, (int)min((int64_t)T::BN, a.N - n0) * K, kBufferFlags);
-        wsp = (const Scale*)a.ws + min((n0 + wn * 16 * TN) / 128, ((int64_t)a.N - 1) / 128) * nkb;
-    };
+    const int mrows = min((int64_t)T::BM, a.M - m0), nrows = min((int64_t)T::BN, a.N - n0);
+    const __amdgpu_buffer_rsrc_t rx =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(a.xc + m0 * K), (short)0, mrows * K, kBufferFlags);
+    const __amdgpu_buffer_rsrc_t rw =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(a.wc + n0 * K), (short)0, nrows * K, kBufferFlags);
 
     // Load i of a wavefront: rows (i kWaves + wave) 8 .. + 7, lane l the slot l % 8 of row l / 8.
     // The rows of two loads differ by a multiple of 32, so a lane's chunk is the same in all.
@@ -274,6 +258,8 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
 
     // scales of the lane's rows (one per 16-row block) and of the wavefront's channels
     const int rr = lane & 15, g = lane >> 4;
+    const int64_t wblk = min((n0 + wn * 16 * TN) / 128, ((int64_t)a.N - 1) / 128) * nkb;
+    const Scale* const wsp = (const Scale*)a.ws + wblk;
     struct Factors {
         Scale x[TM], w;
     };
@@ -295,6 +281,10 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
     };
 
     float4v acc[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) acc[i][j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 
     // byte offsets of the lane's two chunks: its key is the same in every 16-row block
     const int x0 = group * kX + (wm * TM * 16 + rr) * BK, w0 = group * kW + (wn * 16 * TN + chan(0, rr)) * BK;
@@ -410,79 +400,60 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
 
     Lds *const x_0 = (Lds*)X0, *const x_1 = (Lds*)X1;
     Lds *const w_0 = (Lds*)W0, *const w_1 = (Lds*)W1, *const w_2 = (Lds*)W2;
-    // The first two steps of the tile.  A step's barrier counts the loads of the step behind it, so
-    // no load may move from one step's to the other's.
-    auto first = [&] {
-        scales(s0, group);
-        issue_all(x_0, w_0, group);
-        order_loads();
-        scales(s1, KS + group);
-        issue_all(x_1, w_1, KS + group);
-        order_loads();
-    };
+    // A step's barrier counts the loads of the step behind it, so none may move from one step's to
+    // another's.
+    scales(s0, group);
+    issue_all(x_0, w_0, group);
+    order_loads();
+    scales(s1, KS + group);
+    issue_all(x_1, w_1, KS + group);
+    order_loads();
     const int steps = (nkb + KS - 1) / KS;  // the same for all groups: steps past the last block are zeros
-    const int tiles = a.tm * a.tn;
-    take_tile(blockIdx.x);
-    first();
-    for (int id = blockIdx.x;;) {
-#pragma unroll
-        for (int i = 0; i < TN; ++i)
-#pragma unroll
-            for (int t = 0; t < TM; ++t) acc[i][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int j = 0;; j += 6) {
-            step(x_0, w_0, w_2, s0, j);
-            if (j + 1 >= steps) break;
-            step(x_1, w_1, w_0, s1, j + 1);
-            if (j + 2 >= steps) break;
-            step(x_0, w_2, w_1, s0, j + 2);
-            if (j + 3 >= steps) break;
-            step(x_1, w_0, w_2, s1, j + 3);
-            if (j + 4 >= steps) break;
-            step(x_0, w_1, w_0, s0, j + 4);
-            if (j + 5 >= steps) break;
-            step(x_1, w_2, w_1, s1, j + 5);
-            if (j + 6 >= steps) break;
-        }
-        landed_barrier<0>();  // no write to LDS outlives the workgroup or meets what follows
+    for (int j = 0;; j += 6) {
+        step(x_0, w_0, w_2, s0, j);
+        if (j + 1 >= steps) break;
+        step(x_1, w_1, w_0, s1, j + 1);
+        if (j + 2 >= steps) break;
+        step(x_0, w_2, w_1, s0, j + 2);
+        if (j + 3 >= steps) break;
+        step(x_1, w_0, w_2, s1, j + 3);
+        if (j + 4 >= steps) break;
+        step(x_0, w_1, w_0, s0, j + 4);
+        if (j + 5 >= steps) break;
+        step(x_1, w_2, w_1, s1, j + 5);
+        if (j + 6 >= steps) break;
+    }
+    landed_barrier<0>();  // no write to LDS outlives the workgroup or meets the sums below
 
-        if constexpr (KS > 1) {
-            auto part = [&](int q, int i, int t) {  // block (i, t) of this wavefront's counterpart in group q
-                float4v* p = (float4v*)((i < TN / 2 ? W0 : W1) + q * kW);
-                return p + ((wave * (TN / 2) + i % (TN / 2)) * TM + t) * 64 + lane;
-            };
-            if (group > 0) {
+    if constexpr (KS > 1) {
+        auto part = [&](int q, int i, int t) {  // block (i, t) of this wavefront's counterpart in group q
+            float4v* p = (float4v*)((i < TN / 2 ? W0 : W1) + q * kW);
+            return p + ((wave * (TN / 2) + i % (TN / 2)) * TM + t) * 64 + lane;
+        };
+        if (group > 0) {
 #pragma unroll
-                for (int i = 0; i < TN; ++i)
+            for (int i = 0; i < TN; ++i)
 #pragma unroll
-                    for (int t = 0; t < TM; ++t) *part(group, i, t) = acc[i][t];
-            }
-            __syncthreads();
-            if (group > 0) return;  // one tile per workgroup
-#pragma unroll
-            for (int q = 1; q < KS; ++q)
-#pragma unroll
-                for (int i = 0; i < TN; ++i)
-#pragma unroll
-                    for (int t = 0; t < TM; ++t) acc[i][t] += *part(q, i, t);
+                for (int t = 0; t < TM; ++t) *part(group, i, t) = acc[i][t];
         }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int q = 1; q < KS; ++q)
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+#pragma unroll
+                for (int t = 0; t < TM; ++t) acc[i][t] += *part(q, i, t);
+    }
 
-        // The next tile's first loads are on their way while this one's results are written (they
-        // wait for no store: a step's barrier counts the loads behind it, and stores only add).
-        const int64_t m1 = m0 + wm * TM * 16 + rr, n1 = n0 + wn * 16 * TN + g * 8;
-        id += gridDim.x;
-        const bool more = many_rounds<T>(MODE) && id < tiles;
-        if (more) {
-            take_tile(id);
-            first();
-        }
 #pragma unroll
-        for (int t = 0; t < TM; ++t) {
-            if (m1 + t * 16 < a.M) {
+    for (int t = 0; t < TM; ++t) {
+        const int64_t m = m0 + (wm * TM + t) * 16 + rr;
+        if (m < a.M) {
 #pragma unroll
-                for (int i = 0; i < TN; i += 2) store8<YT>(a, m1 + t * 16, n1 + (i >> 1) * 32, acc[i][t], acc[i + 1][t]);
-            }
+            for (int i = 0; i < TN; i += 2)
+                store8<YT>(a, m, n0 + wn * 16 * TN + (i >> 1) * 32 + g * 8, acc[i][t], acc[i + 1][t]);
         }
-        if (!more) break;
     }
 }
 
@@ -607,10 +578,7 @@ template <class T, int MODE, int YT>
 void launch_tile(BlockArgs a, hipStream_t s) {
     a.tm = (a.M + T::BM - 1) / T::BM;
     a.tn = (a.N + T::BN - 1) / T::BN;
-    // as many workgroups as stay resident, each with a tile of every round
-    const int64_t tiles = (int64_t)a.tm * a.tn, slots = (int64_t)T::kPerCu * cham_device_cus();
-    const dim3 grid((unsigned)(many_rounds<T>(MODE) ? std::min(tiles, slots) : tiles));
-    hipLaunchKernelGGL((tile_kernel<T, MODE, YT>), grid, dim3(T::kWaves * T::KS * 64), 0, s, a);
+    hipLaunchKernelGGL((tile_kernel<T, MODE, YT>), dim3((unsigned)(a.tm * a.tn)), dim3(T::kWaves * T::KS * 64), 0, s, a);
 }
 template <int TM, int TN, int NW, int MODE, int YT>
 void launch_few(BlockArgs a, hipStream_t s) {
