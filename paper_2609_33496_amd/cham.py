@@ -770,11 +770,11 @@ def _matrix(t: torch.Tensor, name: str, shape=None, device=None) -> int:
     ty = _TYPES.get(t.dtype)
     if ty is None:
         raise ValueError(f"{name} must be float32, float16 or bfloat16")
-    if t.dim() != 2 or (shape is not None and t.shape != shape):
+    if t.shape != shape if shape is not None else t.dim() != 2:
         raise ValueError(f"{name} must be a matrix" + (f" of shape {tuple(shape)}" if shape is not None else ""))
-    if not t.is_cuda or (device is not None and t.device != device):
+    if t.device != device if device is not None else not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor" + (f" on {device}" if device is not None else ""))
-    if t.stride(1) != 1 and t.shape[1] > 1:
+    if not t.is_contiguous() and t.stride(1) != 1 and t.shape[1] > 1:
         raise ValueError(f"{name} must have unit stride along its columns")
     return ty
 
@@ -800,19 +800,19 @@ def _on_device(dev, stream, call, *args):
         return call(*args, _stream_now(dev.index) if stream is None else stream.cuda_stream)
 
 
-def _empty(shape, dtype, dev, stream):
+def _empty(rows, cols, dtype, dev, stream):
     """Memory of the launch stream's pool: that of another stream's may still be in use there."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return torch.empty(rows, cols, dtype=dtype, device=dev)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return torch.empty(rows, cols, dtype=dtype, device=dev)
 
 
 def _row_out(out, fmt, M, K, dev, pow2, stream):
     """The output of a row pass (the caller's, else a new one) and its C descriptor."""
     if fmt == A_BLOCK128:
         if out is None:
-            out = BQ(M, K, _empty((M, K), torch.uint8, dev, stream), _empty((_cdiv(K, BLOCK), M), _scale_type(pow2), dev, stream))
+            out = BQ(M, K, _empty(M, K, torch.uint8, dev, stream), _empty(_cdiv(K, BLOCK), M, _scale_type(pow2), dev, stream))
             return out, _BQ(M, K, int(bool(pow2)), out.codes.data_ptr(), out.scale.data_ptr())
         if not isinstance(out, BQ) or (out.M, out.K) != (M, K) or out.codes.device != dev:
             raise ValueError(f"out must be a BQ of shape ({M}, {K}) on {dev}")
@@ -821,8 +821,8 @@ def _row_out(out, fmt, M, K, dev, pow2, stream):
         return out, out.struct()
     mx = fmt in (A_MXFP8, A_MXINT8)
     if out is None:
-        out = AQ(M, K, fmt, _empty((M, K), torch.uint8, dev, stream), _empty((M, K // 32), torch.uint8, dev, stream) if mx else None,
-                 _empty(M, torch.float32, dev, stream), _empty(M, torch.float32, dev, stream), M)
+        out = AQ(M, K, fmt, _empty(M, K, torch.uint8, dev, stream), _empty(M, K // 32, torch.uint8, dev, stream) if mx else None,
+                 *_empty(2, M, torch.float32, dev, stream).unbind(0), M)
         return out, out.struct()
     if not isinstance(out, AQ) or (out.M, out.K) != (M, K) or out.codes.device != dev:
         raise ValueError(f"out must be an AQ of shape ({M}, {K}) on {dev}")
@@ -852,7 +852,7 @@ def rms_norm_quantize(X: torch.Tensor, weight: Optional[torch.Tensor] = None, ep
         rt = _matrix(residual, "residual", X.shape, dev)
         r_ptr, ldr = residual.data_ptr(), _ld(residual)
         if residual_out is None:
-            residual_out = _empty((M, K), residual.dtype, dev, stream)
+            residual_out = _empty(M, K, residual.dtype, dev, stream)
             ldh = K
         elif _matrix(residual_out, "residual_out", X.shape, dev) != rt:
             raise ValueError("residual_out must have the residual's type")
@@ -908,8 +908,8 @@ def block_quantize_weights(W: torch.Tensor, pow2: bool = False, out: Optional[BW
     N, K = W.shape
     dev = W.device
     if out is None:
-        out = BW(N, K, _empty((N, K), torch.uint8, dev, stream),
-                 _empty((_cdiv(N, BLOCK), _cdiv(K, BLOCK)), _scale_type(pow2), dev, stream))
+        out = BW(N, K, _empty(N, K, torch.uint8, dev, stream),
+                 _empty(_cdiv(N, BLOCK), _cdiv(K, BLOCK), _scale_type(pow2), dev, stream))
         st = _BW(N, K, int(bool(pow2)), out.codes.data_ptr(), out.scale.data_ptr())
     elif (out.N, out.K) != (N, K) or out.codes.device != dev or (out.scale.dtype is torch.uint8) != bool(pow2):
         raise ValueError("out does not fit W and pow2")
@@ -932,7 +932,7 @@ def block_linear(xb: BQ, wb: BW, Y: Optional[torch.Tensor] = None, dtype: torch.
         ty, ld = _TYPES.get(dtype), wb.N
         if ty is None:
             raise ValueError("dtype must be float32, float16 or bfloat16")
-        Y = _empty((xb.M, ld), dtype, dev, stream)
+        Y = _empty(xb.M, ld, dtype, dev, stream)
     else:
         ty, ld = _matrix(Y, "Y", (xb.M, wb.N), dev), _ld(Y)
     rc = _on_device(dev, stream, lib().cham_block_linear, ctypes.byref(a), ctypes.byref(w), Y.data_ptr(), ty, ld)

@@ -11,6 +11,7 @@ import pytest
 import torch
 
 from paper_2609_33496_amd import cham
+from paper_2609_33496_amd.feed_forward import FeedForward
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -541,6 +542,21 @@ def test_feed_forward_block(M, d, hid, gated, pow2):
     v, rel = _gate_ref(t[:, :hid].cpu(), t[:, hid:].cpu() if gated else None, "gelu")
     _check_out(q2, "block", v, rel.clamp(max=2e-3), pow2)
     _check_product(y, _e4m3(q2.codes) * _held(q2.scale).t().repeat_interleave(128, 1)[:, :hid], _wide(w2, d, hid), x.dtype)
+
+
+@pytest.mark.parametrize("gated,pow2", [(True, False), (False, True)])
+def test_feed_forward_class_makes_the_same_calls(gated, pow2):
+    case(f"FeedForward gated={gated} pow2={pow2}")
+    d, hid = 320, 640
+    w_in = _x(4, hid * (2 if gated else 1), d, torch.float32, 0.03).to(DEV)
+    w_out = _x(5, d, hid, torch.float32, 0.03).to(DEV)
+    x, r, g, w1, w2, _ = _block_args(33, d, hid, gated, pow2)
+    block = FeedForward(w_in, w_out, g, act=cham.ACT_SILU, gated=gated, pow2=pow2)
+    y, h = block(x, r)
+    want, hwant = _block(x, r, g, w1, w2, pow2, cham.ACT_SILU)
+    assert torch.equal(y, want) and torch.equal(h, hwant)
+    with pytest.raises(ValueError):
+        FeedForward(w_in, w_out.t().contiguous(), g, gated=gated)
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8", "mxfp8"])
