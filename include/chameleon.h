@@ -472,8 +472,9 @@ typedef struct cham_bw {
 } cham_bw;
 
 /* h = x + r (binary32), y = h / sqrt(mean(h^2) + eps) * g: the norm sees the unrounded sum; h is
- * written rounded to its own type.  The mean is taken over the row in binary32 (rows whose sum
- * of squares overflows binary32 come out as zeros). */
+ * written rounded to its own type.  Squares of 8 neighbours are added in binary32, those sums and
+ * the mean in binary64 (a row in which 8 squares overflow binary32, |h| from 6e18 up, comes out
+ * as zeros). */
 typedef struct cham_norm {
     int64_t M, K;      /* K <= 32768                                                         */
     const void* x;     /* [M][K], row stride ldx elements                                    */
@@ -492,7 +493,8 @@ typedef struct cham_norm {
 
 /* The norm of n, written in the block format (out->M, K equal n's).
  * Errors: CHAM_EINVAL (NULL, sizes, strides, alignment, eps), CHAM_EFORMAT (types),
- * CHAM_ESHAPE (K % 32, K > 32768, M >= 2^31), CHAM_EHIP. */
+ * CHAM_ESHAPE (K % 32, K > 32768, M >= 2^31, or a launch of 2^32 lanes: M 64 lanes up to K =
+ * 2048, 256 up to 8192, then 1024), CHAM_EHIP. */
 int cham_rms_norm_quantize_block(const cham_norm* n, cham_bq* out, void* stream);
 
 /* The norm of n, written in activation format fmt of section 3 with dynamic scales of each
@@ -523,20 +525,26 @@ typedef struct cham_gate {
 
 /* The gate of a, written in the block format (out->M, K equal a's), or in an activation
  * format with one scale per token (as cham_rms_norm_quantize).  Errors: CHAM_EINVAL,
- * CHAM_EFORMAT (types, act, fmt), CHAM_ESHAPE, CHAM_EHIP. */
+ * CHAM_EFORMAT (types, act, fmt), CHAM_ESHAPE (K % 32, K > 32768 with one scale per token, K >
+ * 2^30 otherwise, M >= 2^31, or a launch of 2^32 lanes: one per 16 elements in the block and MX
+ * formats, as in the norm in the others), CHAM_EHIP. */
 int cham_gated_quantize_block(const cham_gate* a, cham_bq* out, void* stream);
 int cham_gated_quantize(const cham_gate* a, int32_t fmt, cham_aq* out, void* stream);
 
 /* Weights W [N][K] (row stride ldw elements) brought to the block format: out->N, K and pow2
- * are given.  N >= 1.  Errors: CHAM_EINVAL, CHAM_EFORMAT, CHAM_ESHAPE, CHAM_EHIP. */
+ * are given.  N >= 1.  Errors: CHAM_EINVAL, CHAM_EFORMAT, CHAM_ESHAPE (K % 32, or 2^32 lanes at
+ * 512 for each block of 128 x 128), CHAM_EHIP. */
 int cham_block_quantize_weights(const void* W, int32_t type, int64_t ldw, cham_bw* out, void* stream);
 
-/* Y[m][n] = sum over blocks b of xs[b][m] ws[n / 128][b] sum_{k in b} xc[m][k] wc[n][k], the
- * inner sums and their total in binary32, rounded once to y_type.  Y [M][N], row stride ldy
- * elements (any; any N).  x->pow2 must equal w->pow2.  Products and partial sums are added in a fixed order (no atomics on values): Y is bitwise reproducible run to run.
- * The product of an activation's and a weight's scale must not overflow binary32.  Limits:
- * K <= 2^20, M and N < 2^31.  No workspace.  Errors: CHAM_EINVAL, CHAM_EFORMAT (y_type), CHAM_ESHAPE,
- * CHAM_EHIP. */
+/* Y[m][n] = sum over blocks b of xs[b][m] ws[n / 128][b] sum_{k in b} xc[m][k] wc[n][k],
+ * accumulated in binary32 and rounded once to y_type.  Binary32 outputs form every product
+ * exactly; 16-bit outputs use the 8-bit matrix instructions, which drop what lies more than 13
+ * bits below the largest product of a group of neighbouring k (3e-5 of the result, a sixteenth of
+ * a binary16 rounding at most).  Y [M][N], row stride ldy elements (any; any N).  x->pow2 must
+ * equal w->pow2.  The order of the additions is fixed by the sizes (no atomics): Y is bitwise
+ * reproducible run to run.  The product of an activation's and a weight's scale must not
+ * overflow binary32.  No workspace.  Errors: CHAM_EINVAL, CHAM_EFORMAT (y_type), CHAM_ESHAPE
+ * (K % 32, K > 2^20, M or N > 2^31 - 257, or a launch of 2^32 lanes), CHAM_EHIP. */
 int cham_block_linear(const cham_bq* x, const cham_bw* w, void* Y, int32_t y_type, int64_t ldy,
                       void* stream);
 

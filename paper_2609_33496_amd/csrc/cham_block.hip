@@ -574,17 +574,25 @@ __global__ __launch_bounds__(NW * 64) void few_rows_kernel(BlockArgs a) {
 // ------------------------------------------------------------------------------------
 // launches
 // ------------------------------------------------------------------------------------
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 template <class T, int MODE, int YT>
-void launch_tile(BlockArgs a, hipStream_t s) {
-    a.tm = (a.M + T::BM - 1) / T::BM;
-    a.tn = (a.N + T::BN - 1) / T::BN;
+int launch_tile(BlockArgs a, hipStream_t s) {
+    a.tm = (int)ceil_div(a.M, T::BM);
+    a.tn = (int)ceil_div(a.N, T::BN);
+    if (!cham_launchable((int64_t)a.tm * a.tn, T::kWaves * T::KS * 64)) return CHAM_ESHAPE;
     hipLaunchKernelGGL((tile_kernel<T, MODE, YT>), dim3((unsigned)(a.tm * a.tn)), dim3(T::kWaves * T::KS * 64), 0, s, a);
+    CHAM_CHECK_LAUNCH();
+    return CHAM_OK;
 }
 template <int TM, int TN, int NW, int MODE, int YT>
-void launch_few(BlockArgs a, hipStream_t s) {
-    a.tm = (a.M + 16 * TM - 1) / (16 * TM);
-    a.tn = (a.N + 16 * TN - 1) / (16 * TN);
+int launch_few(BlockArgs a, hipStream_t s) {
+    a.tm = (int)ceil_div(a.M, 16 * TM);
+    a.tn = (int)ceil_div(a.N, 16 * TN);
+    if (!cham_launchable((int64_t)a.tm * a.tn, NW * 64)) return CHAM_ESHAPE;
     hipLaunchKernelGGL((few_rows_kernel<TM, TN, NW, MODE, YT>), dim3((unsigned)(a.tm * a.tn)), dim3(NW * 64), 0, s, a);
+    CHAM_CHECK_LAUNCH();
+    return CHAM_OK;
 }
 
 // Modeled time (us) of one tile shape: the tiles of the busiest CU, each its k-steps and a fixed
@@ -607,7 +615,6 @@ constexpr TileCost kCostHalf[kTiles] = {{0, 0, 0, 0, 0, 0},              {0, 0, 
                                         {32, 64, 1, 0.33, 0.20, 0.40},   {32, 64, 2, 0.493, 0.397, 0.98},
                                         {64, 128, 1, 0.64, 0.551, 1.66}};
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int plan_tile(const BlockArgs& a, const TileCost* costs) {
     const int cus = cham_device_cus();
@@ -632,7 +639,7 @@ bool few_rows(const BlockArgs& a, bool half) {
 }
 
 template <int MODE, int YT>
-void launch_plan(const BlockArgs& a, hipStream_t s) {
+int launch_plan(const BlockArgs& a, hipStream_t s) {
     if (few_rows(a, exact(MODE))) return launch_few<1, 1, 8, MODE, YT>(a, s);
     const int tile = plan_tile(a, exact(MODE) ? kCostHalf : kCostCodes);
     if constexpr (exact(MODE)) {
@@ -647,10 +654,12 @@ void launch_plan(const BlockArgs& a, hipStream_t s) {
     return launch_tile<Tile<2, 2, 1, 2, 2>, MODE, YT>(a, s);
 }
 
+// the last row of the last tile is still a 32-bit index
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 257;
+
 int block_check(const cham_bq* x, const cham_bw* w) {
     if (!x || !w || x->M < 0 || w->N < 1 || x->K < 1 || x->K != w->K) return CHAM_EINVAL;
-    if (x->K % 32 != 0 || x->K > (1 << 20) || x->M >= (int64_t)1 << 31 || w->N >= (int64_t)1 << 31) return CHAM_ESHAPE;
-    if (ceil_div(x->M, 32) * ceil_div(w->N, 16) >= (int64_t)1 << 31) return CHAM_ESHAPE;  // workgroups of any plan
+    if (x->K % 32 != 0 || x->K > (1 << 20) || x->M > kMostRows || w->N > kMostRows) return CHAM_ESHAPE;
     if ((x->M > 0 && (!x->codes || !x->scale)) || !w->codes || !w->scale) return CHAM_EINVAL;
     if (((uintptr_t)x->codes & 15u) || ((uintptr_t)w->codes & 15u)) return CHAM_EINVAL;
     if ((!x->pow2 && ((uintptr_t)x->scale & 3u)) || (!w->pow2 && ((uintptr_t)w->scale & 3u))) return CHAM_EINVAL;
@@ -684,24 +693,15 @@ extern "C" int cham_block_linear(const cham_bq* x, const cham_bw* w, void* Y, in
     a.nkb = (a.K + BK - 1) / BK;
     a.vec = ((uintptr_t)Y & 15u) == 0 && ldy * size % 16 == 0;
     const hipStream_t s = (hipStream_t)stream;
-    if (y_type == CHAM_T_F32) {
-        if (x->pow2) launch_plan<kHalfPow2, CHAM_T_F32>(a, s);
-        else launch_plan<kHalf, CHAM_T_F32>(a, s);
-    } else if (y_type == CHAM_T_F16) {
-        if (x->pow2) launch_plan<kCodesPow2, CHAM_T_F16>(a, s);
-        else launch_plan<kCodes, CHAM_T_F16>(a, s);
-    } else {
-        if (x->pow2) launch_plan<kCodesPow2, CHAM_T_BF16>(a, s);
-        else launch_plan<kCodes, CHAM_T_BF16>(a, s);
-    }
-    CHAM_CHECK_LAUNCH();
-    return CHAM_OK;
+    if (y_type == CHAM_T_F32) return x->pow2 ? launch_plan<kHalfPow2, CHAM_T_F32>(a, s) : launch_plan<kHalf, CHAM_T_F32>(a, s);
+    if (y_type == CHAM_T_F16) return x->pow2 ? launch_plan<kCodesPow2, CHAM_T_F16>(a, s) : launch_plan<kCodes, CHAM_T_F16>(a, s);
+    return x->pow2 ? launch_plan<kCodesPow2, CHAM_T_BF16>(a, s) : launch_plan<kCodes, CHAM_T_BF16>(a, s);
 }
 
 extern "C" int cham_block_linear_plan(int64_t M, int64_t N, int64_t K, int32_t y_type, int32_t* out, int32_t out_len) {
     if (!out || out_len < 3 || M < 1 || N < 1 || K < 1) return CHAM_EINVAL;
     if (y_type < 0 || y_type >= CHAM_T_N) return CHAM_EFORMAT;
-    if (K % 32 != 0 || K > (1 << 20) || M >= (int64_t)1 << 31 || N >= (int64_t)1 << 31) return CHAM_ESHAPE;
+    if (K % 32 != 0 || K > (1 << 20) || M > kMostRows || N > kMostRows) return CHAM_ESHAPE;
     BlockArgs a{};
     a.M = (int)M;
     a.N = (int)N;

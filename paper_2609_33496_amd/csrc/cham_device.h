@@ -318,6 +318,10 @@ CHAM_DEV uint32_t narrow(float a, float b) {
 }  // namespace cham
 
 // host-side helpers shared by the entry points
+// whether a grid of so many workgroups can be launched: a launch counts its threads in 32 bits
+inline bool cham_launchable(int64_t workgroups, int64_t threads) {
+    return workgroups < (int64_t)1 << 31 && workgroups * threads < (int64_t)1 << 32;
+}
 int cham_device_cus();  // compute units of the current device (256 if none is visible)
 #define CHAM_CHECK_LAUNCH()                                     \
     do {                                                        \

@@ -5,6 +5,8 @@
 // held in registers between the reduction that its scale needs and its codes, so nothing is
 // read twice; a lane holds chunks of 8 consecutive elements, 16 lanes a block of 128, 4 lanes
 // an MX block of 32, and block maxima are DPP rotations within 16 lanes (no LDS).
+#include <algorithm>
+
 #include "cham_device.h"
 
 namespace cham {
@@ -582,16 +584,21 @@ int out_token(int32_t fmt, cham_aq* q, int64_t M, int64_t K, Out* o) {
 
 // Lanes per row: a wavefront where its registers hold the row (no barrier, four rows per
 // workgroup), else 256 or 1024 lanes.
-int team(int64_t M, int64_t K) {
-    (void)M;
+int team(int64_t K) {
     return K <= kWave * kV * kChunk ? kWave : K <= 256 * kV * kChunk ? 256 : 1024;
 }
-unsigned row_grid(int64_t M, int T) { return (unsigned)(T == kWave ? (M + 3) / 4 : M); }
+int64_t row_grid(int64_t M, int T) { return T == kWave ? (M + 3) / 4 : M; }
+bool rows_launchable(int64_t M, int64_t K) {
+    const int T = team(K);
+    return cham_launchable(row_grid(M, T), std::max(T, 256));
+}
+// workgroups of the block and MX forms of the gate
+int64_t gate_grid(int64_t M, int64_t K) { return (M * ((K + 127) / 128) + kGatePer - 1) / kGatePer; }
 
 template <int XT, int RT, int OUT>
 void launch_norm_t(const NormArgs& a, hipStream_t s) {
-    const int T = team(a.o.M, a.o.K);
-    const dim3 grid(row_grid(a.o.M, T));
+    const int T = team(a.o.K);
+    const dim3 grid((unsigned)row_grid(a.o.M, T));
     if (T == kWave) hipLaunchKernelGGL((norm_kernel<XT, RT, kWave, OUT>), grid, dim3(256), 0, s, a);
     else if (T == 256) hipLaunchKernelGGL((norm_kernel<XT, RT, 256, OUT>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((norm_kernel<XT, RT, 1024, OUT>), grid, dim3(1024), 0, s, a);
@@ -629,6 +636,7 @@ int norm_check(const cham_norm* n) {
 
 int norm_launch(const cham_norm* n, const Out& o, int out, hipStream_t s) {
     if (n->M == 0) return CHAM_OK;
+    if (!rows_launchable(n->M, n->K)) return CHAM_ESHAPE;
     const NormArgs a{n->x, n->r, n->h, n->g, n->ldx, n->ldr, n->ldh, n->g_type, n->eps, o};
     if (n->x_type == CHAM_T_F32) launch_norm_r<CHAM_T_F32>(a, n->r_type, out, s);
     else if (n->x_type == CHAM_T_F16) launch_norm_r<CHAM_T_F16>(a, n->r_type, out, s);
@@ -651,21 +659,21 @@ int gate_check(const cham_gate* g, int64_t most) {
 template <int XT>
 void launch_gate_t(const GateArgs& a, int out, hipStream_t s) {
     if (out == kOutRow) {
-        const int T = team(a.o.M, a.o.K);
-        const dim3 grid(row_grid(a.o.M, T));
+        const int T = team(a.o.K);
+        const dim3 grid((unsigned)row_grid(a.o.M, T));
         if (T == kWave) hipLaunchKernelGGL((gate_row_kernel<XT, kWave>), grid, dim3(256), 0, s, a);
         else if (T == 256) hipLaunchKernelGGL((gate_row_kernel<XT, 256>), grid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL((gate_row_kernel<XT, 1024>), grid, dim3(1024), 0, s, a);
         return;
     }
-    const int64_t blocks = a.o.M * ((a.o.K + 127) / 128), per = kGatePer;
-    const dim3 grid((unsigned)((blocks + per - 1) / per));
+    const dim3 grid((unsigned)gate_grid(a.o.M, a.o.K));
     if (out == kOutBlock) hipLaunchKernelGGL((gate_block_kernel<XT, kOutBlock>), grid, dim3(kGateThreads), 0, s, a);
     else hipLaunchKernelGGL((gate_block_kernel<XT, kOutMx>), grid, dim3(kGateThreads), 0, s, a);
 }
 
 int gate_launch(const cham_gate* g, const Out& o, int out, hipStream_t s) {
     if (g->M == 0) return CHAM_OK;
+    if (out == kOutRow ? !rows_launchable(g->M, g->K) : !cham_launchable(gate_grid(g->M, g->K), kGateThreads)) return CHAM_ESHAPE;
     const GateArgs a{g->x, g->u, g->ldx, g->ldu, g->act, o};
     if (g->type == CHAM_T_F32) launch_gate_t<CHAM_T_F32>(a, out, s);
     else if (g->type == CHAM_T_F16) launch_gate_t<CHAM_T_F16>(a, out, s);
@@ -723,7 +731,7 @@ extern "C" int cham_block_quantize_weights(const void* W, int32_t type, int64_t 
         return CHAM_EINVAL;
     if (out->pow2 != 0 && out->pow2 != 1) return CHAM_EINVAL;
     const int64_t nb = (out->K + 127) / 128, blocks = (out->N + 127) / 128 * nb;
-    if (blocks >= (int64_t)1 << 31) return CHAM_ESHAPE;
+    if (!cham_launchable(blocks, kWThreads)) return CHAM_ESHAPE;
     const dim3 grid((unsigned)blocks);
     const hipStream_t s = (hipStream_t)stream;
 #define CHAM_W(T)                                                                                                      \

@@ -132,6 +132,26 @@ def test_linear_refusals(x, w, Y, ty, ldy, status):
     assert L.cham_block_linear(ctypes.byref(_bq()), None, P(64), 0, 4, None) == cham.EINVAL
 
 
+def test_launches_past_32_bits_are_refused():
+    """A launch counts its threads in 32 bits; the sizes before that limit are taken (M of 0 apart,
+    no call here passes the checks that come before it)."""
+    L = cham.lib()
+    M = 1 << 30
+    assert L.cham_rms_norm_quantize_block(ctypes.byref(_norm(M=M)), ctypes.byref(_bq(M=M)), None) == cham.ESHAPE
+    assert L.cham_rms_norm_quantize(ctypes.byref(_norm(M=M)), 1, ctypes.byref(_aq(M=M, nsamples=M)), None) == cham.ESHAPE
+    assert L.cham_gated_quantize(ctypes.byref(_gate(M=M)), 1, ctypes.byref(_aq(M=M, nsamples=M)), None) == cham.ESHAPE
+    K = 1 << 16
+    g = _gate(M=M, K=K, ldx=K, ldu=K)
+    assert L.cham_gated_quantize_block(ctypes.byref(g), ctypes.byref(_bq(M=M, K=K)), None) == cham.ESHAPE
+    assert L.cham_gated_quantize(ctypes.byref(g), 3, ctypes.byref(_aq(M=M, nsamples=M, K=K)), None) == cham.ESHAPE
+    N = 1 << 31
+    assert L.cham_block_quantize_weights(P(64), 0, K, ctypes.byref(_bw(N=N, K=K)), None) == cham.ESHAPE
+    N = 1 << 30
+    assert L.cham_block_linear(ctypes.byref(_bq(M=N)), ctypes.byref(_bw(N=N)), P(64), 0, N, None) == cham.ESHAPE
+    for M, N in (((1 << 31) - 1, 64), (64, (1 << 31) - 1)):  # the last tile's rows would pass 32 bits
+        assert L.cham_block_linear(ctypes.byref(_bq(M=M)), ctypes.byref(_bw(N=N)), P(64), 0, N, None) == cham.ESHAPE
+
+
 def test_binding_refuses_host_tensors_and_wrong_shapes():
     x = torch.zeros(4, 64)
     for call in (lambda: cham.rms_norm_quantize(x), lambda: cham.gated_quantize(x), lambda: cham.block_quantize_weights(x)):
