@@ -36,7 +36,7 @@ struct BlockArgs {
     int64_t ldy;
     int M, N, K, nkb;
     int tm, tn;    // tiles
-    int vec;       // rows of Y start at multiples of 16 bytes
+    int vec;       // rows of Y start at multiples of 16 bytes: 2, of 8 bytes: 1, else 0
 };
 
 // How the products of a block are formed.  The 8-bit matrix instructions align the products of
@@ -108,7 +108,7 @@ template <int YT>
 CHAM_DEV void store4(const BlockArgs& a, int64_t m, int64_t n, float4v p) {
     if (m >= a.M) return;
     const int64_t i = m * a.ldy + n;
-    if (a.vec && n + 4 <= a.N) {
+    if (a.vec >= (YT == CHAM_T_F32 ? 2 : 1) && n + 4 <= a.N) {
         if constexpr (YT == CHAM_T_F32) *(float4v*)((float*)a.Y + i) = p;
         else *(uint2*)((uint16_t*)a.Y + i) = make_uint2(narrow<YT>(p[0], p[1]), narrow<YT>(p[2], p[3]));
     } else {
@@ -120,7 +120,12 @@ CHAM_DEV void store4(const BlockArgs& a, int64_t m, int64_t n, float4v p) {
 template <int YT>
 CHAM_DEV void store8(const BlockArgs& a, int64_t m, int64_t n, float4v p, float4v q) {
     const int64_t i = m * a.ldy + n;
-    if (a.vec && n + 8 <= a.N) {
+    if (a.vec == 1 && YT != CHAM_T_F32 && n + 8 <= a.N) {
+        if constexpr (YT != CHAM_T_F32) {
+            *(uint2*)((uint16_t*)a.Y + i) = make_uint2(narrow<YT>(p[0], p[1]), narrow<YT>(p[2], p[3]));
+            *(uint2*)((uint16_t*)a.Y + i + 4) = make_uint2(narrow<YT>(q[0], q[1]), narrow<YT>(q[2], q[3]));
+        }
+    } else if (a.vec == 2 && n + 8 <= a.N) {
         if constexpr (YT == CHAM_T_F32) {
             *(float4v*)((float*)a.Y + i) = p;
             *(float4v*)((float*)a.Y + i + 4) = q;
@@ -151,8 +156,8 @@ typedef __attribute__((address_space(3))) uint8_t Lds;
 CHAM_DEV int key_x(int r) { return (r >> 1) & 7; }
 CHAM_DEV int key_w(int r) { return ((r >> 1) & 1) | ((r >> 3) & 3) << 1; }
 
-// channel (within a wavefront's 16 TN) of operand row rr of block t
-CHAM_DEV int chan(int t, int rr) { return (t >> 1) * 32 + (rr >> 2) * 8 + (t & 1) * 4 + (rr & 3); }
+// channel (within a run of 32) of operand row rr of the run's first block; 4 more in its second
+CHAM_DEV int chan(int rr) { return (rr >> 2) * 8 + (rr & 3); }
 
 // KS groups of WM x WN wavefronts: group q takes the k-steps q, q + KS, ... through buffers of its
 // own, and the groups' sums are added in their order at the end.
@@ -164,7 +169,15 @@ struct Tile {
     static constexpr int kLoads = kLoadsX + kLoadsW;
     static constexpr bool kSpread = TM * TN >= 16;  // loads of a step spread over its products
     static constexpr bool kFence = TM * TN >= 8;
-    static_assert(kWaves % 4 == 0 && TN % 2 == 0 && 128 % (16 * TN) == 0 && BN <= 256, "layout");
+    // A wavefront's channels are TN / 2 runs of 32, kRun apart, the first wavefront's from 0, the
+    // next one's from kNext.  They are one piece where that lies in one 128-block of the weights'
+    // scales; else the wavefronts take the runs in turn, so that each run of all wavefronts together
+    // (64 channels) lies in one block, and every run has a scale of its own.
+    static constexpr bool kOneBlock = 128 % (16 * TN) == 0;
+    static constexpr int kRun = kOneBlock ? 32 : 32 * WN, kNext = kOneBlock ? 16 * TN : 32;
+    static constexpr int kSlots = kOneBlock ? 1 : TN / 2;
+    static constexpr int chan(int i) { return (i >> 1) * kRun + (i & 1) * 4; }  // of operand block i
+    static_assert(kWaves % 4 == 0 && TN % 2 == 0 && BN <= 256 && (kOneBlock || 128 % kRun == 0), "layout");
     static_assert(KS == 1 || BM <= 64, "a group's sums fit its slices of two weight buffers");
 };
 
@@ -258,20 +271,26 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
 
     // scales of the lane's rows (one per 16-row block) and of the wavefront's channels
     const int rr = lane & 15, g = lane >> 4;
-    const int64_t wblk = min((n0 + wn * 16 * TN) / 128, ((int64_t)a.N - 1) / 128) * nkb;
-    const Scale* const wsp = (const Scale*)a.ws + wblk;
+    constexpr int kSlots = T::kSlots;
+    const Scale* wsp[kSlots];
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u)
+        wsp[u] = (const Scale*)a.ws + min((n0 + wn * T::kNext + u * T::kRun) / 128, ((int64_t)a.N - 1) / 128) * nkb;
     struct Factors {
-        Scale x[TM], w;
+        Scale x[TM], w[kSlots];
     };
     Factors s0, s1;
     auto scales = [&](Factors& s, int kb) {
-        const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
-            (void*)(wsp + min(kb, nkb - 1)), (short)0, (int)sizeof(Scale), kBufferFlags);
         // one block's scales from the tile's first row on; zeros past the last row
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
             (void*)((const Scale*)a.xs + (int64_t)min(kb, nkb - 1) * a.M + m0), (short)0, mrows * (int)sizeof(Scale), kBufferFlags);
-        if constexpr (byte_scales(MODE)) s.w = __builtin_amdgcn_raw_buffer_load_b8(rb, 0, 0, 0);
-        else s.w = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, 0, 0, 0));
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) {
+            const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
+                (void*)(wsp[u] + min(kb, nkb - 1)), (short)0, (int)sizeof(Scale), kBufferFlags);
+            if constexpr (byte_scales(MODE)) s.w[u] = __builtin_amdgcn_raw_buffer_load_b8(rb, 0, 0, 0);
+            else s.w[u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, 0, 0, 0));
+        }
 #pragma unroll
         for (int t = 0; t < TM; ++t) {
             const int o = (int)((wm * TM * 16 + rr) * sizeof(Scale) + t * 16 * sizeof(Scale));
@@ -287,9 +306,9 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
         for (int j = 0; j < TM; ++j) acc[i][j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 
     // byte offsets of the lane's two chunks: its key is the same in every 16-row block
-    const int x0 = group * kX + (wm * TM * 16 + rr) * BK, w0 = group * kW + (wn * 16 * TN + chan(0, rr)) * BK;
+    const int x0 = group * kX + (wm * TM * 16 + rr) * BK, w0 = group * kW + (wn * T::kNext + chan(rr)) * BK;
     const int xlo = x0 + ((g ^ key_x(rr)) << 4), xhi = x0 + (((g + 4) ^ key_x(rr)) << 4);
-    const int wlo = w0 + ((g ^ key_w(chan(0, rr))) << 4), whi = w0 + (((g + 4) ^ key_w(chan(0, rr))) << 4);
+    const int wlo = w0 + ((g ^ key_w(chan(rr))) << 4), whi = w0 + (((g + 4) ^ key_w(chan(rr))) << 4);
     auto operand = [&](const Lds* buf, int lo, int hi, int off) {
         Codes o;
         o.q[0] = *(const __attribute__((address_space(3))) int4v*)(buf + lo + off);
@@ -300,15 +319,21 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
     // The group's step j: X and W hold it, X and Wn take its step j + 2.
     auto step = [&](Lds* X, const Lds* W, Lds* Wn, Factors& s, int j) {
         const int next = __builtin_amdgcn_readfirstlane((j + 2) * KS + group);
-        landed_barrier<T::kLoads + TM + 1>();  // step j is there; W of step j - 1 is free
-        float f[TM];
-        Scale cx[TM], cw = s.w;
-        keep(cw);
+        landed_barrier<T::kLoads + TM + kSlots>();  // step j is there; W of step j - 1 is free
+        float f[kSlots][TM];
+        Scale cx[TM], cw[kSlots];
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) {
+            cw[u] = s.w[u];
+            keep(cw[u]);
+        }
 #pragma unroll
         for (int t = 0; t < TM; ++t) {
             cx[t] = s.x[t];
             keep(cx[t]);
-            if constexpr (MODE != kCodesPow2) f[t] = factor(cx[t]) * factor(cw);
+#pragma unroll
+            for (int u = 0; u < kSlots; ++u)
+                if constexpr (MODE != kCodesPow2) f[u][t] = factor(cx[t]) * factor(cw[u]);
         }
         Codes b[TM];
 #pragma unroll
@@ -331,7 +356,7 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
         // compiler from gathering all reads in front (more registers than there are).
         auto add = [&](int i, int t, const float4v& p) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) acc[i][t][q] = __builtin_fmaf(p[q], f[t], acc[i][t][q]);
+            for (int q = 0; q < 4; ++q) acc[i][t][q] = __builtin_fmaf(p[q], f[i * kSlots / TN][t], acc[i][t][q]);
         };
         // The loads of step j + 2 go out between the products, a few at a time: all at once they
         // hold up the wavefront until the memory pipe has taken them (1 KB each, 16 cycles or
@@ -354,7 +379,7 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
             float4v d[TM];
 #pragma unroll
             for (int i = 0; i < TN; ++i) {
-                if (i + 1 < TN) w[(i + 1) & 1] = operand(W, wlo, whi, chan(i + 1, 0) * BK);
+                if (i + 1 < TN) w[(i + 1) & 1] = operand(W, wlo, whi, T::chan(i + 1) * BK);
                 const Halves hw = to_half(w[i & 1]);
 #pragma unroll
                 for (int h = 0; h < 4; ++h)
@@ -370,12 +395,12 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
             float4v d[kLag + 1];
 #pragma unroll
             for (int i = 0; i < TN; ++i) {
-                if (i + 1 < TN) w[(i + 1) & 1] = operand(W, wlo, whi, chan(i + 1, 0) * BK);
+                if (i + 1 < TN) w[(i + 1) & 1] = operand(W, wlo, whi, T::chan(i + 1) * BK);
 #pragma unroll
                 for (int t = 0; t < TM; ++t) {
                     const int j = i * TM + t, k = j - kLag;
                     if constexpr (MODE == kCodesPow2) {
-                        acc[i][t] = mfma_pow2(w[i & 1], b[t], acc[i][t], cw, cx[t]);
+                        acc[i][t] = mfma_pow2(w[i & 1], b[t], acc[i][t], cw[i * kSlots / TN], cx[t]);
                     } else {
                         d[j & kLag] = mfma(w[i & 1], b[t], zero);
                         if (k >= 0) add(k / TM, k % TM, d[k & kLag]);
@@ -452,7 +477,7 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
         if (m < a.M) {
 #pragma unroll
             for (int i = 0; i < TN; i += 2)
-                store8<YT>(a, m, n0 + wn * 16 * TN + (i >> 1) * 32 + g * 8, acc[i][t], acc[i + 1][t]);
+                store8<YT>(a, m, n0 + wn * T::kNext + (i >> 1) * T::kRun + g * 8, acc[i][t], acc[i + 1][t]);
         }
     }
 }
@@ -596,21 +621,25 @@ int launch_few(BlockArgs a, hipStream_t s) {
 }
 
 // Modeled time (us) of one tile shape: the tiles of the busiest CU, each its k-steps and a fixed
-// part (first loads, output).  Fitted to 286 forced launches over 26 shapes (M 32 - 16384,
-// N 640 - 16384, K 320 - 8192; 3 sets of operands in turn); there the choice takes 0.6 % longer
-// than the best tile on average and 13 % at worst (8192 x 640 x 1920: 20.5 us against 18.1).
+// part (first loads, output).  A k-step among others is faster where the last round leaves CUs
+// idle (they share the clock and the L2s).  Fitted to forced launches of every tile over 33 shapes
+// (M 32 - 16384, N 512 - 10240, K 640 - 9216; 3 sets of operands in turn); there the choice takes
+// 0.5 % longer than the best tile on average and 10 % at worst (16384 x 640 x 640: 15.5 us against
+// 14.1).  f16 instructions: 27 shapes, 0.3 % and 4 %.
 struct TileCost {
     int bm, bn, ks;
     double lone, step, fixed;  // us: a k-step alone on a CU, among others, and the fixed part
 };
-enum { kT256, kT128, kT64, kT64x2, kT32, kT32x2, kTWide, kTiles };
+enum { kT256, kT192, kT128, kT64, kT64x2, kT32, kT32x2, kTWide, kTiles };
 // 8-bit matrix instructions
-constexpr TileCost kCostCodes[kTiles] = {{256, 256, 1, 1.13, 1.62, 6.0}, {128, 128, 1, 0.535, 0.492, 1.7},
+constexpr TileCost kCostCodes[kTiles] = {{256, 256, 1, 1.13, 1.48, 7.0}, {256, 192, 1, 0.95, 1.25, 7.5},
+                                         {128, 128, 1, 0.535, 0.492, 1.7},
                                          {64, 64, 1, 0.28, 0.20, 0.44},  {64, 64, 2, 0.375, 0.437, 1.33},
                                          {32, 64, 1, 0.24, 0.138, 0.30}, {32, 64, 2, 0.318, 0.267, 0.82},
                                          {0, 0, 0, 0, 0, 0}};
 // f16 matrix instructions
 constexpr TileCost kCostHalf[kTiles] = {{0, 0, 0, 0, 0, 0},              {0, 0, 0, 0, 0, 0},
+                                        {0, 0, 0, 0, 0, 0},
                                         {64, 64, 1, 0.43, 0.306, 0.82},  {64, 64, 2, 0.666, 0.727, 1.66},
                                         {32, 64, 1, 0.33, 0.20, 0.40},   {32, 64, 2, 0.493, 0.397, 0.98},
                                         {64, 128, 1, 0.64, 0.551, 1.66}};
@@ -624,7 +653,9 @@ int plan_tile(const BlockArgs& a, const TileCost* costs) {
         const TileCost& c = costs[i];
         if (c.bm == 0) continue;
         const int64_t tiles = ceil_div(a.M, c.bm) * ceil_div(a.N, c.bn), k = ceil_div(tiles, cus);
-        const double t = (double)k * ((double)ceil_div(a.nkb, c.ks) * (k == 1 ? c.lone : c.step) + c.fixed);
+        const double idle = 1.0 - (double)tiles / (double)(k * cus);  // share of the CUs' rounds without a tile
+        const double step = k == 1 ? c.lone : c.step * (1.0 - 0.2 * idle);
+        const double t = (double)k * ((double)ceil_div(a.nkb, c.ks) * step + c.fixed);
         if (best < 0 || t < least) { best = i; least = t; }
     }
     return best;
@@ -646,6 +677,9 @@ int launch_plan(const BlockArgs& a, hipStream_t s) {
         if (tile == kTWide) return launch_tile<Tile<2, 2, 2, 4, 1>, MODE, YT>(a, s);
     } else {
         if (tile == kT256) return launch_tile<Tile<4, 2, 4, 8, 1>, MODE, YT>(a, s);
+        // three quarters of a 256 x 256 tile: fewer CUs idle in the last round at some widths (8192 x
+        // 1152 x 4608 46.8 us against 51.0, 8192 x 1280 x 1280 19.8 against 21.5)
+        if (tile == kT192) return launch_tile<Tile<4, 2, 4, 6, 1>, MODE, YT>(a, s);
         if (tile == kT128) return launch_tile<Tile<2, 2, 4, 4, 1>, MODE, YT>(a, s);
     }
     if (tile == kT64) return launch_tile<Tile<2, 2, 2, 2, 1>, MODE, YT>(a, s);
@@ -691,7 +725,8 @@ extern "C" int cham_block_linear(const cham_bq* x, const cham_bw* w, void* Y, in
     a.N = (int)w->N;
     a.K = (int)x->K;
     a.nkb = (a.K + BK - 1) / BK;
-    a.vec = ((uintptr_t)Y & 15u) == 0 && ldy * size % 16 == 0;
+    const uint64_t at = (uint64_t)(uintptr_t)Y | (uint64_t)ldy * size;
+    a.vec = at % 16 == 0 ? 2 : at % 8 == 0 ? 1 : 0;
     const hipStream_t s = (hipStream_t)stream;
     if (y_type == CHAM_T_F32) return x->pow2 ? launch_plan<kHalfPow2, CHAM_T_F32>(a, s) : launch_plan<kHalf, CHAM_T_F32>(a, s);
     if (y_type == CHAM_T_F16) return x->pow2 ? launch_plan<kCodesPow2, CHAM_T_F16>(a, s) : launch_plan<kCodes, CHAM_T_F16>(a, s);

@@ -41,7 +41,8 @@ def test_every_step_holds_exactly_its_loads(kernels):
     for name, body in kernels:
         wm, wn, tm, tn, _ = map(int, re.search(r"TileILi(\d)ELi(\d)ELi(\d)ELi(\d)ELi(\d)E", name).groups())
         loads = (16 * tm * wm + 16 * tn * wn) // 8 // (wm * wn)
-        step = sorted("s" * (tm + 1) + "d" * loads)
+        scales = tm + (1 if 128 % (16 * tn) == 0 else tn // 2)  # of rows, and of blocks of weights
+        step = sorted("s" * scales + "d" * loads)
         parts = "".join(_events(body)).split("B")
         # in front of the first barrier: the first step's loads, then the second's
         n = len(step)

@@ -371,10 +371,11 @@ SHAPES = [(1, 1, 32, (16, 16, 8)), (1, 1280, 1280, (16, 16, 8)), (3, 77, 96, (16
           (40, 130, 2080, (16, 16, 8))]
 PLANS = {torch.bfloat16: [(17, 2061, 32, (32, 64, 1)), (100, 1030, 96, (32, 64, 1)), (70, 4100, 2080, (32, 64, 2)),
                           (1000, 2600, 96, (64, 64, 1)), (500, 1250, 3232, (64, 64, 2)), (3273, 911, 320, (128, 128, 1)),
-                          (4090, 4090, 1568, (256, 256, 1))],
+                          (4090, 4090, 1568, (256, 256, 1)), (4090, 2300, 800, (256, 192, 1)),
+                          (5000, 1910, 1568, (256, 192, 1))],
          torch.float32: [(17, 2081, 32, (32, 64, 1)), (100, 1030, 96, (32, 64, 1)), (70, 4100, 2080, (32, 64, 2)),
                          (1000, 2600, 96, (64, 64, 1)), (500, 1250, 3232, (64, 64, 2)), (1030, 5000, 672, (64, 128, 1))]}
-PLANS[torch.float16] = PLANS[torch.bfloat16][1:6]
+PLANS[torch.float16] = PLANS[torch.bfloat16][1:6] + PLANS[torch.bfloat16][7:8]
 
 
 def test_shapes_reach_every_plan():
@@ -406,7 +407,8 @@ def test_product_of_few_blocks(K):
 
 
 @pytest.mark.parametrize("pow2", [False, True])
-@pytest.mark.parametrize("M,N,K", [(4, 70, 288), (300, 700, 1184), (3273, 911, 320), (4090, 4090, 416)])
+@pytest.mark.parametrize("M,N,K", [(4, 70, 288), (300, 700, 1184), (3273, 911, 320), (4090, 4090, 416),
+                                   (4090, 2300, 800)])
 def test_product_of_small_integers_is_exact(M, N, K, pow2):
     """Codes of -2 .. 2 and scales that are powers of two: every sum is exact in every plan, so
     Y has to be the integer result, in binary32 and, where it fits 8 bits, in bfloat16."""

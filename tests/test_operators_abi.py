@@ -166,7 +166,8 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
 def test_every_plan_has_a_kernel_and_covers_the_chip():
     """Plans over a grid of sizes: one of the tiles that exist for the output's type; never the
     largest tile where it would leave most of the chip idle."""
-    kinds = {torch.bfloat16: {(16, 16, 8), (256, 256, 1), (128, 128, 1), (64, 64, 1), (64, 64, 2), (32, 64, 1), (32, 64, 2)},
+    kinds = {torch.bfloat16: {(16, 16, 8), (256, 256, 1), (256, 192, 1), (128, 128, 1), (64, 64, 1), (64, 64, 2), (32, 64, 1),
+                              (32, 64, 2)},
              torch.float32: {(16, 16, 8), (64, 128, 1), (64, 64, 1), (64, 64, 2), (32, 64, 1), (32, 64, 2)}}
     for dt, known in kinds.items():
         seen = set()
@@ -176,7 +177,7 @@ def test_every_plan_has_a_kernel_and_covers_the_chip():
                     p = cham.block_linear_plan(M, N, K, dt)
                     assert p in known, (M, N, K, dt, p)
                     if p[0] == 256:
-                        assert M * N >= 64 * 65536, (M, N, K)
+                        assert M * N >= 64 * p[0] * p[1], (M, N, K)
                     seen.add(p)
         assert seen == known, known - seen
     assert cham.block_linear_plan(512, 640, 640, torch.float16) == cham.block_linear_plan(512, 640, 640, torch.bfloat16)
