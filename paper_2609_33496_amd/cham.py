@@ -6,7 +6,9 @@ shared library is missing or a call fails, an exception is raised.
 
 Functions keep the C names without the ``cham_`` prefix:
 ``select_weight_formats``, ``act_stats_reset``, ``act_stats_accumulate``,
-``build_act_lut``, ``quantize_act``, ``quantize_act_lut``, ``mixed_linear``.
+``build_act_lut``, ``quantize_act``, ``quantize_act_lut``, ``mixed_linear``;
+around 8-bit linear layers ``rms_norm_quantize``, ``gated_quantize`` (each with either of the
+C functions for its output format), ``block_quantize_weights``, ``block_linear``.
 """
 from __future__ import annotations
 
@@ -741,12 +743,13 @@ def _cdiv(a: int, b: int) -> int:
 
 def _scales(scale, rows, cols, codes, n, k) -> int:
     """Check a block-format pair of tensors; whether its scales are powers of two."""
-    if codes.dtype is not torch.uint8 or codes.shape != (n, k) or not codes.is_contiguous() or not codes.is_cuda:
+    at = codes.get_device()  # negative on the host; cheaper than a comparison of device objects
+    if at < 0 or codes.dtype is not torch.uint8 or codes.shape != (n, k) or not codes.is_contiguous():
         raise ValueError(f"codes must be a contiguous device uint8 [{n}, {k}]")
     pow2 = scale.dtype is torch.uint8
     if (not pow2 and scale.dtype is not torch.float32) or scale.shape != (rows, cols) or not scale.is_contiguous():
         raise ValueError(f"scale must be a contiguous float32 or uint8 [{rows}, {cols}]")
-    if scale.device != codes.device:
+    if scale.get_device() != at:
         raise ValueError("codes and scale must be on one device")
     return int(pow2)
 
@@ -772,16 +775,16 @@ def _matrix(t: torch.Tensor, name: str, shape=None, device=None) -> int:
         raise ValueError(f"{name} must be float32, float16 or bfloat16")
     if t.shape != shape if shape is not None else t.dim() != 2:
         raise ValueError(f"{name} must be a matrix" + (f" of shape {tuple(shape)}" if shape is not None else ""))
-    if t.device != device if device is not None else not t.is_cuda:
+    if t.get_device() != device.index if device is not None else not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor" + (f" on {device}" if device is not None else ""))
     if not t.is_contiguous() and t.stride(1) != 1 and t.shape[1] > 1:
         raise ValueError(f"{name} must have unit stride along its columns")
     return ty
 
 
-def _ld(t: torch.Tensor) -> int:
+def _ld(t: torch.Tensor, rows: int, cols: int) -> int:
     """Row stride in elements; a single row's stride says nothing, so it counts as packed."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.stride(0) if rows > 1 else cols
 
 
 # the current device and its current stream's handle, without the stream object that
@@ -850,14 +853,14 @@ def rms_norm_quantize(X: torch.Tensor, weight: Optional[torch.Tensor] = None, ep
     rt = r_ptr = ldr = h_ptr = ldh = gt = g_ptr = 0
     if residual is not None:
         rt = _matrix(residual, "residual", X.shape, dev)
-        r_ptr, ldr = residual.data_ptr(), _ld(residual)
+        r_ptr, ldr = residual.data_ptr(), _ld(residual, M, K)
         if residual_out is None:
             residual_out = _empty(M, K, residual.dtype, dev, stream)
             ldh = K
         elif _matrix(residual_out, "residual_out", X.shape, dev) != rt:
             raise ValueError("residual_out must have the residual's type")
         else:
-            ldh = _ld(residual_out)
+            ldh = _ld(residual_out, M, K)
         h_ptr = residual_out.data_ptr()
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
@@ -867,7 +870,7 @@ def rms_norm_quantize(X: torch.Tensor, weight: Optional[torch.Tensor] = None, ep
             raise ValueError(f"weight must be a contiguous float32, float16 or bfloat16 [{K}] on {dev}")
         g_ptr = weight.data_ptr()
     out, st = _row_out(out, fmt, M, K, dev, pow2, stream)
-    n = _Norm(M, K, X.data_ptr(), _ld(X), r_ptr, ldr, h_ptr, ldh, g_ptr, xt, rt, gt, eps)
+    n = _Norm(M, K, X.data_ptr(), _ld(X, M, K), r_ptr, ldr, h_ptr, ldh, g_ptr, xt, rt, gt, eps)
     if fmt == A_BLOCK128:
         rc = _on_device(dev, stream, lib().cham_rms_norm_quantize_block, ctypes.byref(n), ctypes.byref(st))
     else:
@@ -889,9 +892,9 @@ def gated_quantize(X: torch.Tensor, up: Optional[torch.Tensor] = None, act: int 
     if up is not None:
         if _matrix(up, "up", X.shape, dev) != xt:
             raise ValueError("X and up must have one type")
-        u_ptr, ldu = up.data_ptr(), _ld(up)
+        u_ptr, ldu = up.data_ptr(), _ld(up, M, K)
     out, st = _row_out(out, fmt, M, K, dev, pow2, stream)
-    g = _Gate(M, K, X.data_ptr(), _ld(X), u_ptr, ldu, xt, act)
+    g = _Gate(M, K, X.data_ptr(), _ld(X, M, K), u_ptr, ldu, xt, act)
     if fmt == A_BLOCK128:
         rc = _on_device(dev, stream, lib().cham_gated_quantize_block, ctypes.byref(g), ctypes.byref(st))
     else:
@@ -915,7 +918,7 @@ def block_quantize_weights(W: torch.Tensor, pow2: bool = False, out: Optional[BW
         raise ValueError("out does not fit W and pow2")
     else:
         st = out.struct()
-    rc = _on_device(dev, stream, lib().cham_block_quantize_weights, W.data_ptr(), ty, _ld(W), ctypes.byref(st))
+    rc = _on_device(dev, stream, lib().cham_block_quantize_weights, W.data_ptr(), ty, _ld(W, N, K), ctypes.byref(st))
     _check(rc, "block_quantize_weights")
     return out
 
@@ -926,7 +929,7 @@ def block_linear(xb: BQ, wb: BW, Y: Optional[torch.Tensor] = None, dtype: torch.
     decides the type where it is given, else dtype."""
     dev = xb.codes.device
     a, w = xb.struct(), wb.struct()
-    if wb.codes.device != dev:
+    if wb.codes.get_device() != dev.index:
         raise ValueError(f"the weights must be on {dev}")
     if Y is None:
         ty, ld = _TYPES.get(dtype), wb.N
@@ -934,7 +937,7 @@ def block_linear(xb: BQ, wb: BW, Y: Optional[torch.Tensor] = None, dtype: torch.
             raise ValueError("dtype must be float32, float16 or bfloat16")
         Y = _empty(xb.M, ld, dtype, dev, stream)
     else:
-        ty, ld = _matrix(Y, "Y", (xb.M, wb.N), dev), _ld(Y)
+        ty, ld = _matrix(Y, "Y", (xb.M, wb.N), dev), _ld(Y, xb.M, wb.N)
     rc = _on_device(dev, stream, lib().cham_block_linear, ctypes.byref(a), ctypes.byref(w), Y.data_ptr(), ty, ld)
     _check(rc, "block_linear")
     return Y
