@@ -150,6 +150,17 @@ CHAM_DEV void store8(const BlockArgs& a, int64_t m, int64_t n, float4v p, float4
 // that read one chunk of 16 rows in one operand load then spread over all banks (no conflicts
 // counted).  The channel order inside a wavefront's block is chosen so that a lane's results of
 // two neighbouring operand blocks are 8 consecutive channels of Y.
+//
+// What bounds it, in tiles of 256 x 256: a step's products hold the matrix cores for 2048 cycles,
+// and its LDS traffic (192 KB read, 64 KB written, 128 bytes a cycle) takes as many; the reads of
+// the activations at a step's start overlap with no product.  8192 x 8192 x 8192: 445 us with
+// binary32 scales (2.47 PFLOP/s, matrix cores busy 64 %), 402 with powers of two (2.73); the
+// library's 8-bit product with one scale per tensor 337 (3.27).  Smaller tiles read more LDS per
+// product (128 x 128: 64 KB for 512 cycles; 2048 x 10240 x 1280 35.4 us, 1.52 PFLOP/s); the
+// smallest are bound by the loads into one CU's LDS (about 85 bytes a ns).  f16 route: 8192 x 8192
+// x 8192 1180 us (0.93 PFLOP/s), 240 x 1152 x 4096 12.2 us (144 workgroups, conversions and LDS
+// latency in turn at 0.5 us a step).
+//
 // bytes of LDS; the address space is part of the type, so that reads of it cannot become others
 typedef __attribute__((address_space(3))) uint8_t Lds;
 
@@ -488,7 +499,8 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
 // A workgroup makes 16 TM rows x 16 TN channels; wavefront v of NW takes the k-steps v, v + NW,
 // ...  With few rows every weight is read by few workgroups, so LDS would only stand in the way:
 // a lane loads its operands of the next step while it multiplies.  The partial sums meet in LDS
-// and are added in the order of the wavefronts (no second launch, no atomics).
+// and are added in the order of the wavefronts (no second launch, no atomics).  Bound by the
+// weights' bytes and the launch: 1 x 10240 x 1280 5.2 us (13 MB, 2.5 TB/s).
 template <int TM, int TN, int NW, int MODE, int YT>
 __global__ __launch_bounds__(NW * 64) void few_rows_kernel(BlockArgs a) {
     using Scale = typename ScaleOf<byte_scales(MODE)>::type;
