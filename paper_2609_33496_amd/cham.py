@@ -719,8 +719,8 @@ class BQ:
     scale: torch.Tensor              # [ceil(K / 128), M]
 
     def struct(self) -> _BQ:
-        return _BQ(self.M, self.K, _scales(self.scale, _cdiv(self.K, BLOCK), self.M, self.codes, self.M, self.K),
-                   self.codes.data_ptr(), self.scale.data_ptr())
+        M, K, codes, scale = self.M, self.K, self.codes, self.scale
+        return _BQ(M, K, _scales(scale, _cdiv(K, BLOCK), M, codes, M, K), codes.data_ptr(), scale.data_ptr())
 
 
 @dataclass
@@ -732,9 +732,8 @@ class BW:
     scale: torch.Tensor              # [ceil(N / 128), ceil(K / 128)]
 
     def struct(self) -> _BW:
-        return _BW(self.N, self.K,
-                   _scales(self.scale, _cdiv(self.N, BLOCK), _cdiv(self.K, BLOCK), self.codes, self.N, self.K),
-                   self.codes.data_ptr(), self.scale.data_ptr())
+        N, K, codes, scale = self.N, self.K, self.codes, self.scale
+        return _BW(N, K, _scales(scale, _cdiv(N, BLOCK), _cdiv(K, BLOCK), codes, N, K), codes.data_ptr(), scale.data_ptr())
 
 
 def _cdiv(a: int, b: int) -> int:

@@ -158,7 +158,7 @@ CHAM_DEV void store8(const BlockArgs& a, int64_t m, int64_t n, float4v p, float4
 // library's 8-bit product with one scale per tensor 337 (3.27).  Smaller tiles read more LDS per
 // product (128 x 128: 64 KB for 512 cycles; 2048 x 10240 x 1280 35.4 us, 1.52 PFLOP/s); the
 // smallest are bound by the loads into one CU's LDS (about 85 bytes a ns).  f16 route: 8192 x 8192
-// x 8192 1180 us (0.93 PFLOP/s), 240 x 1152 x 4096 12.2 us (144 workgroups, conversions and LDS
+// x 8192 1220 us (0.90 PFLOP/s), 240 x 1152 x 4096 11.3 us (144 workgroups, conversions and LDS
 // latency in turn at 0.5 us a step).
 //
 // bytes of LDS; the address space is part of the type, so that reads of it cannot become others
@@ -236,6 +236,74 @@ CHAM_DEV void read_barrier() {
     __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);  // lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     order_loads();
+}
+
+// A wavefront's part of the tile where rows of Y are not aligned: 16 rows at a time pass through
+// LDS (16-byte chunks swizzled by the row), so that neighbouring lanes store neighbouring elements
+// of a row: 4 bytes each, and where a row starts between two such words its first and last element
+// alone.  Each lane storing its own 8 elements one by one took 45.7 us for bfloat16 3001 x 4001 x
+// 1280, now 32.9; binary32 67.0, now 45.7.
+template <class T, int YT>
+CHAM_DEV void store_through_lds(const BlockArgs& a, const float4v (&acc)[T::TN][T::TM], Lds* buf, int64_t m0, int64_t n0,
+                                int lane) {
+    typedef __attribute__((address_space(3))) int4v Lds16;
+    typedef __attribute__((address_space(3))) uint32_t Lds4;
+    typedef __attribute__((address_space(3))) uint16_t Lds2;
+    constexpr bool kWide = YT == CHAM_T_F32;
+    constexpr int kSize = kWide ? 4 : 2, W = 16 * T::TN, kRow = W * kSize;
+    constexpr int kMask = kRow / 16 % 8 == 0 ? 7 : 3;
+    constexpr int kSeg = T::kOneBlock ? W : 32;          // consecutive channels
+    constexpr int P = kWide ? kSeg : kSeg / 2, R = 64 / P;  // lanes a row, rows an instruction
+    static_assert(16 * kRow * T::kWaves <= T::BN * BK && 64 % P == 0 && kRow / 16 % (kMask + 1) == 0, "layout");
+    const int rr = lane & 15, g = lane >> 4;
+    auto at = [&](int row, int e) { return buf + row * kRow + (((e * kSize >> 4) ^ (row & kMask)) << 4) + (e * kSize & 15); };
+#pragma unroll
+    for (int t = 0; t < T::TM; ++t) {
+        order_loads();  // the rows before are in registers
+#pragma unroll
+        for (int i = 0; i < T::TN; i += 2) {
+            const float4v p = acc[i][t], q = acc[i + 1][t];
+            const int e = i * 16 + g * 8;
+            if constexpr (kWide) {
+                *(Lds16*)at(rr, e) = __builtin_bit_cast(int4v, p);
+                *(Lds16*)at(rr, e + 4) = __builtin_bit_cast(int4v, q);
+            } else {
+                *(Lds16*)at(rr, e) = int4v{(int)narrow<YT>(p[0], p[1]), (int)narrow<YT>(p[2], p[3]), (int)narrow<YT>(q[0], q[1]),
+                                           (int)narrow<YT>(q[2], q[3])};
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        order_loads();  // one wavefront's LDS accesses are done in their order
+#pragma unroll
+        for (int sg = 0; sg < W / kSeg; ++sg) {
+            const int64_t n = n0 + sg * T::kRun;
+#pragma unroll
+            for (int r = 0; r < 16; r += R) {
+                const int row = r + lane / P, d = lane % P;
+                const int64_t m = m0 + t * 16 + row, i = m * a.ldy + n;
+                if constexpr (kWide) {
+                    const uint32_t v = *(Lds4*)at(row, sg * kSeg + d);
+                    if (m < a.M && n + d < a.N) ((uint32_t*)a.Y)[i + d] = v;
+                } else {
+                    const int odd = (int)(((uint64_t)(uintptr_t)a.Y / 2 + (uint64_t)i) & 1), e = 2 * d - odd;
+                    const uint32_t lo = *(Lds2*)at(row, sg * kSeg + max(e, 0)), hi = *(Lds2*)at(row, sg * kSeg + e + 1);
+                    uint16_t* const y = (uint16_t*)a.Y + i + e;
+                    if (m < a.M) {
+                        if (e >= 0 && n + e + 1 < a.N) *(uint32_t*)y = lo | hi << 16;
+                        else if (e < 0 && n < a.N) y[1] = (uint16_t)hi;
+                        else if (e >= 0 && n + e < a.N) y[0] = (uint16_t)lo;
+                    }
+                }
+            }
+            if constexpr (!kWide) {  // the last element of the rows that start between words
+                const int64_t m = m0 + t * 16 + rr, i = m * a.ldy + n + kSeg - 1;
+                const uint16_t v = *(Lds2*)at(rr, sg * kSeg + kSeg - 1);
+                // its word's lower half: the row's start, an odd number of elements before, is an upper one
+                if (g == 0 && (((uint64_t)(uintptr_t)a.Y / 2 + (uint64_t)i) & 1) == 0 && m < a.M && n + kSeg - 1 < a.N)
+                    ((uint16_t*)a.Y)[i] = v;
+            }
+        }
+    }
 }
 
 template <class T, int MODE, int YT>
@@ -397,7 +465,10 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
 #pragma unroll
                     for (int t = 0; t < TM; ++t) d[t] = mfma_half(hw.h[h], hb[t].h[h], h == 0 ? zero : d[t]);
 #pragma unroll
-                for (int t = 0; t < TM; ++t) add(i, t, d[t]);
+                for (int t = 0; t < TM; ++t) {
+                    add(i, t, d[t]);
+                    asm volatile("" : "+v"(acc[i][t]));  // in place: each exit of the loop took registers of its own
+                }
                 if constexpr (T::kFence) __builtin_amdgcn_sched_barrier(0);
                 spread(i);
             }
@@ -460,11 +531,12 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
         if (j + 6 >= steps) break;
     }
     landed_barrier<0>();  // no write to LDS outlives the workgroup or meets the sums below
+    const int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));  // the lane, in no register till here
 
     if constexpr (KS > 1) {
         auto part = [&](int q, int i, int t) {  // block (i, t) of this wavefront's counterpart in group q
             float4v* p = (float4v*)((i < TN / 2 ? W0 : W1) + q * kW);
-            return p + ((wave * (TN / 2) + i % (TN / 2)) * TM + t) * 64 + lane;
+            return p + ((wave * (TN / 2) + i % (TN / 2)) * TM + t) * 64 + l;
         };
         if (group > 0) {
 #pragma unroll
@@ -482,13 +554,20 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
                 for (int t = 0; t < TM; ++t) acc[i][t] += *part(q, i, t);
     }
 
+    // 16-bit rows that start at multiples of 8 bytes are stored directly too (8192 x 2300 x 1280
+    // 35.3 us, through LDS 45.4)
+    if (a.vec < (YT == CHAM_T_F32 ? 2 : 1)) {
+        Lds* const buf = (Lds*)W0 + wave * (16 * 16 * TN * (YT == CHAM_T_F32 ? 4 : 2));
+        store_through_lds<T, YT>(a, acc, buf, m0 + wm * TM * 16, n0 + wn * T::kNext, l);
+        return;
+    }
 #pragma unroll
     for (int t = 0; t < TM; ++t) {
-        const int64_t m = m0 + (wm * TM + t) * 16 + rr;
+        const int64_t m = m0 + (wm * TM + t) * 16 + (l & 15);
         if (m < a.M) {
 #pragma unroll
             for (int i = 0; i < TN; i += 2)
-                store8<YT>(a, m, n0 + wn * T::kNext + (i >> 1) * T::kRun + g * 8, acc[i][t], acc[i + 1][t]);
+                store8<YT>(a, m, n0 + wn * T::kNext + (i >> 1) * T::kRun + (l >> 4) * 8, acc[i][t], acc[i + 1][t]);
         }
     }
 }
@@ -633,40 +712,41 @@ int launch_few(BlockArgs a, hipStream_t s) {
 }
 
 // Modeled time (us) of one tile shape: the tiles of the busiest CU, each its k-steps and a fixed
-// part (first loads, output).  A k-step among others is faster where the last round leaves CUs
-// idle (they share the clock and the L2s).  Fitted to forced launches of every tile over 33 shapes
-// (M 32 - 16384, N 512 - 10240, K 640 - 9216; 3 sets of operands in turn); there the choice takes
-// 0.5 % longer than the best tile on average and 10 % at worst (16384 x 640 x 640: 15.5 us against
-// 14.1).  f16 instructions: 27 shapes, 0.3 % and 4 %.
+// part (first loads, output).  8-bit instructions: a k-step among others is a little faster where
+// the last round leaves CUs idle.  Fitted to forced launches of every tile over 33 shapes (M 32 -
+// 16384, N 512 - 10240, K 512 - 9216; 3 sets of operands in turn); there the choice takes 0.5 %
+// longer than the best tile on average and 10 % at worst (16384 x 640 x 640: 15.5 us against 14.1).
+// f16 instructions: 33 shapes, 0.4 % and 6 % (120 x 4608 x 1152: 7.2 us against 6.8).
 struct TileCost {
     int bm, bn, ks;
     double lone, step, fixed;  // us: a k-step alone on a CU, among others, and the fixed part
 };
 enum { kT256, kT192, kT128, kT64, kT64x2, kT32, kT32x2, kTWide, kTiles };
+struct Costs {
+    TileCost tile[kTiles];
+    double idle;  // share of a k-step that a round without tiles would save
+};
 // 8-bit matrix instructions
-constexpr TileCost kCostCodes[kTiles] = {{256, 256, 1, 1.13, 1.48, 7.0}, {256, 192, 1, 0.95, 1.25, 7.5},
-                                         {128, 128, 1, 0.535, 0.492, 1.7},
-                                         {64, 64, 1, 0.28, 0.20, 0.44},  {64, 64, 2, 0.375, 0.437, 1.33},
-                                         {32, 64, 1, 0.24, 0.138, 0.30}, {32, 64, 2, 0.318, 0.267, 0.82},
-                                         {0, 0, 0, 0, 0, 0}};
+constexpr Costs kCostCodes = {{{256, 256, 1, 1.13, 1.48, 7.0}, {256, 192, 1, 0.95, 1.25, 7.5}, {128, 128, 1, 0.535, 0.492, 1.7},
+                               {64, 64, 1, 0.28, 0.20, 0.44}, {64, 64, 2, 0.375, 0.437, 1.33},
+                               {32, 64, 1, 0.24, 0.138, 0.30}, {32, 64, 2, 0.318, 0.267, 0.82},
+                               {0, 0, 0, 0, 0, 0}}, 0.2};
 // f16 matrix instructions
-constexpr TileCost kCostHalf[kTiles] = {{0, 0, 0, 0, 0, 0},              {0, 0, 0, 0, 0, 0},
-                                        {0, 0, 0, 0, 0, 0},
-                                        {64, 64, 1, 0.43, 0.306, 0.82},  {64, 64, 2, 0.666, 0.727, 1.66},
-                                        {32, 64, 1, 0.33, 0.20, 0.40},   {32, 64, 2, 0.493, 0.397, 0.98},
-                                        {64, 128, 1, 0.64, 0.551, 1.66}};
+constexpr Costs kCostHalf = {{{0, 0, 0, 0, 0, 0}, {0, 0, 0, 0, 0, 0}, {0, 0, 0, 0, 0, 0},
+                              {64, 64, 1, 0.409, 0.298, 0.747}, {64, 64, 2, 0.685, 0.596, 1.264},
+                              {32, 64, 1, 0.323, 0.192, 0.442}, {32, 64, 2, 0.484, 0.389, 0.99},
+                              {64, 128, 1, 0.64, 0.534, 1.524}}, 0.0};
 
-
-int plan_tile(const BlockArgs& a, const TileCost* costs) {
+int plan_tile(const BlockArgs& a, const Costs& costs) {
     const int cus = cham_device_cus();
     int best = -1;
     double least = 0.0;
     for (int i = 0; i < kTiles; ++i) {
-        const TileCost& c = costs[i];
+        const TileCost& c = costs.tile[i];
         if (c.bm == 0) continue;
         const int64_t tiles = ceil_div(a.M, c.bm) * ceil_div(a.N, c.bn), k = ceil_div(tiles, cus);
         const double idle = 1.0 - (double)tiles / (double)(k * cus);  // share of the CUs' rounds without a tile
-        const double step = k == 1 ? c.lone : c.step * (1.0 - 0.2 * idle);
+        const double step = k == 1 ? c.lone : c.step * (1.0 - costs.idle * idle);
         const double t = (double)k * ((double)ceil_div(a.nkb, c.ks) * step + c.fixed);
         if (best < 0 || t < least) { best = i; least = t; }
     }
@@ -760,7 +840,8 @@ extern "C" int cham_block_linear_plan(int64_t M, int64_t N, int64_t K, int32_t y
         out[2] = 8;
         return CHAM_OK;
     }
-    const TileCost& c = (half ? kCostHalf : kCostCodes)[plan_tile(a, half ? kCostHalf : kCostCodes)];
+    const Costs& costs = half ? kCostHalf : kCostCodes;
+    const TileCost& c = costs.tile[plan_tile(a, costs)];
     out[0] = c.bm;
     out[1] = c.bn;
     out[2] = c.ks;

@@ -598,7 +598,9 @@ int out_token(int32_t fmt, cham_aq* q, int64_t M, int64_t K, Out* o) {
 }
 
 // Lanes per row: a wavefront where its registers hold the row (no barrier, four rows per
-// workgroup), else 256 or 1024 lanes.
+// workgroup), else 256 or 1024 lanes.  Norm, us: 8100 x 640, E4M3 per token, 64 lanes 9.0 and 256
+// lanes 15.3; 8192 x 1152, INT8 per token 22.4 and 25.5, block format 21.7 and 20.7; one row of 1280
+// 3.8 and 2.8 (under a host call of 10); 4096 x 5120, 256 lanes 56.1 and 1024 lanes 65.9.
 int team(int64_t K) {
     return K <= kWave * kV * kChunk ? kWave : K <= 256 * kV * kChunk ? 256 : 1024;
 }

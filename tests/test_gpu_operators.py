@@ -464,6 +464,23 @@ def test_product_into_strided_and_unaligned_rows(dt, pad, off):
         assert bool((buf[:, :off] == 7.0).all()) and bool((buf[:, off + N:] == 7.0).all())
 
 
+@pytest.mark.parametrize("pow2", [False, True])
+@pytest.mark.parametrize("dt,M,N,K", [(dt, *s[:3]) for dt in DTS for s in PLANS[dt]])
+def test_every_plan_into_rows_of_any_alignment(dt, M, N, K, pow2):
+    """The same bits as into 16-byte aligned rows, from any element on and at any row stride, and
+    nothing beside them."""
+    xb, wb, _, _ = _operands(M + K, M, N, K, pow2)
+    full = -(-N // 8) * 8
+    want = cham.block_linear(xb, wb, torch.empty((M, full), dtype=dt, device=DEV)[:, :N])
+    for off, width in ((0, full + 1), (1, full + 1), (1, full + 2), (2, full + 4), (4, full + 4), (3, full + 8)):
+        case(f"alignment M={M} N={N} K={K} {dt} pow2={pow2} off={off} width={width}")
+        width = max(width, N + off)
+        buf = torch.full((M + 1, width), 7.0, dtype=dt, device=DEV)
+        cham.block_linear(xb, wb, buf[:M, off:off + N])
+        assert torch.equal(buf[:M, off:off + N], want), (off, width)
+        assert bool((buf[:, :off] == 7.0).all()) and bool((buf[:, off + N:] == 7.0).all()) and bool((buf[M] == 7.0).all())
+
+
 def test_empty_and_refused_calls():
     case("empty calls")
     xb = cham.gated_quantize(torch.zeros(0, 64, device=DEV), None, cham.ACT_NONE)
