@@ -429,13 +429,17 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
             }
         }
         // Operand block i + 1 is read from LDS while block i is multiplied, and 8-bit products are
-        // scaled and added behind later ones, so that no instruction waits for the one before it.  The scheduling groups interleave matrix and
-        // vector instructions evenly (16 additions behind 4 products left the matrix cores idle
-        // in between: 8192 x 8192 x 8192 in 256 x 256 tiles 476 us -> 455); the fences keep the
-        // compiler from gathering all reads in front (more registers than there are).
+        // scaled and added behind later ones, so that no instruction waits for the one before it.
+        // The scheduling groups interleave matrix and vector instructions evenly (16 additions
+        // behind 4 products left the matrix cores idle in between: 8192 x 8192 x 8192 in 256 x 256
+        // tiles 476 us -> 455); the fences keep the compiler from gathering all reads in front (more
+        // registers than there are).  Small tiles add in place: each exit of the loop took registers
+        // of its own for the sums (64 x 64 with two k groups 145 registers, now 73; 2048 x 10240 x
+        // 1280 in such tiles 73.4 us -> 56.6).
         auto add = [&](int i, int t, const float4v& p) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) acc[i][t][q] = __builtin_fmaf(p[q], f[i * kSlots / TN][t], acc[i][t][q]);
+            if constexpr (!T::kSpread) asm volatile("" : "+v"(acc[i][t]));
         };
         // The loads of step j + 2 go out between the products, a few at a time: all at once they
         // hold up the wavefront until the memory pipe has taken them (1 KB each, 16 cycles or
@@ -465,10 +469,7 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
 #pragma unroll
                     for (int t = 0; t < TM; ++t) d[t] = mfma_half(hw.h[h], hb[t].h[h], h == 0 ? zero : d[t]);
 #pragma unroll
-                for (int t = 0; t < TM; ++t) {
-                    add(i, t, d[t]);
-                    asm volatile("" : "+v"(acc[i][t]));  // in place: each exit of the loop took registers of its own
-                }
+                for (int t = 0; t < TM; ++t) add(i, t, d[t]);
                 if constexpr (T::kFence) __builtin_amdgcn_sched_barrier(0);
                 spread(i);
             }
@@ -728,7 +729,7 @@ struct Costs {
 };
 // 8-bit matrix instructions
 constexpr Costs kCostCodes = {{{256, 256, 1, 1.13, 1.48, 7.0}, {256, 192, 1, 0.95, 1.25, 7.5}, {128, 128, 1, 0.535, 0.492, 1.7},
-                               {64, 64, 1, 0.28, 0.20, 0.44}, {64, 64, 2, 0.375, 0.437, 1.33},
+                               {64, 64, 1, 0.28, 0.20, 0.44}, {64, 64, 2, 0.375, 0.37, 1.3},
                                {32, 64, 1, 0.24, 0.138, 0.30}, {32, 64, 2, 0.318, 0.267, 0.82},
                                {0, 0, 0, 0, 0, 0}}, 0.2};
 // f16 matrix instructions
