@@ -493,8 +493,8 @@ typedef struct cham_norm {
 
 /* The norm of n, written in the block format (out->M, K equal n's).
  * Errors: CHAM_EINVAL (NULL, sizes, strides, alignment, eps), CHAM_EFORMAT (types),
- * CHAM_ESHAPE (K % 32, K > 32768, M >= 2^31, or a launch of 2^32 lanes: M 64 lanes up to K =
- * 2048, 256 up to 8192, then 1024), CHAM_EHIP. */
+ * CHAM_ESHAPE (K % 32, K > 32768, M >= 2^31, or a launch of 2^32 lanes: a row takes 64 up to
+ * K = 2048, 256 up to 8192, then 1024), CHAM_EHIP. */
 int cham_rms_norm_quantize_block(const cham_norm* n, cham_bq* out, void* stream);
 
 /* The norm of n, written in activation format fmt of section 3 with dynamic scales of each

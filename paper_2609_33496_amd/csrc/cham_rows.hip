@@ -359,11 +359,11 @@ struct NormArgs {
 
 // h = x + r, y = h / sqrt(mean h^2 + eps) g, then the codes of y.  The whole row is loaded before
 // its first use (up to 4 chunks a lane in flight), so one wavefront per row with no barrier holds
-// rows up to 2048 and workgroups the longer ones.  h goes past the caches (nothing here reads it
+// rows up to 2048, and workgroups the longer ones and those of few rows.  h goes past the caches (nothing here reads it
 // again soon), the codes stay in them for the product that follows.
 // Measured: bfloat16 x, binary32 residual, 8192 x 1152, block output 19.8 us (104 MB, 5.2 TB/s:
 // memory); binary32 x alone, 8100 x 640, E4M3 per token 9.3 us (26 MB, 2.8 TB/s: 64 lanes cover 640
-// in two chunks, the second a quarter full); 1 x 1280 3.6 us (a launch).
+// in two chunks, the second a quarter full); 1 x 1280 2.8 us in a graph (a launch).
 // RT: type of the residual, or -1 for none
 template <int XT, int RT, int T, int OUT>
 __global__ __launch_bounds__(wg_threads<T>()) void norm_kernel(NormArgs a) {
@@ -598,15 +598,19 @@ int out_token(int32_t fmt, cham_aq* q, int64_t M, int64_t K, Out* o) {
 }
 
 // Lanes per row: a wavefront where its registers hold the row (no barrier, four rows per
-// workgroup), else 256 or 1024 lanes.  Norm, us: 8100 x 640, E4M3 per token, 64 lanes 9.0 and 256
-// lanes 15.3; 8192 x 1152, INT8 per token 22.4 and 25.5, block format 21.7 and 20.7; one row of 1280
-// 3.8 and 2.8 (under a host call of 10); 4096 x 5120, 256 lanes 56.1 and 1024 lanes 65.9.
-int team(int64_t K) {
-    return K <= kWave * kV * kChunk ? kWave : K <= 256 * kV * kChunk ? 256 : 1024;
+// workgroup), else 256 or 1024 lanes.  Rows of more than a chunk per lane take 256 lanes too where
+// there are at most two of them per CU: latency counts there, and a lane's chunks are worked off in
+// turn.  Norm, us: 8100 x 640, E4M3 per token, 64 lanes 9.0 and 256 lanes 15.3; 8192 x 1152, INT8 per
+// token 22.4 and 25.5, block format 21.7 and 20.7; 4096 x 5120, 256 lanes 56.1 and 1024 lanes 65.9;
+// but 1 x 1152, 64 lanes 3.9 and 256 lanes 2.8, 1 x 2048 4.5 and 2.8, 512 x 1152 4.6 and 3.7, 512 x 640,
+// INT8 4.4 and 4.5; 1024 x 640 4.0 and 4.2.
+int team(int64_t M, int64_t K) {
+    if (K <= kWave * kChunk || (K <= kWave * kV * kChunk && M > 2 * (int64_t)cham_device_cus())) return kWave;
+    return K <= 256 * kV * kChunk ? 256 : 1024;
 }
 int64_t row_grid(int64_t M, int T) { return T == kWave ? (M + 3) / 4 : M; }
 bool rows_launchable(int64_t M, int64_t K) {
-    const int T = team(K);
+    const int T = team(M, K);
     return cham_launchable(row_grid(M, T), std::max(T, 256));
 }
 // workgroups of the block and MX forms of the gate
@@ -614,7 +618,7 @@ int64_t gate_grid(int64_t M, int64_t K) { return (M * ((K + 127) / 128) + kGateP
 
 template <int XT, int RT, int OUT>
 void launch_norm_t(const NormArgs& a, hipStream_t s) {
-    const int T = team(a.o.K);
+    const int T = team(a.o.M, a.o.K);
     const dim3 grid((unsigned)row_grid(a.o.M, T));
     if (T == kWave) hipLaunchKernelGGL((norm_kernel<XT, RT, kWave, OUT>), grid, dim3(256), 0, s, a);
     else if (T == 256) hipLaunchKernelGGL((norm_kernel<XT, RT, 256, OUT>), grid, dim3(256), 0, s, a);
@@ -676,7 +680,7 @@ int gate_check(const cham_gate* g, int64_t most) {
 template <int XT>
 void launch_gate_t(const GateArgs& a, int out, hipStream_t s) {
     if (out == kOutRow) {
-        const int T = team(a.o.K);
+        const int T = team(a.o.M, a.o.K);
         const dim3 grid((unsigned)row_grid(a.o.M, T));
         if (T == kWave) hipLaunchKernelGGL((gate_row_kernel<XT, kWave>), grid, dim3(256), 0, s, a);
         else if (T == 256) hipLaunchKernelGGL((gate_row_kernel<XT, 256>), grid, dim3(256), 0, s, a);

@@ -204,7 +204,7 @@ def _norm_ref(x, r, g, eps):
 
 
 @pytest.mark.parametrize("M,K", [(1, 32), (1, 1280), (5, 160), (30, 640), (66, 1152), (3, 2048), (5, 2080), (3, 8192), (2, 8224),
-                                 (2, 32768)])
+                                 (2, 32768), (530, 640), (701, 1152), (600, 2048)])  # many rows: 64 lanes each
 @pytest.mark.parametrize("fmt", ["block", "e4m3", "int8", "mxfp8"])
 def test_norm_lengths(M, K, fmt):
     case(f"norm M={M} K={K} fmt={fmt}")
@@ -323,7 +323,7 @@ def test_gate_functions(act, dt, up, fmt):
 
 @pytest.mark.parametrize("M,K,fmt", [(1, 32, "block"), (1, 4608, "block"), (7, 5120, "e4m3"), (3, 10240, "int8"),
                                      (2, 32768, "e5m2"), (2, 40960, "block"), (2, 40960, "mxint8"), (333, 96, "mxfp8"),
-                                     (257, 160, "block")])
+                                     (257, 160, "block"), (5, 1184, "e4m3"), (601, 1184, "e5m2"), (530, 2048, "int8")])
 def test_gate_lengths(M, K, fmt):
     case(f"gate M={M} K={K} fmt={fmt}")
     x, u = _x(10, M, K, torch.bfloat16), _x(11, M, K, torch.bfloat16)
