@@ -12,6 +12,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "cham_block_load.h"
 #include "cham_device.h"
 
 namespace cham {
@@ -23,9 +24,7 @@ typedef int int4v __attribute__((ext_vector_type(4)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 
-constexpr int BK = 128;                 // one block of the format: bytes of a row per step
 constexpr int kBufferFlags = 0x00020000;  // buffer descriptor word 3: 32-bit data, raw
-constexpr uint32_t kOutside = 0x80000000u;  // an offset past every buffer: such loads give zeros
 
 struct BlockArgs {
     const uint8_t* xc;
@@ -333,15 +332,16 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
     const int r0 = wave * 8 + (lane >> 3);
     const int cx0 = (lane & 7) ^ key_x(r0), cw0 = (lane & 7) ^ key_w(r0);
     uint32_t offx = (uint32_t)r0 * K + cx0 * 16, offw = (uint32_t)r0 * K + cw0 * 16;
-    const bool lastx = (nkb - 1) * BK + cx0 * 16 >= K, lastw = (nkb - 1) * BK + cw0 * 16 >= K;
+    const bool lastx = past_row(nkb, cx0, K), lastw = past_row(nkb, cw0, K);
     const uint32_t rstep = (uint32_t)T::kWaves * 8 * K;
     // load i of a step: its weights first, then its activations
     auto issue = [&](Lds* x, Lds* w, int i, int kb) {
-        const bool isx = i >= T::kLoadsW, past = kb >= nkb || (kb == nkb - 1 && (isx ? lastx : lastw));
+        const bool isx = i >= T::kLoadsW;
         const int j = isx ? i - T::kLoadsW : i;
+        const LoadAt at = load_at(isx ? offx : offw, isx ? lastx : lastw, kb, nkb);
         Lds* const to = (isx ? x + group * kX : w + group * kW) + (j * T::kWaves + wave) * 1024;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(isx ? rx : rw, (__attribute__((address_space(3))) void*)to, 16,
-                                                 (past ? kOutside : isx ? offx : offw) + j * rstep, kb * BK, 0, 0);
+                                                 at.lane + j * rstep, at.wave, 0, 0);
     };
     auto issue_all = [&](Lds* x, Lds* w, int kb) {
 #pragma unroll
