@@ -474,8 +474,10 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
                 spread(i);
             }
         } else {
-            constexpr int kLag = 3;  // products between one and its addition
-            float4v d[kLag + 1];
+            // products between one and its addition: the ring d holds them and the one being formed
+            constexpr int kRing = 4, kLag = TN * TM < kRing ? TN * TM : kRing - 1;
+            static_assert(kLag < kRing && TN * TM >= kLag, "every product is added once, from the first on");
+            float4v d[kRing];
 #pragma unroll
             for (int i = 0; i < TN; ++i) {
                 if (i + 1 < TN) w[(i + 1) & 1] = operand(W, wlo, whi, T::chan(i + 1) * BK);
@@ -485,8 +487,8 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
                     if constexpr (MODE == kCodesPow2) {
                         acc[i][t] = mfma_pow2(w[i & 1], b[t], acc[i][t], cw[i * kSlots / TN], cx[t]);
                     } else {
-                        d[j & kLag] = mfma(w[i & 1], b[t], zero);
-                        if (k >= 0) add(k / TM, k % TM, d[k & kLag]);
+                        d[j % kRing] = mfma(w[i & 1], b[t], zero);
+                        if (k >= 0) add(k / TM, k % TM, d[k % kRing]);
                     }
                 }
                 if constexpr (MODE == kCodes && T::kFence) {
@@ -501,7 +503,7 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
             }
             if constexpr (MODE == kCodes) {
 #pragma unroll
-                for (int k = TN * TM - kLag; k < TN * TM; ++k) add(k / TM, k % TM, d[k & kLag]);
+                for (int k = TN * TM - kLag; k < TN * TM; ++k) add(k / TM, k % TM, d[k % kRing]);
             }
         }
     };
