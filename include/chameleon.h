@@ -294,7 +294,8 @@ typedef struct cham_aq {
     int32_t nsamples;  /* S >= 1 samples of M/S consecutive rows each (M % S == 0), e.g. the
                           two halves of a CFG-doubled batch; each has its own (s, z)          */
     uint8_t* codes;    /* [M][K] INT8-asym unsigned q, FP8 / MXFP8 codes, MXINT8 two's compl. */
-    uint8_t* e8m0;     /* [M][K/32] biased block exponents (MX formats; may be NULL otherwise)*/
+    uint8_t* e8m0;     /* [M][K/32] biased block exponents, 255 = NaN (MX formats; may be NULL
+                          otherwise)                                                          */
     float* scale;      /* [S] the scale s of each sample (1 for MX formats)                   */
     float* zero;       /* [S] the zero point z of each sample (0 unless INT8-asym)            */
 } cham_aq;
@@ -368,7 +369,8 @@ int cham_quantize_act_lut_accumulate_batch(const float* const* X, const int32_t*
  * dequantized weights, binary64, times (z - z') s in the epilogue).  Block-scaled operands
  * (NF4 and MX weights, MX activations) are held relative to the largest block of their
  * channel or row: blocks within 2^28 of it are exact (NF4: one rounding), blocks further
- * below fall into half precision's subnormal range and lose bits.  xq->K must equal wq->K and be a multiple of
+ * below fall into half precision's subnormal range and lose bits.  An activation block whose
+ * exponent byte is 255 (NaN) makes its rows of Y NaN.  xq->K must equal wq->K and be a multiple of
  * 64; the kernels address operands with 32-bit offsets, so K <= 2^20, N < 2^21 and the
  * weights' decode layout (cham_packed_bytes) stays below 2^31 bytes (CHAM_ESHAPE otherwise);
  * xq->codes, wq->codes and Y must be 16-byte aligned.  Y [M][N] is written in the
@@ -499,8 +501,9 @@ int cham_rms_norm_quantize_block(const cham_norm* n, cham_bq* out, void* stream)
 
 /* The norm of n, written in activation format fmt of section 3 with dynamic scales of each
  * token: out->nsamples must be M (scale [M], zero [M]; e8m0 [M][K/32] for MX formats), codes
- * 8-byte aligned.  A row that holds a NaN or an infinity takes the scale NaN (MX formats take
- * finite rows only).  Errors: as above, CHAM_EFORMAT also for fmt. */
+ * 8-byte aligned.  A row that holds a NaN or an infinity takes the scale NaN; in MX formats its
+ * block of 32 takes the exponent byte 255, which is NaN, and MXFP8 codes that are NaN.  Errors: as
+ * above, CHAM_EFORMAT also for fmt. */
 int cham_rms_norm_quantize(const cham_norm* n, int32_t fmt, cham_aq* out, void* stream);
 
 /* Activation functions */

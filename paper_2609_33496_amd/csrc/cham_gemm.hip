@@ -410,17 +410,23 @@ CHAM_DEV int far_eref(float z) {
     return zm >= 32768.0f ? floor_log2(zm) - 14 : 0;
 }
 
-// largest of the bytes p[o0 .. o1), at most 16 (any alignment)
-CHAM_DEV int max_bytes(const uint8_t* p, int o0, int o1) {
+// largest of the exponent bytes p[o0 .. o1), at most 16 (any alignment); 255, the scale NaN, does
+// not count: it has no size
+CHAM_DEV int max_exponent(const uint8_t* p, int o0, int o1) {
     int m = 0;
+    auto take = [&](uint32_t b) { m = max(m, b == 255u ? 0 : (int)b); };
     if (o1 - o0 == 16) {
         uint32_t w[4];
         __builtin_memcpy(w, p + o0, 16);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            m = max(m, max(max((int)(w[i] & 0xFFu), (int)((w[i] >> 8) & 0xFFu)), max((int)((w[i] >> 16) & 0xFFu), (int)(w[i] >> 24))));
+        for (int i = 0; i < 4; ++i) {
+            take(w[i] & 0xFFu);
+            take((w[i] >> 8) & 0xFFu);
+            take((w[i] >> 16) & 0xFFu);
+            take(w[i] >> 24);
+        }
     } else {
-        for (int o = o0; o < o1; ++o) m = max(m, (int)p[o]);
+        for (int o = o0; o < o1; ++o) take(p[o]);
     }
     return m;
 }
@@ -435,11 +441,12 @@ struct ActDecode {
 
 // E8M0 byte e8 relative to a row whose largest is emax, ebias = 141 - emax: the block scale
 // 2^(e8 - emax + 14) puts the largest block in [2^14, 2^15), so blocks down to 2^-28 of it stay
-// normal in half precision.  Scales below 2^-126 only decode to zeros and are clamped there.
+// normal in half precision.  Scales below 2^-126 only decode to zeros and are clamped there.  The
+// byte 255 is the scale NaN: its MXFP8 codes are NaN themselves, MXINT8 codes become NaN here.
 template <int AF>
 CHAM_DEV ActDecode mx_decode(int e8, int ebias) {
     ActDecode d;
-    const int b = max(e8 + ebias, 1);  // binary32 exponent field of the scale
+    const int b = min(max(e8 + ebias, 1), 141);  // binary32 exponent field of the scale (more than 141 only for 255)
     d.scale = __uint_as_float((uint32_t)b << 23);
     if (AF == CHAM_A_MXINT8) {  // 6 fraction bits; q 2^e1 is a normal half, times 2^e2 rounds once
         const int e = b - 127 - 6, e1 = max(e, -14), e2 = max(e - e1, -24);
@@ -447,6 +454,7 @@ CHAM_DEV ActDecode mx_decode(int e8, int ebias) {
         const _Float16 c = (_Float16)__uint_as_float((uint32_t)(e2 + 127) << 23);
         d.f1 = half2v{a, a};
         d.f2 = half2v{c, c};
+        if (e8 == 255) d.f2 = __builtin_bit_cast(half2v, 0x7E007E00u);
     }
     return d;
 }
@@ -754,7 +762,7 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
                 const int c0 = m0 + d * a.W, ext = lines ? 1 : a.W + 1;
                 const int p0 = max(c0 - ext, 0), p1 = min(c0 + rows + ext, a.M);
                 const int e0 = p0 * (CK / 32), e1 = p1 * (CK / 32);
-                for (int o = e0 + 16 * t; o < e1; o += 16 * NT) mx = max(mx, max_bytes(a.xe8, o, min(o + 16, e1)));
+                for (int o = e0 + 16 * t; o < e1; o += 16 * NT) mx = max(mx, max_exponent(a.xe8, o, min(o + 16, e1)));
             }
             for (int o = 32; o > 0; o >>= 1) mx = max(mx, __shfl_xor(mx, o, kWave));
             if (lane == 0) Re[wave] = mx;
@@ -763,7 +771,7 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
             const int r = t / TPR;
             const uint8_t* row = a.xe8 + (int64_t)(m0 + (r < rows ? r : 0)) * (K / 32) + kb * 2;
             int mx = 0;
-            for (int o = 16 * (t % TPR); o < 2 * nsteps; o += 16 * TPR) mx = max(mx, max_bytes(row, o, min(o + 16, 2 * nsteps)));
+            for (int o = 16 * (t % TPR); o < 2 * nsteps; o += 16 * TPR) mx = max(mx, max_exponent(row, o, min(o + 16, 2 * nsteps)));
 #pragma unroll
             for (int o = 1; o < TPR; o <<= 1) mx = max(mx, __shfl_xor(mx, o, kWave));
             if (t % TPR == 0) Re[r] = mx;

@@ -229,9 +229,12 @@ CHAM_DEV void emit_block(const Out& o, int64_t row, int c, bool in, const float 
     }
 }
 
-// A chunk of an MX row: 4 lanes hold a block of 32, which is whole (K % 32 == 0).
+// A chunk of an MX row: 4 lanes hold a block of 32, which is whole (K % 32 == 0).  A block that
+// holds a NaN or an infinity takes the scale NaN, and MXFP8 codes that are NaN themselves.
 CHAM_DEV void emit_mx(const Out& o, int64_t row, int c, bool in, const float (&y)[kChunk]) {
-    const int E = mx_exponent(__uint_as_float(max4(chunk_amax(y))), 0);
+    const uint32_t m = max4(chunk_amax(y));
+    const bool bad = m >= kInfBits;
+    const int E = mx_exponent(__uint_as_float(m), 0);
     uint2 w;
     if (o.fmt == CHAM_A_MXFP8_E4M3) {
         float v[kChunk];
@@ -239,6 +242,7 @@ CHAM_DEV void emit_mx(const Out& o, int64_t row, int c, bool in, const float (&y
         for (int j = 0; j < kChunk; ++j) v[j] = clampf(ldexpf(y[j], -E), -448.0f, 448.0f);
         w.x = pack_codes<CHAM_A_FP8_E4M3>(v[0], v[1], v[2], v[3], 0.0f);
         w.y = pack_codes<CHAM_A_FP8_E4M3>(v[4], v[5], v[6], v[7], 0.0f);
+        if (bad) w = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
     } else {
         uint32_t q[2] = {0, 0};
 #pragma unroll
@@ -248,7 +252,7 @@ CHAM_DEV void emit_mx(const Out& o, int64_t row, int c, bool in, const float (&y
     }
     if (in) {
         put_codes(o, row, c, w);
-        if ((c & 3) == 0) o.e8m0[row * (o.K >> 5) + (c >> 2)] = (uint8_t)(E + 127);
+        if ((c & 3) == 0) o.e8m0[row * (o.K >> 5) + (c >> 2)] = bad ? (uint8_t)255 : (uint8_t)(E + 127);
     }
 }
 
