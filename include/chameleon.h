@@ -474,9 +474,8 @@ typedef struct cham_bw {
 } cham_bw;
 
 /* h = x + r (binary32), y = h / sqrt(mean(h^2) + eps) * g: the norm sees the unrounded sum; h is
- * written rounded to its own type.  Squares of 8 neighbours are added in binary32, those sums and
- * the mean in binary64 (a row in which 8 squares overflow binary32, |h| from 6e18 up, comes out
- * as zeros). */
+ * written rounded to its own type.  The squares, their sum and the root are binary64, so every
+ * finite h has its norm; y carries three roundings to binary32 behind it. */
 typedef struct cham_norm {
     int64_t M, K;      /* K <= 32768                                                         */
     const void* x;     /* [M][K], row stride ldx elements                                    */

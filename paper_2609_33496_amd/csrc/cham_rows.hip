@@ -401,12 +401,18 @@ __global__ __launch_bounds__(wg_threads<T>()) void norm_kernel(NormArgs a) {
                 if (a.h && live) store8<RR>(a.h, row * a.ldh + (int64_t)(v * T + lane) * kChunk, h[v]);
             }
 #pragma unroll
-            for (int j = 0; j < kChunk; j += 4)  // pairs of pairs: a chunk's sum carries three roundings
-                ss += (double)((h[v][j] * h[v][j] + h[v][j + 1] * h[v][j + 1]) + (h[v][j + 2] * h[v][j + 2] + h[v][j + 3] * h[v][j + 3]));
+            for (int j = 0; j < kChunk; ++j) {  // squares of binary32 are exact, and in range, in binary64
+                const double d = (double)h[v][j];
+                ss = __builtin_fma(d, d, ss);
+            }
         }
     }
     ss = team_reduce<T>(ss, sh, [](double p, double q) { return p + q; });
-    const float rstd = (float)(1.0 / sqrt(ss / (double)a.o.K + (double)a.eps));
+    // rows near either end of binary32 have a factor outside its normal numbers: a power of two of
+    // it goes to h first, exactly
+    const double rs = 1.0 / sqrt(ss / (double)a.o.K + (double)a.eps);
+    const float pre = rs < 0x1p-120 ? 0x1p-64f : rs > 0x1p120 ? 0x1p64f : 1.0f;
+    const float rstd = (float)(rs < 0x1p-120 ? rs * 0x1p64 : rs > 0x1p120 ? rs * 0x1p-64 : rs);
 #pragma unroll
     for (int v = 0; v < kV; ++v) {
         const int c = v * T + lane;
@@ -414,7 +420,7 @@ __global__ __launch_bounds__(wg_threads<T>()) void norm_kernel(NormArgs a) {
             float g[kChunk];
             if (a.g) load_g(a.g, a.g_type, (int64_t)c * kChunk, g);
 #pragma unroll
-            for (int j = 0; j < kChunk; ++j) h[v][j] = a.g ? h[v][j] * rstd * g[j] : h[v][j] * rstd;
+            for (int j = 0; j < kChunk; ++j) h[v][j] = a.g ? h[v][j] * pre * rstd * g[j] : h[v][j] * pre * rstd;
         }
     }
     emit<T, OUT>(a.o, row, live, lane, nch, h, sh);
