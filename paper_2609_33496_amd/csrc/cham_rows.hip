@@ -91,12 +91,17 @@ CHAM_DEV void load_g(const void* g, int type, int64_t i, float (&v)[kChunk]) {
 // ------------------------------------------------------------------------------------
 // activation functions
 // ------------------------------------------------------------------------------------
+// Relative error: up to 1e-6 and 4e-7 of the exponent's argument (|x| for SiLU, x^2 for GELU,
+// 1.6 |x + 0.044715 x^3| for its tanh form), which a rounding of the argument moves by as much.
+// Where 1 + 2^v passes 2^126 the reciprocal instruction gives 0 (it has no subnormal results), so
+// values below 2^-119 may come out as 0: SiLU below x = -87.3, the tanh form below -9.99.  The root of
+// the exponential and a scaled denominator would keep them (8192 x 4608, tanh form, 28.1 us -> 29.8).
 constexpr float kLog2e = 1.44269504f;
 
 // x Phi(x).  With z = |x| and q = Phi(-z), it is -z q for x < 0 and x - z q otherwise, so that
 // neither tail cancels.  q = exp(-z^2/2) t P(t), t = 1/(1 + 0.36 z), P a polynomial of degree 6
 // fitted to the scaled complementary error function by reweighted least squares over
-// 0 <= z <= 15 (largest relative error 1.1e-6: an eighth bit of an 8-bit code is 6e-2).
+// 0 <= z <= 15 (the polynomial's largest relative error 1.1e-6; half a step of E4M3 is 6e-2).
 CHAM_DEV float gelu(float x) {
     const float z = fabsf(x);
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(z, 0.36f, 1.0f));
