@@ -450,6 +450,7 @@ int cham_linear_plan(int64_t M, int64_t N, int64_t K, int32_t code_bits, int32_t
 #define CHAM_T_F16 1
 #define CHAM_T_BF16 2
 #define CHAM_T_N 3
+#define CHAM_T_EXACT 256  /* or-ed into y_type: a 16-bit Y of cham_block_linear from exact products */
 
 /* The block format: E4M3 codes with one scale per row and 128 consecutive elements (the last
  * block of a row holds K mod 128 if 128 does not divide K):
@@ -540,10 +541,13 @@ int cham_gated_quantize(const cham_gate* a, int32_t fmt, cham_aq* out, void* str
 int cham_block_quantize_weights(const void* W, int32_t type, int64_t ldw, cham_bw* out, void* stream);
 
 /* Y[m][n] = sum over blocks b of xs[b][m] ws[n / 128][b] sum_{k in b} xc[m][k] wc[n][k],
- * accumulated in binary32 and rounded once to y_type.  Binary32 outputs form every product
- * exactly; 16-bit outputs use the 8-bit matrix instructions, which drop what lies more than 13
- * bits below the largest product of a group of neighbouring k (3e-5 of the result, a sixteenth of
- * a binary16 rounding at most).  Y [M][N], row stride ldy elements (any; any N).  x->pow2 must
+ * accumulated in binary32 and rounded once to y_type.  Binary32 outputs, and 16-bit ones with
+ * CHAM_T_EXACT or-ed into y_type, form every product exactly: the error before the rounding is at
+ * most (128 + blocks) 2^-23 S, S = sum over b of xs ws sum |xc wc|.  Other 16-bit outputs use the
+ * 8-bit matrix instructions at twice the rate: of 8 neighbouring k they drop what lies more than 13
+ * bits below the largest product, at most 7 2^-13 S in all.  On heavy-tailed data that is 3e-5 to 4e-5
+ * of the result (root mean square, measured; a binary16 rounding is 2e-4), but where large products
+ * cancel, what is left of the sum may be lost.  Y [M][N], row stride ldy elements (any; any N).  x->pow2 must
  * equal w->pow2.  The order of the additions is fixed by the sizes (no atomics): Y is bitwise
  * reproducible run to run.  The product of an activation's and a weight's scale must not
  * overflow binary32.  No workspace.  Errors: CHAM_EINVAL, CHAM_EFORMAT (y_type), CHAM_ESHAPE
@@ -551,7 +555,7 @@ int cham_block_quantize_weights(const void* W, int32_t type, int64_t ldw, cham_b
 int cham_block_linear(const cham_bq* x, const cham_bw* w, void* Y, int32_t y_type, int64_t ldy,
                       void* stream);
 
-/* The launch plan cham_block_linear takes for M x N x K (diagnostics; host only): out (host,
+/* The launch plan cham_block_linear takes for M x N x K and y_type (diagnostics; host only): out (host,
  * out_len >= 3) receives {tile rows, tile channels, wavefront groups that split k inside a
  * workgroup}; tiles of 16 x 16 are the few-row kernel's.  Depends on the current device's CU
  * count (256 when no device is visible).  Errors: CHAM_EINVAL, CHAM_EFORMAT, CHAM_ESHAPE. */

@@ -707,6 +707,7 @@ BLOCK = 128
 A_BLOCK128 = 16
 ACT_NONE, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(4)
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_EXACT = 256  # CHAM_T_EXACT
 
 
 @dataclass
@@ -923,9 +924,10 @@ def block_quantize_weights(W: torch.Tensor, pow2: bool = False, out: Optional[BW
 
 
 def block_linear(xb: BQ, wb: BW, Y: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
-                 stream=None) -> torch.Tensor:
+                 stream=None, exact: bool = False) -> torch.Tensor:
     """Y [M, N] = activations times weights^T, both in the block format; Y (rows may be strided)
-    decides the type where it is given, else dtype."""
+    decides the type where it is given, else dtype.  exact: a 16-bit Y from exact products too, as
+    a float32 one always is, instead of the 8-bit matrix instructions' (see cham_block_linear)."""
     dev = xb.codes.device
     a, w = xb.struct(), wb.struct()
     if wb.codes.get_device() != dev.index:
@@ -937,13 +939,15 @@ def block_linear(xb: BQ, wb: BW, Y: Optional[torch.Tensor] = None, dtype: torch.
         Y = _empty(xb.M, ld, dtype, dev, stream)
     else:
         ty, ld = _matrix(Y, "Y", (xb.M, wb.N), dev), _ld(Y, xb.M, wb.N)
+    if exact:
+        ty |= _EXACT
     rc = _on_device(dev, stream, lib().cham_block_linear, ctypes.byref(a), ctypes.byref(w), Y.data_ptr(), ty, ld)
     _check(rc, "block_linear")
     return Y
 
 
-def block_linear_plan(M: int, N: int, K: int, dtype: torch.dtype = torch.bfloat16) -> tuple:
+def block_linear_plan(M: int, N: int, K: int, dtype: torch.dtype = torch.bfloat16, exact: bool = False) -> tuple:
     """(tile rows, tile channels, k groups) block_linear takes for these sizes (host only)."""
     out = (ctypes.c_int32 * 3)()
-    _check(lib().cham_block_linear_plan(M, N, K, _TYPES[dtype], out, 3), "block_linear_plan")
+    _check(lib().cham_block_linear_plan(M, N, K, _TYPES[dtype] | (_EXACT if exact else 0), out, 3), "block_linear_plan")
     return tuple(out)

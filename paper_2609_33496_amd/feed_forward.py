@@ -16,14 +16,16 @@ class FeedForward:
 
     The weights ([H or 2 H, K] and [K, H], any float type, on the device) are brought to the block
     format once; pow2 takes scales that are powers of two, which the matrix instructions apply
-    themselves."""
+    themselves; exact forms the products as block_linear's exact does."""
 
     def __init__(self, w_in: torch.Tensor, w_out: torch.Tensor, norm_weight: Optional[torch.Tensor] = None,
-                 eps: float = 1e-6, act: int = cham.ACT_GELU, gated: bool = False, pow2: bool = False):
+                 eps: float = 1e-6, act: int = cham.ACT_GELU, gated: bool = False, pow2: bool = False,
+                 exact: bool = False):
         K, H = w_out.shape
         if w_in.shape != (2 * H if gated else H, K):
             raise ValueError(f"w_in must be [{2 * H if gated else H}, {K}], got {tuple(w_in.shape)}")
         self.K, self.H, self.gated, self.act, self.eps, self.pow2 = K, H, gated, act, eps, pow2
+        self.exact = exact
         self.norm_weight = norm_weight
         self.w_in = cham.block_quantize_weights(w_in, pow2=pow2)
         self.w_out = cham.block_quantize_weights(w_out, pow2=pow2)
@@ -33,7 +35,7 @@ class FeedForward:
         """(y, h): the block's output in x's type, and h = x + residual (None without one)."""
         q, h = cham.rms_norm_quantize(x, self.norm_weight, self.eps, residual=residual, residual_out=residual_out,
                                       pow2=self.pow2, stream=stream)
-        t = cham.block_linear(q, self.w_in, dtype=x.dtype, stream=stream)
+        t = cham.block_linear(q, self.w_in, dtype=x.dtype, stream=stream, exact=self.exact)
         q = cham.gated_quantize(t[:, :self.H], t[:, self.H:] if self.gated else None, self.act, pow2=self.pow2,
                                 stream=stream)
-        return cham.block_linear(q, self.w_out, dtype=x.dtype, stream=stream), h
+        return cham.block_linear(q, self.w_out, dtype=x.dtype, stream=stream, exact=self.exact), h

@@ -1,0 +1,123 @@
+"""What the block product's two routes lose on the GPU: groups of k whose large products cancel, and the
+exact route into 16-bit outputs."""
+import pytest
+import torch
+
+from paper_2609_33496_amd import cham
+from paper_2609_33496_amd.feed_forward import FeedForward
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+# shapes of every plan of each route
+CODES = [(1, 40, 288, (16, 16, 8)), (100, 1030, 96, (32, 64, 1)), (70, 4100, 2080, (32, 64, 2)), (1000, 2600, 96, (64, 64, 1)),
+         (500, 1250, 3232, (64, 64, 2)), (3273, 911, 320, (128, 128, 1)), (4090, 2300, 800, (256, 192, 1)),
+         (4090, 4090, 1568, (256, 256, 1))]
+HALF = [(1, 40, 288, (16, 16, 8)), (17, 2081, 32, (32, 64, 1)), (70, 4100, 2080, (32, 64, 2)), (1000, 2600, 96, (64, 64, 1)),
+        (500, 1250, 3232, (64, 64, 2)), (1030, 5000, 672, (64, 128, 1))]
+
+
+def case(msg):
+    print(f"[case] {msg}", flush=True)
+
+
+def _cancelling(M, N, K, pow2):
+    """Of every 8 neighbouring k the first two products are +-448 * 448 and cancel, the other six are
+    -4 .. 4.  Scales 1/2 .. 2, with powers of two or without; (operands, x, w) in float64."""
+    g = torch.Generator(device=DEV).manual_seed(M + N + K)
+
+    def ints(lo, hi, *shape):
+        return torch.randint(lo, hi + 1, shape, generator=g, device=DEV)
+    x, w = ints(-2, 2, M, K).float(), ints(-2, 2, N, K).float()
+    x[:, 0::8], x[:, 1::8] = 448.0, -448.0
+    w[:, 0::8], w[:, 1::8] = 448.0, 448.0
+    nb = -(-K // 128)
+    ex, ew = ints(-1, 1, nb, M), ints(-1, 1, -(-N // 128), nb)
+    if pow2:
+        xs, ws = (ex + 127).to(torch.uint8), (ew + 127).to(torch.uint8)
+        hx, hw = torch.exp2(ex.double()), torch.exp2(ew.double())
+    else:
+        xs, ws = (torch.rand(s.shape, generator=g, device=DEV) + 0.5 for s in (ex, ew))
+        hx, hw = xs.double(), ws.double()
+
+    def codes(v):
+        return v.to(torch.float8_e4m3fn).view(torch.uint8)
+    xd = x.double() * hx.t().repeat_interleave(128, 1)[:, :K]
+    wd = w.double() * hw.repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K]
+    return cham.BQ(M, K, codes(x), xs), cham.BW(N, K, codes(w), ws), xd, wd
+
+
+def _last(dt):
+    return {F32: 2.0 ** -24, F16: 2.0 ** -11, BF16: 2.0 ** -8}[dt]
+
+
+@pytest.mark.parametrize("pow2", [False, True])
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("M,N,K,plan", CODES)
+def test_cancelling_products_stay_within_the_stated_bound(M, N, K, plan, dt, pow2):
+    """8-bit instructions: 7 2^-13 of the sum of magnitudes, whatever is left of the sum."""
+    assert cham.block_linear_plan(M, N, K, dt) == plan
+    case(f"cancelling M={M} N={N} K={K} {dt} pow2={pow2}")
+    xb, wb, x, w = _cancelling(M, N, K, pow2)
+    y, S = x @ w.t().contiguous(), x.abs() @ w.abs().t().contiguous()
+    err = (cham.block_linear(xb, wb, dtype=dt).double() - y).abs()
+    n = -(-K // 128)
+    assert bool((err <= (7 * 2.0 ** -13 + (n + 2) * 2.0 ** -23) * S + _last(dt) * (y.abs() + 7 * 2.0 ** -13 * S)).all())
+
+
+@pytest.mark.parametrize("pow2", [False, True])
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("M,N,K,plan", HALF)
+def test_cancelling_products_leave_the_exact_sum(M, N, K, plan, dt, pow2):
+    """Exact route: integers below 2^24, so the sums of a block are exact; with scales that are
+    powers of two Y is the rounded result itself."""
+    assert cham.block_linear_plan(M, N, K, dt, exact=True) == plan
+    case(f"cancelling, exact M={M} N={N} K={K} {dt} pow2={pow2}")
+    xb, wb, x, w = _cancelling(M, N, K, pow2)
+    y = x @ w.t().contiguous()
+    Y = cham.block_linear(xb, wb, dtype=dt, exact=True)
+    assert Y.dtype == dt
+    if pow2:
+        assert torch.equal(Y, y.to(dt))
+    else:  # per block a rounded factor and a rounded addition, each relative to sums of blocks
+        n = -(-K // 128)
+        x[:, 0::8], x[:, 1::8] = 0.0, 0.0
+        S = x.abs() @ w.abs().t().contiguous()
+        assert bool(((Y.double() - y).abs() <= (n + 2) * 2.0 ** -23 * S + _last(dt) * y.abs() * 1.001).all())
+
+
+def _operands(M, N, K, pow2):
+    g = torch.Generator(device=DEV).manual_seed(K)
+    x, w = torch.randn(M, K, generator=g, device=DEV), torch.randn(N, K, generator=g, device=DEV) * 0.02
+    return cham.gated_quantize(x, None, cham.ACT_NONE, pow2=pow2), cham.block_quantize_weights(w, pow2=pow2)
+
+
+@pytest.mark.parametrize("pow2", [False, True])
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("M,N,K,plan", HALF)
+def test_exact_16_bit_outputs_are_the_binary32_ones_rounded(M, N, K, plan, dt, pow2):
+    """Into aligned rows, and into rows of other alignments with nothing written beside them."""
+    assert cham.block_linear_plan(M, N, K, F32) == plan
+    case(f"exact M={M} N={N} K={K} {dt} pow2={pow2}")
+    xb, wb = _operands(M, N, K, pow2)
+    want = cham.block_linear(xb, wb, dtype=F32).to(dt)
+    assert torch.equal(cham.block_linear(xb, wb, dtype=dt, exact=True), want)
+    for off, width in ((0, N + 1), (1, N + 2), (4, N + 8)):
+        buf = torch.full((M + 1, width), 7.0, dtype=dt, device=DEV)
+        cham.block_linear(xb, wb, buf[:M, off:off + N], exact=True)
+        assert torch.equal(buf[:M, off:off + N], want), (off, width)
+        assert bool((buf[:, :off] == 7.0).all()) and bool((buf[:, off + N:] == 7.0).all()) and bool((buf[M] == 7.0).all())
+
+
+def test_exact_feed_forward_block():
+    case("exact feed-forward")
+    M, d, hid = 33, 320, 640
+    g = torch.Generator().manual_seed(1)
+    w_in, w_out = (torch.randn(s, generator=g).to(DEV) * 0.03 for s in ((hid, d), (d, hid)))
+    x = torch.randn(M, d, generator=g).to(DEV, BF16)
+    y, _ = FeedForward(w_in, w_out, act=cham.ACT_SILU, exact=True)(x)
+    q, _ = cham.rms_norm_quantize(x)
+    t = cham.block_linear(q, cham.block_quantize_weights(w_in), dtype=BF16, exact=True)
+    q = cham.gated_quantize(t, None, cham.ACT_SILU)
+    assert torch.equal(y, cham.block_linear(q, cham.block_quantize_weights(w_out), dtype=BF16, exact=True))
