@@ -483,8 +483,8 @@ typedef struct cham_norm {
     int64_t ldx;
     const void* r;     /* the residual [M][K], row stride ldr; NULL = none                   */
     int64_t ldr;
-    void* h;           /* [M][K], row stride ldh, of r's type; may be r itself (same stride);
-                          NULL = not written                                                  */
+    void* h;           /* [M][K], row stride ldh, of r's type; may be r itself (same stride), no
+                          other overlap with the inputs; NULL = not written                   */
     int64_t ldh;
     const void* g;     /* [K] weights, 16-byte aligned; NULL = ones                          */
     int32_t x_type;
@@ -545,18 +545,19 @@ int cham_block_quantize_weights(const void* W, int32_t type, int64_t ldw, cham_b
  * CHAM_T_EXACT or-ed into y_type, form every product exactly: the error before the rounding is at
  * most (128 + blocks) 2^-23 S, S = sum over b of xs ws sum |xc wc|.  Other 16-bit outputs use the
  * 8-bit matrix instructions at twice the rate: of 8 neighbouring k they drop what lies more than 13
- * bits below the largest product, at most 7 2^-13 S in all.  On heavy-tailed data that is 3e-5 to 4e-5
- * of the result (root mean square, measured; a binary16 rounding is 2e-4), but where large products
- * cancel, what is left of the sum may be lost.  Y [M][N], row stride ldy elements (any; any N).  x->pow2 must
- * equal w->pow2.  The order of the additions is fixed by the sizes (no atomics): Y is bitwise
- * reproducible run to run.  The product of an activation's and a weight's scale must not
- * overflow binary32.  No workspace.  Errors: CHAM_EINVAL, CHAM_EFORMAT (y_type), CHAM_ESHAPE
- * (K % 32, K > 2^20, M or N > 2^31 - 257, or a launch of 2^32 lanes), CHAM_EHIP. */
+ * bits below the largest product, at most 7 2^-13 S in all.  On heavy-tailed data that is 3e-5 to
+ * 4e-5 of the result (root mean square, measured; a binary16 rounding is 2e-4), but where large
+ * products cancel, what is left of the sum may be lost.  The product of an activation's and a
+ * weight's scale is formed in binary32: where it overflows, Y is infinite or NaN, and below 2^-126 it
+ * loses bits of Y.  x->pow2 must equal w->pow2.  Y [M][N], row stride ldy elements (any; any N).  The
+ * order of the additions is fixed by the sizes and y_type (no atomics): Y is bitwise reproducible.
+ * No workspace.  Errors: CHAM_EINVAL, CHAM_EFORMAT (y_type), CHAM_ESHAPE (K % 32, K > 2^20, M or N >
+ * 2^31 - 257, or a launch of 2^32 lanes), CHAM_EHIP. */
 int cham_block_linear(const cham_bq* x, const cham_bw* w, void* Y, int32_t y_type, int64_t ldy,
                       void* stream);
 
-/* The launch plan cham_block_linear takes for M x N x K and y_type (diagnostics; host only): out (host,
- * out_len >= 3) receives {tile rows, tile channels, wavefront groups that split k inside a
+/* The launch plan cham_block_linear takes for M x N x K and y_type (diagnostics; host only): out
+ * (host, out_len >= 3) receives {tile rows, tile channels, wavefront groups that split k inside a
  * workgroup}; tiles of 16 x 16 are the few-row kernel's.  Depends on the current device's CU
  * count (256 when no device is visible).  Errors: CHAM_EINVAL, CHAM_EFORMAT, CHAM_ESHAPE. */
 int cham_block_linear_plan(int64_t M, int64_t N, int64_t K, int32_t y_type, int32_t* out, int32_t out_len);

@@ -16,7 +16,8 @@ class FeedForward:
 
     The weights ([H or 2 H, K] and [K, H], any float type, on the device) are brought to the block
     format once; pow2 takes scales that are powers of two, which the matrix instructions apply
-    themselves; exact forms the products as block_linear's exact does."""
+    themselves; exact forms the products as block_linear's exact does.  The weights are quantized on the
+    current stream: a call on another one has to wait for it."""
 
     def __init__(self, w_in: torch.Tensor, w_out: torch.Tensor, norm_weight: Optional[torch.Tensor] = None,
                  eps: float = 1e-6, act: int = cham.ACT_GELU, gated: bool = False, pow2: bool = False,

@@ -110,6 +110,25 @@ def test_exact_16_bit_outputs_are_the_binary32_ones_rounded(M, N, K, plan, dt, p
         assert bool((buf[:, :off] == 7.0).all()) and bool((buf[:, off + N:] == 7.0).all()) and bool((buf[M] == 7.0).all())
 
 
+@pytest.mark.parametrize("pow2", [False, True])
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("M,N", [(1, 1), (600, 2000)])
+def test_scales_whose_product_nears_either_end(M, N, dt, pow2):
+    """Powers of two whose product lies between 2^-148 and 2^127: Y is the exact power of two."""
+    for code, ex, ew in ((256.0, -80, -40), (256.0, -80, -68), (256.0, -126, -20), (1.0, -60, -66), (1.0, -70, -70),
+                         (2.0 ** -9, 70, 50), (2.0 ** -9, 119, 8)):
+        case(f"scales 2^{ex} 2^{ew} M={M} {dt} pow2={pow2}")
+        K = 128
+
+        def held(e, *shape):
+            return torch.full(shape, e + 127, dtype=torch.uint8, device=DEV) if pow2 else torch.full(shape, 2.0 ** e, device=DEV)
+        c = torch.tensor(code).to(torch.float8_e4m3fn).view(torch.uint8).to(DEV)
+        xb = cham.BQ(M, K, c.expand(M, K).contiguous(), held(ex, 1, M))
+        wb = cham.BW(N, K, c.expand(N, K).contiguous(), held(ew, -(-N // 128), 1))
+        Y = cham.block_linear(xb, wb, dtype=dt)
+        assert bool((Y.double() == code * code * K * 2.0 ** (ex + ew)).all())
+
+
 def test_exact_feed_forward_block():
     case("exact feed-forward")
     M, d, hid = 33, 320, 640
