@@ -154,13 +154,16 @@ CHAM_DEV void store8(const BlockArgs& a, int64_t m, int64_t n, float4v p, float4
 //
 // What bounds it, in tiles of 256 x 256: a step's products hold the matrix cores for 2048 cycles,
 // and its LDS traffic (192 KB read, 64 KB written, 128 bytes a cycle) takes as many; the reads of
-// the activations at a step's start overlap with no product.  8192 x 8192 x 8192: 445 us with
-// binary32 scales (2.47 PFLOP/s, matrix cores busy 64 %), 402 with powers of two (2.73); the
-// library's 8-bit product with one scale per tensor 337 (3.27).  Smaller tiles read more LDS per
-// product (128 x 128: 64 KB for 512 cycles; 2048 x 10240 x 1280 35.4 us, 1.52 PFLOP/s); the
-// smallest are bound by the loads into one CU's LDS (about 85 bytes a ns).  f16 route: 8192 x 8192
-// x 8192 1220 us (0.90 PFLOP/s), 240 x 1152 x 4096 11.3 us (144 workgroups, conversions and LDS
-// latency in turn at 0.5 us a step).
+// the activations at a step's start overlap with no product.  8192 x 8192 x 8192: 437 us with
+// binary32 scales (2.51 PFLOP/s, matrix cores busy 64 %), 394 with powers of two (2.79); the
+// library's 8-bit product with one scale per tensor 333 (3.30).  Smaller tiles read more LDS per
+// product (128 x 128: 64 KB for 512 cycles, 0.49 us a step beside others, 2.3 times its products; 2048
+// x 10240 x 1280 33.4 us, 1.61 PFLOP/s); the smallest are bound by the loads into one CU's LDS (about
+// 85 bytes a ns).  f16 route, tiles of 64 x 128: a wavefront's step is 32 products, 96 conversions (each
+// code is converted in two wavefronts) and 32 scaled additions, so vector work takes as long as the
+// products: 8192 x 8192 x 8192 1129 us (0.97 PFLOP/s; the library's bfloat16 product 664), 2048 x 10240 x
+// 1280 67.3.  240 x 1152 x 4096 there 11.3 us (144 workgroups on 256 CUs, conversions and LDS latency in
+// turn at 0.5 us a step).
 //
 // bytes of LDS; the address space is part of the type, so that reads of it cannot become others
 typedef __attribute__((address_space(3))) uint8_t Lds;
@@ -584,7 +587,9 @@ __global__ __launch_bounds__(T::kWaves * T::KS * 64, 2) void tile_kernel(BlockAr
 // ...  With few rows every weight is read by few workgroups, so LDS would only stand in the way:
 // a lane loads its operands of the next step while it multiplies.  The partial sums meet in LDS
 // and are added in the order of the wavefronts (no second launch, no atomics).  Bound by the
-// weights' bytes and the launch: 1 x 10240 x 1280 5.2 us (13 MB, 2.5 TB/s).
+// weights' bytes and the launch: 1 x 10240 x 1280 4.5 us (13 MB, 2.9 TB/s; 5.3 in a kernel trace).  32
+// x 1280 x 5120 6.8 us for 6.7 MB: 160 workgroups, whose eight wavefronts make five steps in turn, each
+// a memory latency with one step in flight ahead.
 template <int TM, int TN, int NW, int MODE, int YT>
 __global__ __launch_bounds__(NW * 64) void few_rows_kernel(BlockArgs a) {
     using Scale = typename ScaleOf<byte_scales(MODE)>::type;
@@ -718,10 +723,11 @@ int launch_few(BlockArgs a, hipStream_t s) {
 
 // Modeled time (us) of one tile shape: the tiles of the busiest CU, each its k-steps and a fixed
 // part (first loads, output).  8-bit instructions: a k-step among others is a little faster where
-// the last round leaves CUs idle.  Fitted to forced launches of every tile over 33 shapes (M 32 -
-// 16384, N 512 - 10240, K 512 - 9216; 3 sets of operands in turn); there the choice takes 0.5 %
-// longer than the best tile on average and 10 % at worst (16384 x 640 x 640: 15.5 us against 14.1).
-// f16 instructions: 33 shapes, 0.4 % and 6 % (120 x 4608 x 1152: 7.2 us against 6.8).
+// the last round leaves CUs idle.  Against forced launches of every tile over 39 shapes (M 32 -
+// 16384, N 512 - 10240, K 512 - 9216; 3 sets of operands in turn) the choice takes 0.8 % longer than
+// the best tile on average and 9 % at worst (16384 x 640 x 640: 14.4 us against 13.2), with scales that
+// are powers of two 0.6 % and 8 %, with f16 instructions 0.4 % and 7 % (120 x 4608 x 1152: 7.2 us against
+// 6.7).
 struct TileCost {
     int bm, bn, ks;
     double lone, step, fixed;  // us: a k-step alone on a CU, among others, and the fixed part
@@ -759,9 +765,11 @@ int plan_tile(const BlockArgs& a, const Costs& costs) {
 }
 
 // Few rows go without LDS where the launch is at most one workgroup per CU, or where the
-// activations' repeated rows cost nothing: 1 x 10240 x 1280 4.5 us against 5.0 in tiles of 32 x 64
-// (f16 route 4.5 against 5.7), 32 x 1280 x 5120 6.9 against 8.8; but 16 x 10240 x 1280 5.7 against
-// 5.1 (f16 route 5.7 against 5.9).
+// activations' repeated rows cost little, against the tiles of 32 x 64 with two k groups that the plan
+// takes else: 1 x 10240 x 1280 4.5 us and 4.7 (f16 route 4.6 and 5.6), 32 x 1280 x 5120 6.8 and 8.4 (6.8
+// and 12.9), 48 x 1152 x 4608 6.3 and 7.8; 8 x 10240 x 1280 5.0 and 4.8 (5.1 and 5.7), 16 x 10240 x 1280
+// 5.6 and 4.9 (5.7 and 5.8), 17 x 10240 x 1280 8.1 and 4.9 (8.3 and 5.8), 16 x 8192 x 8192 16.9 and 13.7
+// (17.1 and 19.1).
 bool few_rows(const BlockArgs& a, bool half) {
     return ceil_div(a.M, 16) * ceil_div(a.N, 16) <= cham_device_cus() || a.M <= (half ? 16 : 8);
 }
@@ -775,7 +783,7 @@ int launch_plan(const BlockArgs& a, hipStream_t s) {
     } else {
         if (tile == kT256) return launch_tile<Tile<4, 2, 4, 8, 1>, MODE, YT>(a, s);
         // three quarters of a 256 x 256 tile: fewer CUs idle in the last round at some widths (8192 x
-        // 1152 x 4608 46.8 us against 51.0, 8192 x 1280 x 1280 19.8 against 21.5)
+        // 1152 x 4608 44.9 us against 50.1, 8192 x 1280 x 1280 18.4 against 20.3 in tiles of 128 x 128)
         if (tile == kT192) return launch_tile<Tile<4, 2, 4, 6, 1>, MODE, YT>(a, s);
         if (tile == kT128) return launch_tile<Tile<2, 2, 4, 4, 1>, MODE, YT>(a, s);
     }

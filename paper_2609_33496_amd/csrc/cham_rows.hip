@@ -2,7 +2,7 @@
 // the (gated) activation function, and the block quantizer of weights.
 //
 // All are bound by memory, or by their launch where they are small: each input is read once and
-// each output written once (a copy of 2 GiB reaches 5.1 TB/s on this card).  A row is
+// each output written once (a copy of 1 GiB reaches 5.1 TB/s on this card).  A row is
 // held in registers between the reduction that its scale needs and its codes, so nothing is
 // read twice; a lane holds chunks of 8 consecutive elements, 16 lanes a block of 128, 4 lanes
 // an MX block of 32, and block maxima are DPP rotations within 16 lanes (no LDS).
@@ -368,11 +368,13 @@ struct NormArgs {
 
 // h = x + r, y = h / sqrt(mean h^2 + eps) g, then the codes of y.  The whole row is loaded before
 // its first use (up to 4 chunks a lane in flight), so one wavefront per row with no barrier holds
-// rows up to 2048, and workgroups the longer ones and those of few rows.  h goes past the caches (nothing here reads it
-// again soon), the codes stay in them for the product that follows.
-// Measured: bfloat16 x, binary32 residual, 8192 x 1152, block output 19.8 us (104 MB, 5.2 TB/s:
-// memory); binary32 x alone, 8100 x 640, E4M3 per token 9.3 us (26 MB, 2.8 TB/s: 64 lanes cover 640
-// in two chunks, the second a quarter full); 1 x 1280 2.8 us in a graph (a launch).
+// rows up to 2048, and workgroups the longer ones and those of few rows.  h goes past the caches
+// (nothing here reads it again soon), the codes stay in them for the product that follows.
+// Measured in a graph: bfloat16 x, binary32 residual, 8192 x 1152, block output 20.0 us (104 MB, 5.2
+// TB/s: memory); bfloat16 x and residual, 4096 x 5120, block output 31.4 us, MXFP8 30.4, MXINT8 31.0,
+// INT8 per token 32.3 (147 MB, 4.6 to 4.8 TB/s); 1 x 1280 2.8 us (a launch).  binary32 x alone, 8100 x
+// 640, E4M3 per token 9.2 us (26 MB, 2.8 TB/s): a launch's 2.7 us beside 5.1 of memory, and the chains
+// of the two reductions, which all rows run at about the same time (block output, one reduction: 8.7).
 // RT: type of the residual, or -1 for none
 template <int XT, int RT, int T, int OUT>
 __global__ __launch_bounds__(wg_threads<T>()) void norm_kernel(NormArgs a) {
@@ -455,7 +457,10 @@ CHAM_DEV void gate_chunk(const Raw<XT>& x, const Raw<XT>& u, bool gated, int act
 }
 
 // One scale per token: the row in registers, as in the norm (a scale needs the whole row's range).
-// Bound as the block form below, and by the range's reduction where rows are short.
+// Bound as the block form below, and by the range's reductions where rows are short.  Measured,
+// bfloat16 gated SiLU, E4M3 and INT8 (two more reductions): 8192 x 4608 38.7 and 44.6 us (189 MB, 4.9
+// TB/s), 8192 x 2560 28.1 and 33.5 (105 MB), 8192 x 1152 13.6 and 15.0 (47 MB), 2048 x 5120 12.7 and
+// 14.3 (52 MB).
 template <int XT, int T>
 __global__ __launch_bounds__(wg_threads<T>()) void gate_row_kernel(GateArgs a) {
     __shared__ float sh[T > kWave ? T / kWave : 1];
@@ -490,9 +495,9 @@ __global__ __launch_bounds__(wg_threads<T>()) void gate_row_kernel(GateArgs a) {
 // Block and MX formats need no more than 16 neighbouring lanes: the tensor is a list of blocks
 // of 128 (those of a row's ragged end are short), 16 lanes a block, any K.  A workgroup takes 32
 // consecutive blocks; where its first one lies is found once, in scalar registers.
-// Measured: bfloat16 gated GELU 2048 x 5120 14.4 us (53 MB, 3.7 TB/s, a launch's 3.6 us
-// among them), plain GELU's tanh form 8192 x 4608 26.1 us (115 MB, 4.4
-// TB/s: memory), 240 x 4608 4.2 us (a launch).
+// Measured: bfloat16 gated GELU 2048 x 5120 14.0 us (53 MB, 3.8 TB/s, a launch's 2.7 us among
+// them), plain GELU's tanh form 8192 x 4608 26 us (115 MB, 4.4 TB/s: memory), gated SiLU 8192 x 4608
+// 37.2 us in block format, 36.5 in MXFP8, 37.3 in MXINT8 (190 MB, 5.1 TB/s), 240 x 4608 3.6 us (a launch).
 constexpr int kGateThreads = 256;
 constexpr int kGateBlocks = 2;  // blocks per 16 lanes, their loads in flight together
 constexpr int kGatePer = kGateThreads / 16 * kGateBlocks;
@@ -612,13 +617,20 @@ int out_token(int32_t fmt, cham_aq* q, int64_t M, int64_t K, Out* o) {
     return CHAM_OK;
 }
 
-// Lanes per row: a wavefront where its registers hold the row (no barrier, four rows per
-// workgroup), else 256 or 1024 lanes.  Rows of more than a chunk per lane take 256 lanes too where
-// there are at most two of them per CU: latency counts there, and a lane's chunks are worked off in
-// turn.  Norm, us: 8100 x 640, E4M3 per token, 64 lanes 9.0 and 256 lanes 15.3; 8192 x 1152, INT8 per
-// token 22.4 and 25.5, block format 21.7 and 20.7; 4096 x 5120, 256 lanes 56.1 and 1024 lanes 65.9;
-// but 1 x 1152, 64 lanes 3.9 and 256 lanes 2.8, 1 x 2048 4.5 and 2.8, 512 x 1152 4.6 and 3.7, 512 x 640,
-// INT8 4.4 and 4.5; 1024 x 640 4.0 and 4.2.
+// Lanes per row: a wavefront where its registers hold the row (no barrier, four rows per workgroup),
+// else 256 lanes, and 1024 for rows that 256 cannot hold.  Rows of more than a chunk per lane take 256
+// lanes too where there are at most two of them per CU: latency counts there, and a lane's chunks are
+// worked off in turn.  Norm of bfloat16 rows and residual, us with 64, 256 and 1024 lanes (block
+// output / INT8 per token):
+//   8100 x 640    10.5 14.7 50.1 / 11.8 19.8 91.9      8192 x 1152   15.6 16.7 50.8 / 16.8 21.5 92.7
+//   1024 x 640     3.9  4.0  8.3 /  4.4  5.1 13.3      512 x 640      3.7  3.4  5.1 /  4.2  4.4  7.6
+//   512 x 1152     4.5  3.5  5.2 /  4.9  4.5  7.8      1 x 1152       3.9  2.8  3.3 /  4.4  3.8  5.0
+//   1 x 2048       4.5  2.8  3.4 /  5.0  3.8  5.0      4096 x 2048   13.0 12.7 27.6 / 13.6 15.3 47.8
+//   1 x 4096          -  3.5  3.5 /    -  4.4  5.1     1 x 8192          -  4.8  4.1 /    -  5.7  5.8
+//   4096 x 5120       - 31.4 37.7 /    - 32.2 59.7     4096 x 8192       - 50.9 50.7 /    - 50.7 71.7
+// Gated SiLU, E4M3 per token: 1 x 2048 4.2 2.7 2.8, 1 x 4096 - 3.2 3.0, 1 x 8192 - 4.3 3.7, 2048 x 5120
+// - 12.8 21.4.  So 1024 lanes would save a few rows of 4097 to 8192 elements up to 0.7 us, below the
+// host's call; the rule has no line for them.
 int team(int64_t M, int64_t K) {
     if (K <= kWave * kChunk || (K <= kWave * kV * kChunk && M > 2 * (int64_t)cham_device_cus())) return kWave;
     return K <= 256 * kV * kChunk ? 256 : 1024;
