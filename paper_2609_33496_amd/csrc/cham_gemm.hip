@@ -410,11 +410,12 @@ CHAM_DEV int far_eref(float z) {
     return zm >= 32768.0f ? floor_log2(zm) - 14 : 0;
 }
 
-// largest of the exponent bytes p[o0 .. o1), at most 16 (any alignment); 255, the scale NaN, does
-// not count: it has no size
+// largest of the exponent bytes p[o0 .. o1), at most 16 (any alignment); SKIP: 255, the scale NaN,
+// does not count
+template <bool SKIP>
 CHAM_DEV int max_exponent(const uint8_t* p, int o0, int o1) {
     int m = 0;
-    auto take = [&](uint32_t b) { m = max(m, b == 255u ? 0 : (int)b); };
+    auto take = [&](uint32_t b) { m = max(m, SKIP && b == 255u ? 0 : (int)b); };
     if (o1 - o0 == 16) {
         uint32_t w[4];
         __builtin_memcpy(w, p + o0, 16);
@@ -431,6 +432,8 @@ CHAM_DEV int max_exponent(const uint8_t* p, int o0, int o1) {
     return m;
 }
 
+constexpr uint32_t kE4m3NaN4 = 0x7F7F7F7Fu;  // four E4M3 codes that are NaN
+
 // What a staging row's codes are decoded with: INT8-asym -(1024 + zero point), MX the block's
 // scale (MXINT8 as two half-precision powers of two).
 struct ActDecode {
@@ -442,11 +445,14 @@ struct ActDecode {
 // E8M0 byte e8 relative to a row whose largest is emax, ebias = 141 - emax: the block scale
 // 2^(e8 - emax + 14) puts the largest block in [2^14, 2^15), so blocks down to 2^-28 of it stay
 // normal in half precision.  Scales below 2^-126 only decode to zeros and are clamped there.  The
-// byte 255 is the scale NaN: its MXFP8 codes are NaN themselves, MXINT8 codes become NaN here.
-template <int AF>
+// byte 255 is the scale NaN.  In the linear layer it is its row's largest and makes the row's factor
+// NaN.  In the convolution a block belongs to the rows of several pixels: its codes become NaN as
+// they are staged, and emax is the largest of the other blocks.
+template <int AF, bool CONV>
 CHAM_DEV ActDecode mx_decode(int e8, int ebias) {
     ActDecode d;
-    const int b = min(max(e8 + ebias, 1), 141);  // binary32 exponent field of the scale (more than 141 only for 255)
+    int b = max(e8 + ebias, 1);  // binary32 exponent field of the scale
+    if (CONV) b = min(b, 141);   // more only for 255
     d.scale = __uint_as_float((uint32_t)b << 23);
     if (AF == CHAM_A_MXINT8) {  // 6 fraction bits; q 2^e1 is a normal half, times 2^e2 rounds once
         const int e = b - 127 - 6, e1 = max(e, -14), e2 = max(e - e1, -24);
@@ -454,7 +460,7 @@ CHAM_DEV ActDecode mx_decode(int e8, int ebias) {
         const _Float16 c = (_Float16)__uint_as_float((uint32_t)(e2 + 127) << 23);
         d.f1 = half2v{a, a};
         d.f2 = half2v{c, c};
-        if (e8 == 255) d.f2 = __builtin_bit_cast(half2v, 0x7E007E00u);
+        if (CONV && e8 == 255) d.f2 = __builtin_bit_cast(half2v, 0x7E007E00u);
     }
     return d;
 }
@@ -661,10 +667,12 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
                 d1 = decode_act8_far(S.v[i].z, S.v[i].w, farz[i], farf[i]);
             } else {
                 ActDecode p;
-                if (MX) p = mx_decode<AF>((int)S.e[i], ebias[i]);
+                if (MX) p = mx_decode<AF, CONV>((int)S.e[i], ebias[i]);
                 p.negz = negz[INT8 ? i : 0];
-                d0 = decode_act8<AF>(S.v[i].x, S.v[i].y, p);
-                d1 = decode_act8<AF>(S.v[i].z, S.v[i].w, p);
+                uint4 v = S.v[i];
+                if (CONV && AF == CHAM_A_MXFP8_E4M3 && S.e[i] == 255u) v = make_uint4(kE4m3NaN4, kE4m3NaN4, kE4m3NaN4, kE4m3NaN4);
+                d0 = decode_act8<AF>(v.x, v.y, p);
+                d1 = decode_act8<AF>(v.z, v.w, p);
             }
             if (INT8 && CONV && !S.e[i]) d0 = d1 = make_uint4(0u, 0u, 0u, 0u);  // the padding is 0, not the code 0
             lds[buf][r * 8 + (c ^ sw)] = d0;
@@ -762,7 +770,7 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
                 const int c0 = m0 + d * a.W, ext = lines ? 1 : a.W + 1;
                 const int p0 = max(c0 - ext, 0), p1 = min(c0 + rows + ext, a.M);
                 const int e0 = p0 * (CK / 32), e1 = p1 * (CK / 32);
-                for (int o = e0 + 16 * t; o < e1; o += 16 * NT) mx = max(mx, max_exponent(a.xe8, o, min(o + 16, e1)));
+                for (int o = e0 + 16 * t; o < e1; o += 16 * NT) mx = max(mx, max_exponent<true>(a.xe8, o, min(o + 16, e1)));
             }
             for (int o = 32; o > 0; o >>= 1) mx = max(mx, __shfl_xor(mx, o, kWave));
             if (lane == 0) Re[wave] = mx;
@@ -771,7 +779,7 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
             const int r = t / TPR;
             const uint8_t* row = a.xe8 + (int64_t)(m0 + (r < rows ? r : 0)) * (K / 32) + kb * 2;
             int mx = 0;
-            for (int o = 16 * (t % TPR); o < 2 * nsteps; o += 16 * TPR) mx = max(mx, max_exponent(row, o, min(o + 16, 2 * nsteps)));
+            for (int o = 16 * (t % TPR); o < 2 * nsteps; o += 16 * TPR) mx = max(mx, max_exponent<false>(row, o, min(o + 16, 2 * nsteps)));
 #pragma unroll
             for (int o = 1; o < TPR; o <<= 1) mx = max(mx, __shfl_xor(mx, o, kWave));
             if (t % TPR == 0) Re[r] = mx;
@@ -784,7 +792,10 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
         }
 #pragma unroll
         for (int i = 0; i < (MX ? AQ : 1); ++i) ebias[i] = 141 - (CONV ? tmax : Re[t / 4 + RSTEP * i]);
-        for (int r = t; r < BM; r += NT) Rs[r] = ldexpf(1.0f, (CONV ? tmax : Re[r]) - 141);
+        for (int r = t; r < BM; r += NT) {
+            const int e = CONV ? tmax : Re[r];
+            Rs[r] = !CONV && e == 255 ? __uint_as_float(0x7FC00000u) : ldexpf(1.0f, e - 141);
+        }
     }
     store_a(R[0], 0);
     if (LA == 3) {

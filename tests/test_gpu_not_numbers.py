@@ -98,3 +98,29 @@ def test_mx_blocks_of_no_numbers_in_the_convolution(fmt):
     Y, clean = Y.reshape(H * W, N), clean.reshape(H * W, N)
     assert bool(torch.isnan(Y[near]).all())
     assert torch.equal(Y[~near], clean[~near])
+
+
+@pytest.mark.parametrize("fmt", FMT)
+def test_the_byte_255_is_nan_whatever_codes_lie_under_it(fmt):
+    """As another program may write it: finite codes under the scale NaN, in the linear layer and in
+    the convolution, and a split of k that does not hold the block."""
+    case(f"byte 255 {fmt}")
+    M, N, K = 40, 96, 16384
+    x = cham.gated_quantize(_x(7, M, K).to(DEV), None, cham.ACT_NONE, fmt=FMT[fmt])
+    wq = cham.select_weight_formats(_x(8, N, K).to(DEV) * 0.02, 1 << cham.W_INT8_SYM)
+    clean = cham.mixed_linear(x, wq)
+    x.e8m0[9, 3] = 255
+    Y = cham.mixed_linear(x, wq)
+    keep = [m for m in range(M) if m != 9]
+    assert bool(torch.isnan(Y[9]).all()) and torch.equal(Y[keep], clean[keep])
+    B, H, W, C = 1, 6, 7, 64
+    x = cham.gated_quantize(_x(9, B * H * W, C).to(DEV), None, cham.ACT_NONE, fmt=FMT[fmt])
+    x.nsamples = 1
+    wq = cham.select_weight_formats(_x(10, N, 9 * C).to(DEV) * 0.02, 1 << cham.W_INT8_SYM)
+    top = torch.arange(B * H * W, device=DEV)[x.e8m0[:, 1] < x.e8m0.max()][0].item()  # a block that is not the largest
+    clean = cham.conv3x3_mixed(x, B, H, W, wq).reshape(H * W, N)
+    x.e8m0[top, 1] = 255
+    Y = cham.conv3x3_mixed(x, B, H, W, wq).reshape(H * W, N)
+    r, c = torch.arange(H * W, device=DEV) // W, torch.arange(H * W, device=DEV) % W
+    near = ((r - top // W).abs() <= 1) & ((c - top % W).abs() <= 1)
+    assert bool(torch.isnan(Y[near]).all()) and torch.equal(Y[~near], clean[~near])
