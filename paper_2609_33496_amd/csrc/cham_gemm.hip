@@ -45,6 +45,7 @@
 // The MFMA contracts over k in any order as long as both operands agree: lane half h of a
 // k-step takes k = 32h .. 32h+31, sub-step s the 8 k at 32h + 8s.
 #include <cmath>
+#include <type_traits>
 #include <vector>
 
 #include "cham_device.h"
@@ -432,8 +433,6 @@ CHAM_DEV int max_exponent(const uint8_t* p, int o0, int o1) {
     return m;
 }
 
-constexpr uint32_t kE4m3NaN4 = 0x7F7F7F7Fu;  // four E4M3 codes that are NaN
-
 // What a staging row's codes are decoded with: INT8-asym -(1024 + zero point), MX the block's
 // scale (MXINT8 as two half-precision powers of two).
 struct ActDecode {
@@ -446,13 +445,13 @@ struct ActDecode {
 // 2^(e8 - emax + 14) puts the largest block in [2^14, 2^15), so blocks down to 2^-28 of it stay
 // normal in half precision.  Scales below 2^-126 only decode to zeros and are clamped there.  The
 // byte 255 is the scale NaN.  In the linear layer it is its row's largest and makes the row's factor
-// NaN.  In the convolution a block belongs to the rows of several pixels: its codes become NaN as
-// they are staged, and emax is the largest of the other blocks.
+// NaN.  In the convolution a block belongs to the rows of several pixels: its codes become NaN here,
+// and emax is the largest of the other blocks.
 template <int AF, bool CONV>
 CHAM_DEV ActDecode mx_decode(int e8, int ebias) {
     ActDecode d;
     int b = max(e8 + ebias, 1);  // binary32 exponent field of the scale
-    if (CONV) b = min(b, 141);   // more only for 255
+    if (CONV && AF == CHAM_A_MXFP8_E4M3 && e8 == 255) b = 255;  // the converter's scale NaN
     d.scale = __uint_as_float((uint32_t)b << 23);
     if (AF == CHAM_A_MXINT8) {  // 6 fraction bits; q 2^e1 is a normal half, times 2^e2 rounds once
         const int e = b - 127 - 6, e1 = max(e, -14), e2 = max(e - e1, -24);
@@ -669,10 +668,8 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
                 ActDecode p;
                 if (MX) p = mx_decode<AF, CONV>((int)S.e[i], ebias[i]);
                 p.negz = negz[INT8 ? i : 0];
-                uint4 v = S.v[i];
-                if (CONV && AF == CHAM_A_MXFP8_E4M3 && S.e[i] == 255u) v = make_uint4(kE4m3NaN4, kE4m3NaN4, kE4m3NaN4, kE4m3NaN4);
-                d0 = decode_act8<AF>(v.x, v.y, p);
-                d1 = decode_act8<AF>(v.z, v.w, p);
+                d0 = decode_act8<AF>(S.v[i].x, S.v[i].y, p);
+                d1 = decode_act8<AF>(S.v[i].z, S.v[i].w, p);
             }
             if (INT8 && CONV && !S.e[i]) d0 = d1 = make_uint4(0u, 0u, 0u, 0u);  // the padding is 0, not the code 0
             lds[buf][r * 8 + (c ^ sw)] = d0;
@@ -756,6 +753,7 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
         for (int s = 0; s < 4; ++s) load_w(W[WD - 1][s], 1 < klast ? 1 : klast, s);
     }
     if (MX) {
+        int tmax = 0;
         // the largest block exponent of each row over this split's k (convolution: of the pixels
         // that hold every neighbour of the tile's rows), behind the first loads
         if (CONV) {
@@ -765,15 +763,27 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
             // passes of the workgroup stay one run: three cost their latencies one after another
             // (512 x 512: 45.0 with one, 46.9 with three; 64 x 4096: 45.0 with either).
             const bool lines = a.W > rows + 2 && (a.W + 1) * (CK / 32) > 3 * 8 * NT;
-            int mx = 0;
-            for (int d = lines ? -1 : 0; d <= (lines ? 1 : 0); ++d) {
-                const int c0 = m0 + d * a.W, ext = lines ? 1 : a.W + 1;
-                const int p0 = max(c0 - ext, 0), p1 = min(c0 + rows + ext, a.M);
-                const int e0 = p0 * (CK / 32), e1 = p1 * (CK / 32);
-                for (int o = e0 + 16 * t; o < e1; o += 16 * NT) mx = max(mx, max_exponent<true>(a.xe8, o, min(o + 16, e1)));
+            auto scan = [&](auto skip) __attribute__((always_inline)) {
+                int mx = 0;
+                for (int d = lines ? -1 : 0; d <= (lines ? 1 : 0); ++d) {
+                    const int c0 = m0 + d * a.W, ext = lines ? 1 : a.W + 1;
+                    const int p0 = max(c0 - ext, 0), p1 = min(c0 + rows + ext, a.M);
+                    const int e0 = p0 * (CK / 32), e1 = p1 * (CK / 32);
+                    for (int o = e0 + 16 * t; o < e1; o += 16 * NT)
+                        mx = max(mx, max_exponent<decltype(skip)::value>(a.xe8, o, min(o + 16, e1)));
+                }
+                for (int o = 32; o > 0; o >>= 1) mx = max(mx, __shfl_xor(mx, o, kWave));
+                if (lane == 0) Re[wave] = mx;
+                lds_barrier();
+                tmax = 0;
+#pragma unroll
+                for (int w = 0; w < NW; ++w) tmax = max(tmax, Re[w]);
+            };
+            scan(std::false_type{});
+            if (tmax == 255) {  // the same in every wavefront; rare, so the others do not test each byte for it
+                lds_barrier();  // Re has been read
+                scan(std::true_type{});
             }
-            for (int o = 32; o > 0; o >>= 1) mx = max(mx, __shfl_xor(mx, o, kWave));
-            if (lane == 0) Re[wave] = mx;
         } else {
             constexpr int TPR = NT / BM;  // threads per row, consecutive lanes
             const int r = t / TPR;
@@ -783,12 +793,7 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
 #pragma unroll
             for (int o = 1; o < TPR; o <<= 1) mx = max(mx, __shfl_xor(mx, o, kWave));
             if (t % TPR == 0) Re[r] = mx;
-        }
-        lds_barrier();
-        int tmax = 0;
-        if (CONV) {
-#pragma unroll
-            for (int w = 0; w < NW; ++w) tmax = max(tmax, Re[w]);
+            lds_barrier();
         }
 #pragma unroll
         for (int i = 0; i < (MX ? AQ : 1); ++i) ebias[i] = 141 - (CONV ? tmax : Re[t / 4 + RSTEP * i]);

@@ -110,6 +110,7 @@ def test_the_byte_255_is_nan_whatever_codes_lie_under_it(fmt):
     wq = cham.select_weight_formats(_x(8, N, K).to(DEV) * 0.02, 1 << cham.W_INT8_SYM)
     clean = cham.mixed_linear(x, wq)
     x.e8m0[9, 3] = 255
+    x.codes[9, 96:128] = 0
     Y = cham.mixed_linear(x, wq)
     keep = [m for m in range(M) if m != 9]
     assert bool(torch.isnan(Y[9]).all()) and torch.equal(Y[keep], clean[keep])
@@ -120,6 +121,7 @@ def test_the_byte_255_is_nan_whatever_codes_lie_under_it(fmt):
     top = torch.arange(B * H * W, device=DEV)[x.e8m0[:, 1] < x.e8m0.max()][0].item()  # a block that is not the largest
     clean = cham.conv3x3_mixed(x, B, H, W, wq).reshape(H * W, N)
     x.e8m0[top, 1] = 255
+    x.codes[top, 32:64] = 0  # a block of nothing but zeros is NaN under it too
     Y = cham.conv3x3_mixed(x, B, H, W, wq).reshape(H * W, N)
     r, c = torch.arange(H * W, device=DEV) // W, torch.arange(H * W, device=DEV) % W
     near = ((r - top // W).abs() <= 1) & ((c - top % W).abs() <= 1)
