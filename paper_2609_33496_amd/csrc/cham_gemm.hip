@@ -51,6 +51,7 @@
 #include "cham_device.h"
 #include "cham_group.h"
 #include "cham_records.h"
+#include "cham_store.h"
 
 namespace cham {
 namespace {
@@ -879,7 +880,7 @@ __global__ __launch_bounds__(64 * NW, TM * TN >= 8 ? 2 : TM * TN >= 4 ? 3 : 4) v
                     float v = (acc[i][j][r] * rs[r]) * cs[j];
                     if (CORR) v = v + rc[r] * csum[j];
                     const uint32_t bits = __builtin_bit_cast(uint32_t, v);
-                    const int soff = (8 * (r >> 2) + (r & 3)) * N * 4;
+                    const int soff = (int)row_offset(8 * (r >> 2) + (r & 3), N * 4, rows * N * 4);
                     if (cached) __builtin_amdgcn_raw_buffer_store_b32(bits, ro, voff, soff, 0);
                     else __builtin_amdgcn_raw_buffer_store_b32(bits, ro, voff, soff, kStoreNonTemporal);
                 }
