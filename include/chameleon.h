@@ -563,6 +563,125 @@ int cham_block_linear(const cham_bq* x, const cham_bw* w, void* Y, int32_t y_typ
 int cham_block_linear_plan(int64_t M, int64_t N, int64_t K, int32_t y_type, int32_t* out, int32_t out_len);
 
 /* ---------------------------------------------------------------------------------------
+ * 6. attention
+ *
+ * What a transformer block runs between the product that makes queries, keys and values and the
+ * one that reads attention's output: the norm of each head with the rotation by the token's
+ * position, a paged cache of keys and values that is written and read back, and attention over
+ * whole prompts or over the cache.  Sequences lie packed, one after another, in matrices
+ * [T][H][D] of tokens, heads and D elements.  D % 8 == 0, 8 <= D <= 128.
+ * Query head h reads key head h / (Hq / Hk); Hq % Hk == 0.
+ * ------------------------------------------------------------------------------------- */
+#define CHAM_T_E4M3 3  /* a cache's codes; no other operand's type */
+
+/* Rows of heads [T][H][D]: element d of head h of token t at p[t * token + h * head + d].  p, token
+ * and head are multiples of 16 bytes; rows may overlap in no way where they are written. */
+typedef struct cham_heads {
+    void* p;
+    int64_t token, head;   /* strides in elements                                             */
+    int32_t H;
+    int32_t type;          /* CHAM_T_F32, CHAM_T_F16, CHAM_T_BF16                             */
+} cham_heads;
+
+#define CHAM_ROT_HALF 0    /* element i turns with element i + R/2                            */
+#define CHAM_ROT_PAIRS 1   /* element 2i turns with element 2i + 1                            */
+
+/* y = x / sqrt(mean_D(x^2) + eps) * g (norm), then the pairs (a, b), i = 0 .. R/2 - 1, of the first
+ * R elements turn by the angle t = pos freq[i]: (a cos t - b sin t, b cos t + a sin t) * amp.
+ * The squares, their sum and the root are binary64 (every finite row has its norm); angles are
+ * binary64 up to their reduction by pi/2, so far positions keep their angle (absolute error below
+ * 2^-53 |t| + 2^-24); the rest is binary32, rounded once to the output's type. */
+typedef struct cham_rotate {
+    int64_t T;             /* tokens                                                          */
+    int32_t D;
+    int32_t R;             /* even, 0 (no rotation) .. D                                      */
+    int32_t layout;        /* CHAM_ROT_*                                                      */
+    int32_t norm;          /* 0 or 1                                                          */
+    float eps;             /* >= 0; only read with norm                                       */
+    float amp;             /* factor of the turned pairs; 1 = a rotation                      */
+    const void* qg;        /* weights [D] of the norm, 16-byte aligned; NULL = ones           */
+    const void* kg;
+    int32_t qg_type, kg_type;
+    const int32_t* pos;    /* [T] positions; NULL if R = 0                                    */
+    const double* freq;    /* [R / 2] angle for each position; NULL if R = 0                  */
+} cham_rotate;
+
+/* Norm and rotation of queries and keys: qo = y(q), ko = y(k), of the inputs' types (one type for
+ * all four), any strides; an output may be its input itself, with equal strides, and overlaps
+ * nothing else.  Hq or Hk may be 0 (that pair is not touched).
+ * Errors: CHAM_EINVAL (NULL, sizes, strides, alignment, eps, amp), CHAM_EFORMAT (types, layout),
+ * CHAM_ESHAPE (D, or T >= 2^31 - 64), CHAM_EHIP. */
+int cham_norm_rotate(const cham_rotate* r, const cham_heads* q, const cham_heads* qo, const cham_heads* k,
+                     const cham_heads* ko, void* stream);
+
+/* A cache of keys and values in pages: [pages][H][page][D], so the tokens of a page lie together
+ * for each head.  Token t of a sequence whose pages are table[0], table[1], ... lies in page
+ * table[t / page], place t % page; slot = page index * page + place.
+ * E4M3: codes with one scale for each token and head, s = amax / 448 floored at FLT_MIN,
+ * c = E4M3(y fl(1/s)); a row that holds a NaN or an infinity has the scale NaN. */
+typedef struct cham_cache {
+    int64_t pages;         /* pages * page < 2^31                                             */
+    int32_t H, D;          /* E4M3: D % 16 == 0                                               */
+    int32_t page;          /* tokens of a page: a power of two, 16 .. 32768                   */
+    int32_t type;          /* CHAM_T_F16, CHAM_T_BF16 or CHAM_T_E4M3                          */
+    void* k;               /* 16-byte aligned, as v                                           */
+    void* v;
+    float* ks;             /* E4M3: [pages][H][page]; else NULL                               */
+    float* vs;
+} cham_cache;
+
+/* Norm and rotation (r) of keys and queries in one pass with the keys and the values, which take
+ * neither, written into the cache: token t goes to slot slots[t]; a slot outside 0 .. pages * page - 1
+ * (-1, by custom) takes none.  Two tokens of one slot leave it undefined.  q and qo may be NULL.
+ * One type for q, qo, k and v.  Errors: as cham_norm_rotate. */
+int cham_cache_write(const cham_cache* c, const int32_t* slots, const cham_rotate* r, const cham_heads* k,
+                     const cham_heads* v, const cham_heads* q, const cham_heads* qo, void* stream);
+
+/* Sequences of a cache brought back into packed rows: row cu[b] + t holds token t of sequence b, its
+ * page table[b][t / page].  table [B][width], cu [B + 1] (device, ascending from cu[0] >= 0; rows
+ * from cu[B] on, and before cu[0], are left as they are); ko and vo have T rows of c's heads, of one type, the values code
+ * times scale rounded to it.  A token without a page (outside 0 .. pages - 1, or t / page >= width)
+ * comes back as zeros.  Errors: as cham_norm_rotate. */
+int cham_cache_read(const cham_cache* c, const int32_t* table, int64_t width, const int32_t* cu, int64_t B, int64_t T,
+                    const cham_heads* ko, const cham_heads* vo, void* stream);
+
+/* o_i = sum_j p_ij v_j, p_i the softmax over the keys j that query i sees of scale <q_i, k_j>.
+ * causal: query i of a sequence's nq sees its first nk - nq + i + 1 of nk keys (the last query sees all
+ * of them); else all.  A query that sees none gets zeros; keys that are not seen have no influence,
+ * whatever they hold.  Products in 16 bits (q, k, v as they are; p rounded to their type), sums,
+ * maxima and statistics in binary32, one rounding at the end.  Results are bitwise reproducible. */
+typedef struct cham_attn {
+    int64_t B;             /* sequences, < 2^24                                               */
+    int64_t T;             /* rows of q and o                                                 */
+    int32_t D;
+    int32_t causal;        /* 0 or 1 (cham_cache_attention: always causal, not read)          */
+    float scale;           /* > 0, finite                                                     */
+    int32_t pad;
+    const int32_t* cu_q;   /* [B + 1] first rows, ascending from 0 to at most T: rows behind the
+                              last sequence are left as they are.  NULL: B sequences of T / B   */
+    cham_heads q, o;       /* CHAM_T_F16 or CHAM_T_BF16, one type; o overlaps no input        */
+} cham_attn;
+
+/* Attention over packed keys and values k, v [Tk][Hk][D] of q's type: cu_k as cu_q, NULL: B
+ * sequences of Tk / B rows.  ws: cham_attention_workspace_bytes(a, Hk) bytes, written before they are
+ * read; calls that may overlap (two streams, two graphs) need workspaces of their own.
+ * Errors: CHAM_EINVAL (NULL, sizes, strides, alignment, T % B without cu_q, ...), CHAM_EFORMAT
+ * (types), CHAM_ESHAPE (D, H, or a stride or T of 2^22, 2^31 - 2^16 and more), CHAM_EWORKSPACE, CHAM_EHIP. */
+int cham_attention(const cham_attn* a, const cham_heads* k, const cham_heads* v, int64_t Tk, const int32_t* cu_k,
+                   void* ws, size_t ws_bytes, void* stream);
+
+/* Attention of each sequence's newest tokens over its tokens in a cache: lens[b] (device) counts
+ * sequence b's tokens, the queries' own among them, which have been written before; table [B][width] as
+ * in cham_cache_read.  Always causal.  A token without a page is seen by no query; lens beyond
+ * width * page count as that.  c's type is q's, or E4M3.  ws and errors as cham_attention. */
+int cham_cache_attention(const cham_attn* a, const cham_cache* c, const int32_t* table, int64_t width,
+                         const int32_t* lens, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of both for Hk key heads (0 for sizes out of range).  They depend on the current
+ * device's CU count. */
+size_t cham_attention_workspace_bytes(const cham_attn* a, int32_t Hk);
+
+/* ---------------------------------------------------------------------------------------
  * workspace sizes
  * ------------------------------------------------------------------------------------- */
 #define CHAM_OP_SELECT 0

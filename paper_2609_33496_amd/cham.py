@@ -8,7 +8,8 @@ Functions keep the C names without the ``cham_`` prefix:
 ``select_weight_formats``, ``act_stats_reset``, ``act_stats_accumulate``,
 ``build_act_lut``, ``quantize_act``, ``quantize_act_lut``, ``mixed_linear``;
 around 8-bit linear layers ``rms_norm_quantize``, ``gated_quantize`` (each with either of the
-C functions for its output format), ``block_quantize_weights``, ``block_linear``.
+C functions for its output format), ``block_quantize_weights``, ``block_linear``;
+attention: ``norm_rotate``, ``cache_write``, ``cache_read``, ``attention``, ``cache_attention``.
 """
 from __future__ import annotations
 
@@ -93,6 +94,26 @@ class _Gate(ctypes.Structure):
                 ("ldu", ctypes.c_int64), ("type", ctypes.c_int32), ("act", ctypes.c_int32)]
 
 
+class _Heads(ctypes.Structure):
+    _fields_ = [("p", _P), ("token", ctypes.c_int64), ("head", ctypes.c_int64), ("H", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
+class _Rotate(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("D", ctypes.c_int32), ("R", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("norm", ctypes.c_int32), ("eps", ctypes.c_float), ("amp", ctypes.c_float), ("qg", _P), ("kg", _P),
+                ("qg_type", ctypes.c_int32), ("kg_type", ctypes.c_int32), ("pos", _P), ("freq", _P)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("H", ctypes.c_int32), ("D", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("k", _P), ("v", _P), ("ks", _P), ("vs", _P)]
+
+
+class _Attn(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("D", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("pad", ctypes.c_int32), ("cu_q", _P), ("q", _Heads), ("o", _Heads)]
+
+
 _lib = None
 
 
@@ -150,7 +171,16 @@ def lib():
     L.cham_block_quantize_weights.argtypes = [_P, i32, i64, ctypes.POINTER(_BW), _P]
     L.cham_block_linear.argtypes = [ctypes.POINTER(_BQ), ctypes.POINTER(_BW), _P, i32, i64, _P]
     L.cham_block_linear_plan.argtypes = [i64, i64, i64, i32, ctypes.POINTER(i32), i32]
-    for name in ("cham_select_weight_formats", "cham_select_weight_formats_batch", "cham_pack_weights_batch",
+    heads = ctypes.POINTER(_Heads)
+    L.cham_norm_rotate.argtypes = [ctypes.POINTER(_Rotate), heads, heads, heads, heads, _P]
+    L.cham_cache_write.argtypes = [ctypes.POINTER(_Cache), _P, ctypes.POINTER(_Rotate), heads, heads, heads, heads, _P]
+    L.cham_cache_read.argtypes = [ctypes.POINTER(_Cache), _P, i64, _P, i64, i64, heads, heads, _P]
+    L.cham_attention.argtypes = [ctypes.POINTER(_Attn), heads, heads, i64, _P, _P, sz, _P]
+    L.cham_cache_attention.argtypes = [ctypes.POINTER(_Attn), ctypes.POINTER(_Cache), _P, i64, _P, _P, sz, _P]
+    L.cham_attention_workspace_bytes.argtypes = [ctypes.POINTER(_Attn), i32]
+    L.cham_attention_workspace_bytes.restype = sz
+    for name in ("cham_norm_rotate", "cham_cache_write", "cham_cache_read", "cham_attention", "cham_cache_attention",
+                 "cham_select_weight_formats", "cham_select_weight_formats_batch", "cham_pack_weights_batch",
                  "cham_act_stats_reset", "cham_act_stats_accumulate",
                  "cham_act_stats_accumulate_batch",
                  "cham_build_act_lut", "cham_quantize_act", "cham_quantize_act_lut", "cham_quantize_act_noalloc",
@@ -951,3 +981,300 @@ def block_linear_plan(M: int, N: int, K: int, dtype: torch.dtype = torch.bfloat1
     out = (ctypes.c_int32 * 3)()
     _check(lib().cham_block_linear_plan(M, N, K, _TYPES[dtype] | (_EXACT if exact else 0), out, 3), "block_linear_plan")
     return tuple(out)
+
+
+# -------------------------------------------------------------------------------------------
+# attention
+# -------------------------------------------------------------------------------------------
+ROT_HALF, ROT_PAIRS = range(2)
+_E4M3 = 3  # CHAM_T_E4M3
+_CACHE_TYPES = {torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: _E4M3}
+_NO_HEADS = _Heads()
+
+
+def _heads(t: torch.Tensor, name: str, T: int, D: int, dev, ty: int, H: int = -1) -> _Heads:
+    """Check rows of heads [T, H, D] of type ty on dev, any strides along tokens and heads."""
+    at = t.get_device()
+    if at < 0 or at != dev.index:
+        raise ValueError(f"{name} must be a device tensor on {dev}")
+    if _TYPES.get(t.dtype) != ty:
+        raise ValueError(f"{name} is of type {t.dtype}, which does not fit the others")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != T or shape[2] != D or (H >= 0 and shape[1] != H):
+        raise ValueError(f"{name} must be of shape ({T}, {H if H >= 0 else 'heads'}, {D}), got {tuple(shape)}")
+    if stride[2] != 1 and D > 1:
+        raise ValueError(f"{name} must have unit stride along a head's elements")
+    return _Heads(t.data_ptr(), stride[0], stride[1], shape[1], ty)
+
+
+def _float_type(t: torch.Tensor, name: str) -> int:
+    ty = _TYPES.get(t.dtype)
+    if ty is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16")
+    return ty
+
+
+def _vector(t: torch.Tensor, name: str, n: int, dtype, dev) -> int:
+    """Check a contiguous device vector; its address."""
+    if t.get_device() != dev.index or t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} [{n}] on {dev}")
+    return t.data_ptr()
+
+
+def _empty_heads(T, H, D, dtype, dev, stream):
+    if stream is None:
+        return torch.empty(T, H, D, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(T, H, D, dtype=dtype, device=dev)
+
+
+class Cache:
+    """Pages of keys and values (device tensors, see cham_cache): k, v [pages, heads, page, D] in
+    float16, bfloat16 or float8_e4m3fn, the last with float32 scales k_scale, v_scale [pages, heads, page]."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "pages", "H", "page", "D", "device", "_struct")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        ty, at, shape = _CACHE_TYPES.get(k.dtype), k.get_device(), k.shape
+        if ty is None or v.dtype is not k.dtype:
+            raise ValueError("k and v must both be float16, bfloat16 or float8_e4m3fn")
+        if len(shape) != 4 or v.shape != shape:
+            raise ValueError("k and v must be of one shape [pages, heads, page, D]")
+        if at < 0 or v.get_device() != at or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("k and v must be contiguous device tensors on one device")
+        ks = vs = None
+        if ty == _E4M3:
+            for t in (k_scale, v_scale):
+                if (t is None or t.dtype is not torch.float32 or t.shape != shape[:3] or t.get_device() != at or
+                        not t.is_contiguous()):
+                    raise ValueError(f"an 8-bit cache needs contiguous float32 scales of shape {tuple(shape[:3])} beside it")
+            ks, vs = k_scale.data_ptr(), v_scale.data_ptr()
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("a 16-bit cache has no scales")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.H, self.page, self.D = shape
+        self.device = k.device
+        self._struct = _Cache(shape[0], shape[1], shape[3], shape[2], ty, k.data_ptr(), v.data_ptr(), ks, vs)
+
+
+def alloc_cache(pages: int, H: int, page: int, D: int, dtype: torch.dtype = torch.float8_e4m3fn, device="cuda") -> Cache:
+    """A cache of `pages` pages of `page` tokens (a power of two, 16 and more) and H heads; its
+    memory is not initialized."""
+    k = torch.empty((2, pages, H, page, D), dtype=dtype, device=device)
+    if dtype is not torch.float8_e4m3fn:
+        return Cache(k[0], k[1])
+    s = torch.empty((2, pages, H, page), dtype=torch.float32, device=device)
+    return Cache(k[0], k[1], s[0], s[1])
+
+
+def _rotate(T, D, dev, q_weight, k_weight, eps, norm, positions, freq, layout, amp) -> _Rotate:
+    w = [0, 0, 0, 0]
+    for i, (t, name) in enumerate(((q_weight, "q_weight"), (k_weight, "k_weight"))):
+        if t is not None:
+            if not norm:
+                raise ValueError(f"{name} is a weight of the norm, which norm=False leaves out")
+            w[2 + i] = _float_type(t, name)
+            w[i] = _vector(t, name, D, t.dtype, dev)
+    R = pos = fr = 0
+    if (positions is None) != (freq is None):
+        raise ValueError("a rotation needs positions and freq")
+    if freq is not None:
+        R = 2 * freq.numel()
+        pos, fr = _vector(positions, "positions", T, torch.int32, dev), _vector(freq, "freq", R // 2, torch.float64, dev)
+    return _Rotate(T, D, R, layout, int(bool(norm)), eps, amp, w[0] or None, w[1] or None, w[2], w[3], pos or None, fr or None)
+
+
+def norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], *, q_weight: Optional[torch.Tensor] = None,
+                k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, norm: bool = True,
+                positions: Optional[torch.Tensor] = None, freq: Optional[torch.Tensor] = None, layout: int = ROT_HALF,
+                amp: float = 1.0, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+    """(q', k'): each head x / sqrt(mean(x^2) + eps) * weight (norm=False: as it is), then its first
+    2 len(freq) elements turned by positions[t] * freq[i] and scaled by amp; layout ROT_HALF turns
+    element i with i + len(freq), ROT_PAIRS 2i with 2i + 1.  q [T, Hq, D] and k [T, Hk, D] (slices of one
+    matrix, or None) of one type; positions int32 [T], freq float64 [at most D / 2].  q_out=q and
+    k_out=k work in place."""
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("q or k must be given")
+    if x.dim() != 3:
+        raise ValueError("q and k must be of shape (tokens, heads, D)")
+    T, _, D = x.shape
+    dev, ty = x.device, _float_type(x, "q and k")
+    r = _rotate(T, D, dev, q_weight, k_weight, eps, norm, positions, freq, layout, amp)
+    st = []
+    outs = [q_out, k_out]
+    for i, (t, name) in enumerate(((q, "q"), (k, "k"))):
+        if t is None:
+            if outs[i] is not None:
+                raise ValueError(f"{name}_out without {name}")
+            st += [_Heads(None, 0, 0, 0, ty)] * 2
+            continue
+        s = _heads(t, name, T, D, dev, ty)
+        if outs[i] is None:
+            H = s.H
+            outs[i] = o = _empty_heads(T, H, D, t.dtype, dev, stream)
+            st += [s, _Heads(o.data_ptr(), H * D, D, H, ty)]
+        else:
+            st += [s, _heads(outs[i], name + "_out", T, D, dev, ty, s.H)]
+    rc = _on_device(dev, stream, lib().cham_norm_rotate, r, st[0], st[1], st[2], st[3])
+    _check(rc, "norm_rotate")
+    return outs
+
+
+def cache_write(cache: Cache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None, *,
+                q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                norm: bool = True, positions: Optional[torch.Tensor] = None, freq: Optional[torch.Tensor] = None,
+                layout: int = ROT_HALF, amp: float = 1.0, q_out: Optional[torch.Tensor] = None, stream=None):
+    """Keys (normed and turned as norm_rotate does) and values (as they are) of token t written to slot
+    slots[t] = page index * page + place of the cache; a slot outside it (-1) takes none, and no two
+    tokens may have one slot.  Returns q normed and turned in the same pass (None without q)."""
+    if k.dim() != 3:
+        raise ValueError("k must be of shape (tokens, heads, D)")
+    T, H, D = k.shape
+    dev, ty = k.device, _float_type(k, "k")
+    if cache.device != dev or (H, D) != (cache.H, cache.D):
+        raise ValueError(f"the cache holds {cache.H} heads of {cache.D} on {cache.device}")
+    r = _rotate(T, D, dev, q_weight, k_weight, eps, norm, positions, freq, layout, amp)
+    ks, vs = _heads(k, "k", T, D, dev, ty), _heads(v, "v", T, D, dev, ty, H)
+    at = _vector(slots, "slots", T, torch.int32, dev)
+    qs = os = None
+    if q is not None:
+        qs = _heads(q, "q", T, D, dev, ty)
+        if q_out is None:
+            q_out = _empty_heads(T, qs.H, D, q.dtype, dev, stream)
+        os = _heads(q_out, "q_out", T, D, dev, ty, qs.H)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    elif q_weight is not None:
+        raise ValueError("q_weight without q")
+    _check(_on_device(dev, stream, lib().cham_cache_write, cache._struct, at, r, ks, vs, qs, os), "cache_write")
+    return q_out
+
+
+def _table(table: torch.Tensor, B: int, dev) -> int:
+    if table.dim() != 2 or table.shape[0] != B or table.dtype is not torch.int32 or table.get_device() != dev.index or \
+            not table.is_contiguous():
+        raise ValueError(f"table must be a contiguous int32 [{B}, pages of a sequence] on {dev}")
+    return table.data_ptr()
+
+
+def cache_read(cache: Cache, table: torch.Tensor, cu: torch.Tensor, total: int, *, dtype: torch.dtype = torch.bfloat16,
+               k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, stream=None):
+    """(k, v) [total, heads, D]: rows cu[b] .. cu[b + 1] hold the tokens of sequence b, whose pages
+    are table[b] (int32 [B, pages], cu int32 [B + 1] on the device).  Rows from cu[B] on are left as they are
+    (of new tensors: undefined); tokens without a page come back as zeros."""
+    dev, D, H = cache.device, cache.D, cache.H
+    if (k_out is None) != (v_out is None):
+        raise ValueError("k_out and v_out go together")
+    if k_out is None:
+        ty = _TYPES.get(dtype)
+        if ty is None:
+            raise ValueError("dtype must be float32, float16 or bfloat16")
+        if total < 0:
+            raise ValueError("total must not be negative")
+        k_out, v_out = _empty_heads(total, H, D, dtype, dev, stream), _empty_heads(total, H, D, dtype, dev, stream)
+    else:
+        ty = _float_type(k_out, "k_out")
+    ko, vo = _heads(k_out, "k_out", total, D, dev, ty, H), _heads(v_out, "v_out", total, D, dev, ty, H)
+    if cu.dim() != 1 or cu.shape[0] < 1:
+        raise ValueError("cu must hold a start for each sequence and the end")
+    B = cu.shape[0] - 1
+    c, t = _vector(cu, "cu", B + 1, torch.int32, dev), _table(table, B, dev)
+    _check(_on_device(dev, stream, lib().cham_cache_read, cache._struct, t, table.shape[1], c, B, total, ko, vo), "cache_read")
+    return k_out, v_out
+
+
+def _attn(q, B, cu_q, causal, scale, out, Hk, ws, stream):
+    """The descriptor, output and workspace of an attention call."""
+    if q.dim() != 3:
+        raise ValueError("q must be of shape (tokens, heads, D)")
+    T, Hq, D = q.shape
+    dev, ty = q.device, _float_type(q, "q")
+    if ty == 0:
+        raise ValueError("q must be float16 or bfloat16")
+    if Hk < 1 or Hq % Hk != 0:
+        raise ValueError(f"{Hq} query heads cannot share {Hk} key heads")
+    qs = _heads(q, "q", T, D, dev, ty)
+    if out is None:
+        out = _empty_heads(T, Hq, D, q.dtype, dev, stream)
+        os = _Heads(out.data_ptr(), Hq * D, D, Hq, ty)
+    else:
+        os = _heads(out, "out", T, D, dev, ty, Hq)
+    cu = None if cu_q is None else _vector(cu_q, "cu_q", B + 1, torch.int32, dev)
+    a = _Attn(B, T, D, int(bool(causal)), D ** -0.5 if scale is None else scale, 0, cu, qs, os)
+    if ws is None:
+        ws = _empty(1, attention_workspace_bytes(D, dev), torch.uint8, dev, stream)
+    elif ws.get_device() != dev.index or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
+    return a, out, dev, ws
+
+
+_attn_ws = {}
+
+
+def attention_workspace_bytes(D: int, device="cuda") -> int:
+    """Workspace bytes of attention and cache_attention for heads of D on a device."""
+    dev = device if isinstance(device, torch.device) else torch.device(device)
+    key = (D, dev.index if dev.index is not None else _device_now())
+    n = _attn_ws.get(key)
+    if n is None:
+        h = _Heads(None, 0, 0, 1, 2)
+        with torch.cuda.device(key[1]):
+            n = lib().cham_attention_workspace_bytes(_Attn(0, 0, D, 0, 1.0, 0, None, h, h), 1)
+        _attn_ws[key] = n
+    return n
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, batch: Optional[int] = None,
+              cu_q: Optional[torch.Tensor] = None, cu_k: Optional[torch.Tensor] = None, causal: bool = False,
+              scale: Optional[float] = None, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """softmax(scale q k^T) v of packed sequences: q [Tq, Hq, D], k and v [Tk, Hk, D], float16 or bfloat16,
+    Hq a multiple of Hk; scale: D^-0.5 if None.  Sequences: `batch` (1 if None) of equal lengths, or rows
+    cu_q[b] .. cu_q[b + 1] of q with cu_k[b] .. cu_k[b + 1] of k (int32 [B + 1] on the device; cu_k: cu_q if None).
+    causal is aligned at the sequences' ends: the last query sees every key.  A query that sees none
+    gets zeros; rows from cu_q[B] on are left as they are (of a new tensor: undefined)."""
+    if cu_q is None:
+        if cu_k is not None:
+            raise ValueError("cu_k needs cu_q")
+        B = 1 if batch is None else batch
+        if B < 1 or q.shape[0] % B or k.shape[0] % B:
+            raise ValueError(f"{q.shape[0]} queries and {k.shape[0]} keys are not {B} sequences of equal lengths")
+    else:
+        if batch is not None:
+            raise ValueError("give batch or cu_q")
+        if cu_q.dim() != 1 or cu_q.shape[0] < 1:
+            raise ValueError("cu_q must hold a start for each sequence and the end")
+        B = cu_q.shape[0] - 1
+        if cu_k is None:
+            cu_k = cu_q
+    if k.dim() != 3:
+        raise ValueError("k and v must be of shape (tokens, heads, D)")
+    a, out, dev, ws = _attn(q, B, cu_q, causal, scale, out, k.shape[1], ws, stream)
+    Tk, ty = k.shape[0], a.q.type
+    ks, vs = _heads(k, "k", Tk, a.D, dev, ty), _heads(v, "v", Tk, a.D, dev, ty, k.shape[1])
+    cu = None if cu_k is None else _vector(cu_k, "cu_k", B + 1, torch.int32, dev)
+    _check(_on_device(dev, stream, lib().cham_attention, a, ks, vs, Tk, cu, ws.data_ptr(), ws.numel()), "attention")
+    return out
+
+
+def cache_attention(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.Tensor,
+                    cu_q: Optional[torch.Tensor] = None, *, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                    ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of each sequence's newest tokens over its tokens in the cache, causal: q [T, Hq, D] holds
+    one token of each sequence (cu_q None) or rows cu_q[b] .. cu_q[b + 1] for sequence b; lens[b] (int32 [B]
+    on the device) counts its tokens with these, which cache_write has written before; table int32
+    [B, pages of a sequence].  The cache is of q's type or in 8 bits."""
+    if lens.dim() != 1:
+        raise ValueError("lens must hold a length for each sequence")
+    B = lens.shape[0]
+    if cu_q is None and q.shape[0] != B:
+        raise ValueError(f"without cu_q, q must hold one token of each of {B} sequences")
+    a, out, dev, ws = _attn(q, B, cu_q, True, scale, out, cache.H, ws, stream)
+    if cache.device != dev or cache.D != a.D:
+        raise ValueError(f"the cache holds heads of {cache.D} on {cache.device}")
+    n, t = _vector(lens, "lens", B, torch.int32, dev), _table(table, B, dev)
+    _check(_on_device(dev, stream, lib().cham_cache_attention, a, cache._struct, t, table.shape[1], n, ws.data_ptr(),
+                      ws.numel()), "cache_attention")
+    return out
