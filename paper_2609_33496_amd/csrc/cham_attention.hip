@@ -28,7 +28,8 @@ namespace {
 enum { kPacked, kPages, kCodes };  // where keys and values come from: rows, 16-bit pages, E4M3 pages
 
 constexpr float kLog2e = 1.44269504f;
-constexpr float kGrow = 8.0f;    // the reference follows scores more than 2^8 above it
+constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100, kTrans = 0x400;  // sched_group_barrier's classes
+constexpr float kGrow = 8.0f;    // few_kernel: the reference follows scores more than 2^8 above it
 constexpr float kVGrow = 16.0f;  // and the values' scale follows scales more than 16 times it
 
 constexpr int kRowsTile = 128, kKeysTile = 64;  // of a workgroup of the tiled kernel and its step
@@ -91,10 +92,12 @@ CHAM_DEV Seq sequence(const AttnArgs& a, int b) {
     return s;
 }
 
+// a value that all lanes share, in scalar registers
+CHAM_DEV int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 CHAM_DEV int64_t wave_add(int64_t v) {
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor((long long)v, d);
-    return v;
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
 }
 CHAM_DEV int wave_scan(int v, int lane) {  // inclusive
 #pragma unroll
@@ -132,8 +135,8 @@ CHAM_DEV bool find_piece(const AttnArgs& a, int at, int hk, bool tiles, Piece* p
         const int upto = wave_scan(mine, lane), split_upto = wave_scan(split, lane);
         const uint64_t past = __ballot(before + upto > at);
         if (past == 0) {
-            before += __shfl(upto, kWave - 1);
-            split_before += __shfl(split_upto, kWave - 1);
+            before += __builtin_amdgcn_readlane(upto, kWave - 1);
+            split_before += __builtin_amdgcn_readlane(split_upto, kWave - 1);
             continue;
         }
         const int l = __builtin_ctzll(past);
@@ -186,6 +189,13 @@ CHAM_DEV uint32_t widen2(uint32_t w) {
     if constexpr (T == CHAM_T_F16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
 }
+// c plus two 16-bit values
+template <int T>
+CHAM_DEV float add2(uint32_t w, float c) {
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    if constexpr (T == CHAM_T_F16) return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, w), half2v{(_Float16)1, (_Float16)1}, c, false);
+    else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, w), bf2{(__bf16)1.0f, (__bf16)1.0f}, c, false);
+}
 template <int T>
 CHAM_DEV u4 widen8(uint32_t lo, uint32_t hi) {
     return u4{widen2<T, false>(lo), widen2<T, true>(lo), widen2<T, false>(hi), widen2<T, true>(hi)};
@@ -202,9 +212,8 @@ CHAM_DEV u4 load16(const char* p) { return *(const u4*)p; }
 
 // four transposed 16-bit values: a lane names 8 bytes of a row of LDS and receives, of the four rows
 // that its 16 lanes name, the column of its own place among them
-CHAM_DEV uint2 read_tr(const char* p) {
-    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)(__attribute__((address_space(3))) char*)p));
-}
+typedef __attribute__((address_space(3))) uint8_t Lds;
+CHAM_DEV uint2 read_tr(const Lds* p) { return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)p)); }
 
 CHAM_DEV float max_halves(float v) {  // over lanes l and l ^ 32
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -231,23 +240,40 @@ CHAM_DEV void put4(const cham_heads& o, int64_t at, float a, float b, float c, f
 // ------------------------------------------------------------------------------------
 // the tiled kernel: 128 rows of queries, 32 a wavefront, against steps of 64 keys
 // ------------------------------------------------------------------------------------
-// KS: steps of 16 along D for the scores, DB: blocks of 32 along D for the outputs.  Rows of keys lie
-// 2 KS + 1 chunks of 16 bytes apart (an odd count: 16 rows fall on 16 different bank groups), rows of
-// values SV, 4 mod 8 (a transposing read takes 64 bytes of four rows).
+// KS: steps of 16 along D for the scores, DB: blocks of 32 along D for the outputs.  Keys and values
+// lie in LDS as rows of CU chunks of 16 bytes, without gaps, so that 16-bit ones go there from memory
+// directly; a chunk's place within its row is swizzled so that neither the 16 rows of a score
+// operand nor the four of a transposing read fall on the same banks.
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) u2 LdsU2;
+typedef __attribute__((address_space(3))) u4 LdsU4;
+typedef __attribute__((address_space(3))) f4 LdsF4;
+typedef __attribute__((address_space(3))) float LdsFloat;
+constexpr int kBufferFlags = 0x00020000;    // buffer descriptor word 3: 32-bit data, raw
+constexpr uint32_t kOutside = 0x80000000u;  // an offset past every buffer: such loads give zeros
+
+// 16 bytes a lane from offset `from` of a buffer into LDS, the wavefront's from `to` on
+CHAM_DEV void load_lds(__amdgpu_buffer_rsrc_t b, Lds* to, uint32_t from) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void*)to, 16, from, 0, 0, 0);
+}
+
 template <int KS, int DB>
 struct Tile {
-    static constexpr int SK = 2 * KS + 1, SV = DB == 4 ? 20 : 12;
-    u4 k[2][kKeysTile][SK];
-    u4 v[2][kKeysTile][SV];
-    float ks[2][kKeysTile], vs[2][kKeysTile];  // scales of the keys and values
-    float vmax[2][4];                          // the largest finite of each 16 values' scales
-    int flags[2][4];                           // of each 16 keys: 1 a value is not finite, 2 no page
+    static constexpr int CU = KS == 4 ? 8 : KS <= 6 ? 12 : 16;
+    static constexpr int kBytes = kKeysTile * CU * 16;  // of one buffer
+    static constexpr int kLoads = CU / 4;               // of a wavefront's 16 rows, 1 KB each
+    // place of chunk c of row r: c ^ key
+    static CHAM_DEV int key_k(int r) { return CU == 16 ? r & 15 : CU == 8 ? (r >> 1) & 7 : (r >> 2) & 3; }
+    static CHAM_DEV int key_v(int r) { return CU == 16 ? (r & 3) << 2 : CU == 8 ? (r << 1) & 4 : 0; }
 };
 
 template <int T, int KS, int DB, int SRC>
 __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     using L = Tile<KS, DB>;
-    __shared__ L lds;
+    // each buffer a variable of its own: the compiler then knows that a step's reads do not touch what
+    // the loads under way write, and does not wait for them
+    __shared__ __align__(1024) uint8_t k0[L::kBytes], k1[L::kBytes], v0[L::kBytes], v1[L::kBytes];
+    __shared__ __align__(16) float lds_ks[2][kKeysTile], lds_vs[2][kKeysTile];  // kCodes: scales
     const int hk = blockIdx.x % a.Hk;
     Piece p;
     if (!find_piece<SRC, kRowsTile, kKeysTile>(a, blockIdx.x / a.Hk, hk, false, &p)) return;
@@ -257,12 +283,14 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     const bool causal = SRC != kPacked || a.a.causal;
     // keys that a row sees: the first `lim`
     const auto limit = [&](int row) { return causal ? min(max(p.nk - p.nq + row / a.G + 1, 0), p.nk) : p.nk; };
-    const int my_row = row0 + wave * 32 + col, last_row = min(row0 + kRowsTile, rows) - 1;
+    const int my_row = row0 + wave * 32 + col;
     const bool live = row0 + wave * 32 < rows;
     const int lim = my_row < rows ? limit(my_row) : 0;
     // of the wavefront's rows the fewest and the most, and of the tile's the most
-    const int lim_lo = limit(row0 + wave * 32), lim_hi = limit(min(row0 + wave * 32 + 31, rows - 1));
-    const int end = min(p.end, (limit(last_row) + kKeysTile - 1) / kKeysTile);
+    const int lim_lo = __builtin_amdgcn_readfirstlane(limit(row0 + wave * 32));
+    const int lim_hi = __builtin_amdgcn_readfirstlane(limit(min(row0 + wave * 32 + 31, rows - 1)));
+    const int lim_tile = __builtin_amdgcn_readfirstlane(limit(min(row0 + kRowsTile, rows) - 1));
+    const int end = min(p.end, (lim_tile + kKeysTile - 1) / kKeysTile);
 
     // the queries: second operand of the scores' products
     u4 q[KS];
@@ -274,250 +302,327 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         if (my_row < rows && 16 * s + 8 * h < D) q[s] = load16((const char*)a.a.q.p + (q_at + 16 * s + 8 * h) * 2);
     }
 
-    // staging: a wavefront brings 16 keys of a step
-    constexpr int kUnits = SRC == kCodes ? KS : 2 * KS;  // chunks of 16 bytes of a row, those behind D among them
-    constexpr int kLoads = (16 * kUnits + kWave - 1) / kWave;
-    const int row_units = SRC == kCodes ? D / 16 : D / 8;
-    u4 rk[kLoads], rv[kLoads];
-    float scale_in = 0.0f;
-    int no_page = 0;
-    const auto fetch = [&](int step) {
+    // A wavefront brings 16 keys of a step, which lie in one page.  16-bit rows go to LDS directly:
+    // load i takes the 64 chunks from 64 i on; rows past the last key and chunks past D are outside the
+    // buffer and become zeros.  Codes go through registers, where they are widened.
+    constexpr int kLoads = SRC == kCodes ? (16 * KS + kWave - 1) / kWave : L::kLoads;
+    const int ldk = SRC == kPacked ? (int)(a.k.token * 2) : D * (SRC == kCodes ? 1 : 2);
+    const int ldv = SRC == kPacked ? (int)(a.v.token * 2) : ldk;
+    uint32_t off_k[kLoads], off_v[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int u = lane + kWave * i;
+        if constexpr (SRC == kCodes) {
+            const int row = u / KS, c = u % KS;
+            off_k[i] = off_v[i] = row < 16 && 16 * c < D ? (uint32_t)(row * ldk + c * 16) : kOutside;
+        } else {
+            const int row = u / L::CU, ck = (u % L::CU) ^ L::key_k(row), cv = (u % L::CU) ^ L::key_v(row);
+            off_k[i] = 8 * ck < D ? (uint32_t)(row * ldk + ck * 16) : kOutside;
+            off_v[i] = 8 * cv < D ? (uint32_t)(row * ldv + cv * 16) : kOutside;
+        }
+    }
+    // pages of the next step's keys (one a lane), a step ahead of their use; -1: none
+    const auto page_of = [&](int step) {
+        const int key = step * kKeysTile + lane;
+        int page = -1;
+        if (key < p.nk) page = a.table[(int64_t)p.seq * a.width + (key >> a.shift)];
+        return page >= 0 && page < a.c.pages ? page : -1;
+    };
+    u4 rk[SRC == kCodes ? kLoads : 1], rv[SRC == kCodes ? kLoads : 1];
+    float k_scale = 0.0f, v_scale = 0.0f;
+    int pages = -1;
+    uint32_t no_page = 0, no_page_next = 0;  // which 16 keys of the step have none
+    const auto fetch = [&](int step, Lds* kb, Lds* vb) __attribute__((always_inline)) {
         const int key0 = step * kKeysTile + 16 * wave;
-        const char *kp = nullptr, *vp = nullptr;
-        int64_t ldk = 0, ldv = 0, at = 0;
-        bool in = key0 < p.nk;
-        no_page = 0;
+        const char *kp, *vp;
+        int left = min(max(p.nk - key0, 0), 16);
         if constexpr (SRC == kPacked) {
-            ldk = a.k.token * 2, ldv = a.v.token * 2;
             kp = (const char*)a.k.p + ((int64_t)(p.k0 + key0) * a.k.token + (int64_t)hk * a.k.head) * 2;
             vp = (const char*)a.v.p + ((int64_t)(p.k0 + key0) * a.v.token + (int64_t)hk * a.v.head) * 2;
         } else {
-            const int page = in ? a.table[(int64_t)p.seq * a.width + (key0 >> a.shift)] : 0;
-            if (page < 0 || page >= a.c.pages) {
-                in = false;
-                no_page = 2;
-            }
-            at = (((int64_t)page * a.Hk + hk) << a.shift) + (key0 & ((1 << a.shift) - 1));
-            ldk = ldv = D * (SRC == kCodes ? 1 : 2);
+            const int page = __builtin_amdgcn_readlane(pages, 16 * wave);
+            const uint64_t none = __ballot(pages < 0 && step * kKeysTile + lane < p.nk);
+            no_page_next = (none & 1) | (none >> 15 & 2) | (none >> 30 & 4) | (none >> 45 & 8);
+            if (page < 0) left = 0;
+            const int64_t at = (((int64_t)max(page, 0) * a.Hk + hk) << a.shift) + (key0 & ((1 << a.shift) - 1));
             kp = (const char*)a.c.k + at * ldk;
             vp = (const char*)a.c.v + at * ldv;
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int u = lane + kWave * i, row = u / kUnits, c = u % kUnits;
-            rk[i] = rv[i] = u4{0, 0, 0, 0};
-            if (in && row < 16 && key0 + row < p.nk && c < row_units) {
-                rk[i] = load16(kp + row * (int)ldk + c * 16);
-                rv[i] = load16(vp + row * (int)ldv + c * 16);
-            }
-        }
-        if constexpr (SRC == kCodes) {
-            scale_in = 0.0f;
-            if (in && lane < 32 && key0 + (lane & 15) < p.nk) scale_in = (lane < 16 ? a.c.ks : a.c.vs)[at + (lane & 15)];
-        }
-    };
-    const auto store = [&](int step, int buf) {
-        bool bad = false;
-        const bool look = (step + 1) * kKeysTile > limit(row0);  // some row does not see all of these keys
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int u = lane + kWave * i, row = 16 * wave + u / kUnits, c = u % kUnits;
-            if (16 * kUnits % kWave == 0 || u < 16 * kUnits) {
-                if constexpr (SRC == kCodes) {
-                    const u4 v0 = widen8<T>(rv[i][0], rv[i][1]), v1 = widen8<T>(rv[i][2], rv[i][3]);
-                    lds.k[buf][row][2 * c] = widen8<T>(rk[i][0], rk[i][1]);
-                    lds.k[buf][row][2 * c + 1] = widen8<T>(rk[i][2], rk[i][3]);
-                    lds.v[buf][row][2 * c] = v0;
-                    lds.v[buf][row][2 * c + 1] = v1;
-                    if (look)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) bad |= not_finite<T>(v0[j]) || not_finite<T>(v1[j]);
-                } else {
-                    lds.k[buf][row][c] = rk[i];
-                    lds.v[buf][row][c] = rv[i];
-                    if (look)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) bad |= not_finite<T>(rv[i][j]);
+            if constexpr (SRC == kCodes) {
+                const int key = step * kKeysTile + lane;
+                const int64_t row = (((int64_t)pages * a.Hk + hk) << a.shift) + (key & ((1 << a.shift) - 1));
+                k_scale = v_scale = 0.0f;
+                if (pages >= 0) {
+                    v_scale = a.c.vs[row];
+                    if (wave == 0) k_scale = a.c.ks[row];
                 }
             }
+            pages = page_of(step + 1);
         }
+        // row r < left lies wholly before `size`, row `left` behind it
+        const int row_bytes = D * (SRC == kCodes ? 1 : 2);
+        const auto size = [&](int ld) { return left > 0 ? (left - 1) * ld + row_bytes : 0; };
+        const __amdgpu_buffer_rsrc_t bk = __builtin_amdgcn_make_buffer_rsrc((void*)kp, (short)0, size(ldk), kBufferFlags);
+        const __amdgpu_buffer_rsrc_t bv = __builtin_amdgcn_make_buffer_rsrc((void*)vp, (short)0, size(ldv), kBufferFlags);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if constexpr (SRC == kCodes) {
+                rk[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(bk, off_k[i], 0, 0));
+                rv[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(bv, off_v[i], 0, 0));
+            } else {
+                const int to = (wave * L::kLoads + i) * 1024;
+                load_lds(bk, kb + to, off_k[i]);
+                load_lds(bv, vb + to, off_v[i]);
+            }
+        }
+    };
+    // kCodes: o is the sum over vref, and vs hold the values' scales over it.  All wavefronts see all
+    // scales, so they have one vref; it follows the largest finite scale of a step.
+    float vref = 0.0f, vinv = 0.0f, v_fall = 1.0f;
+    const auto store = [&](int buf, Lds* kb, Lds* vb) __attribute__((always_inline)) {
         if constexpr (SRC == kCodes) {
-            if (lane < 16) lds.ks[buf][16 * wave + lane] = scale_in;
-            else if (lane < 32) lds.vs[buf][16 * wave + lane - 16] = scale_in;
-            uint32_t m = __float_as_uint(scale_in) & 0x7fffffffu;
-            m = lane >= 16 && lane < 32 && m < kInfBits ? m : 0;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int u = lane + kWave * i, in = u / KS, c = 2 * (u % KS);
+                if (16 * KS % kWave == 0 || in < 16) {
+                    const int row = (16 * wave + in) * L::CU;
+                    *(LdsU4*)(kb + 16 * (row + (c ^ L::key_k(in)))) = widen8<T>(rk[i][0], rk[i][1]);
+                    *(LdsU4*)(kb + 16 * (row + ((c + 1) ^ L::key_k(in)))) = widen8<T>(rk[i][2], rk[i][3]);
+                    *(LdsU4*)(vb + 16 * (row + (c ^ L::key_v(in)))) = widen8<T>(rv[i][0], rv[i][1]);
+                    *(LdsU4*)(vb + 16 * (row + ((c + 1) ^ L::key_v(in)))) = widen8<T>(rv[i][2], rv[i][3]);
+                }
+            }
+            uint32_t m = __float_as_uint(v_scale) & 0x7fffffffu;
+            m = m < kInfBits ? m : 0;
             m = dpp_maxu<0x140>(dpp_maxu<0x141>(dpp_maxu<0x4E>(dpp_maxu<0xB1>(m))));
-            if (lane == 16) lds.vmax[buf][wave] = __uint_as_float(m);
+            const float vm = __uint_as_float(uniform(__float_as_uint(max_halves(max_rows16(__uint_as_float(m))))));
+            v_fall = 1.0f;
+            if (vm > kVGrow * vref) {
+                const float next = fmaxf(vm, FLT_MIN);
+                v_fall = vref / next;
+                vref = next;
+                vinv = 1.0f / next;
+            }
+            if (wave == 0) *((LdsFloat*)lds_ks[buf] + lane) = k_scale * a.c2;
+            if (wave == 1) *((LdsFloat*)lds_vs[buf] + lane) = v_scale * vinv;
         }
-        const int f = (__ballot(bad) != 0 ? 1 : 0) | no_page;
-        if (lane == 0) lds.flags[buf][wave] = f;
     };
 
     f16v o[DB] = {};
-    float m = 0.0f, l = 0.0f;   // the reference (in powers of two), and this lane's part of the sum
-    bool any = false;           // the reference has been set
-    float vref = 0.0f, vinv = 0.0f;  // kCodes: o is the sum over vref
-    int step = p.first;
-    if (step < end) {
-        fetch(step);
-        store(step, 0);
-    }
-    for (int buf = 0; step < end; ++step, buf ^= 1) {
-        __syncthreads();  // this step's keys are there; the other buffer's readers are done
-        if (step + 1 < end) fetch(step + 1);
+    // the reference (in powers of two; none before a score), and this lane's part of the sum
+    float m = -INFINITY, l = 0.0f;
+    // where the lane reads: row col of the keys, its chunks 2 t + h; rows 4 h + (lane & 15) / 4 of the
+    // values, 8 bytes of their chunks 4 d ..
+    const int k_at = col * L::CU * 16, k_key = (h ^ L::key_k(col)) << 4;
+    const int v_row = 4 * h + ((lane & 15) >> 2);
+    const int v_at = v_row * L::CU * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8, v_key = L::key_v(v_row) << 4;
+
+    // The reference is set 2^kAbove above the largest score and stays until one passes it: bfloat16 keeps
+    // every probability's bits; in float16 those below 2^-14 of the reference lose some.
+    constexpr float kAbove = T == CHAM_T_F16 ? 3.0f : 7.0f;
+
+    // One step's keys against the wavefront's rows; masked: some row does not see all of them.  The
+    // outputs' sums are touched in three places only, whatever branch made the probabilities, so that they
+    // stay in their registers.
+    const auto compute = [&](bool masked, bool bad, int step, int buf, const Lds* keys, const Lds* vals) __attribute__((always_inline)) {
         const int key0 = step * kKeysTile;
-        if (live && key0 < lim_hi) {
-            f16v s[2] = {};
+        const Lds *kb = keys + k_at, *vb = vals + v_at;
+        // the scores of 32 keys; element i: key 32 b + 8 (i / 4) + 4 h + i % 4
+        f16v s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            s[b] = f16v{};
 #pragma unroll
             for (int t = 0; t < KS; ++t)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) s[b] = mma32<T>(lds.k[buf][32 * b + col][2 * t + h], q[t], s[b]);
-            // element i of block b: key 32 b + 8 (i / 4) + 4 h + i % 4
+                s[b] = mma32<T>(*(const LdsU4*)(kb + 32 * b * L::CU * 16 + ((t << 5) ^ k_key)), q[t], s[b]);
             if constexpr (SRC == kCodes) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int i = 0; i < 16; i += 4) {
+                    const f4 k4 = *((const LdsF4*)lds_ks[buf] + 8 * b + i / 2 + h);
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const f4 k4 = *(const f4*)&lds.ks[buf][32 * b + 2 * i + 4 * h];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) s[b][i + j] *= k4[j];
-                    }
-            }
-            int flags = 0;
-            {
-                const u4 f = *(const u4*)lds.flags[buf];
-                flags = __builtin_amdgcn_readfirstlane(f[0] | f[1] << 2 | f[2] << 4 | f[3] << 6);
-            }
-            const auto seen = [&](int b, int i) {
-                return key0 + 32 * b + 2 * (i & ~3) + 4 * h + (i & 3) < lim && !(flags >> (4 * b + (i >> 3) * 2 + 1) & 1);
-            };
-            const bool masked = key0 + kKeysTile > lim_lo || (flags & 0xaa);
-            if (masked) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!seen(b, i)) s[b][i] = -INFINITY;
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-            top *= a.c2;
-            if (__any(top > m + kGrow || (!any && top > -INFINITY))) {
-                top = max_halves(top);
-                if (top > -INFINITY && (!any || top > m)) {
-                    const float f = any ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
-                    m = top;
-                    any = true;
-                    l *= f;
-#pragma unroll
-                    for (int d = 0; d < DB; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[d][i] *= f;
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.c2, -m));
-                    l += s[b][i];
-                }
-            if constexpr (SRC == kCodes) {
-                const f4 v4 = *(const f4*)lds.vmax[buf];
-                const float vm = fmaxf(fmaxf(v4[0], v4[1]), fmaxf(v4[2], v4[3]));
-                if (vm > kVGrow * vref) {
-                    const float f = vref / fmaxf(vm, FLT_MIN);
-                    vref = fmaxf(vm, FLT_MIN);
-                    vinv = 1.0f / vref;
-#pragma unroll
-                    for (int d = 0; d < DB; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[d][i] *= f;
-                }
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const f4 k4 = *(const f4*)&lds.vs[buf][32 * b + 2 * i + 4 * h];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) s[b][i + j] *= k4[j] * vinv;
-                    }
-                if (masked) {
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (!seen(b, i)) s[b][i] = 0.0f;
-                }
-            }
-            u4 pr[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) pr[t][j] = narrow<T>(s[t >> 1][8 * (t & 1) + 2 * j], s[t >> 1][8 * (t & 1) + 2 * j + 1]);
-            // values of the lane's column of block d, keys as its probabilities lie
-            const int vr = 4 * h + ((lane & 15) >> 2), vc = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-            const auto values = [&](int t, int d) {
-                const char* at = (const char*)&lds.v[buf][16 * t + vr][4 * d] + vc;
-                const uint2 lo = read_tr(at), hi = read_tr(at + 8 * L::SV * 16);
-                return u4{lo.x, lo.y, hi.x, hi.y};
-            };
-            if (!(masked && (flags & 0x55))) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) o[d] = mma32<T>(values(t, d), pr[t], o[d]);
-            } else {
-                // A value that is not finite lies among keys that some rows do not see, and 0 times
-                // it would be NaN there.  Such values count as 0, and then as infinities of either
-                // sign (NaN as both) for the rows that see them: how many is a product with 0 and 1.
-                constexpr uint32_t inf = T == CHAM_T_F16 ? 0x7c00u : 0x7f80u, one = T == CHAM_T_F16 ? 0x3c00u : 0x3f80u;
-#pragma unroll 1
-                for (int t = 0; t < 4; ++t) {
-                    u4 vis, pt;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        if (u == t) {
-                            pt = pr[u];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                vis[j] = (seen(u >> 1, 8 * (u & 1) + 2 * j) ? one : 0) | (seen(u >> 1, 8 * (u & 1) + 2 * j + 1) ? one << 16 : 0);
-                        }
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        const u4 v = values(t, d);
-                        u4 fin, up, down;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            fin[j] = up[j] = down[j] = 0;
-#pragma unroll
-                            for (int e = 0; e < 32; e += 16) {
-                                const uint32_t x = (v[j] >> e) & 0xffffu, mag = x & 0x7fffu;
-                                if (mag < inf) fin[j] |= x << e;
-                                if (mag > inf || x == inf) up[j] |= one << e;
-                                if (mag > inf || x == (inf | 0x8000u)) down[j] |= one << e;
-                            }
-                        }
-                        o[d] = mma32<T>(fin, pt, o[d]);
-                        const f16v zero = {}, nu = mma32<T>(up, vis, zero), nd = mma32<T>(down, vis, zero);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            if (nu[i] > 0.0f) o[d][i] += INFINITY;
-                            if (nd[i] > 0.0f) o[d][i] -= INFINITY;
-                        }
-                    }
+                    for (int j = 0; j < 4; ++j) s[b][i + j] *= k4[j];
                 }
             }
         }
-        if (step + 1 < end) store(step + 1, buf ^ 1);
+        const int rel = lim - key0 - 4 * h;
+        const auto seen = [&](int b, int i) {
+            return 32 * b + 2 * (i & ~3) + (i & 3) < rel && !(no_page >> (2 * b + (i >> 3)) & 1);
+        };
+        if (masked) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!seen(b, i)) s[b][i] = -INFINITY;
+        }
+        // their probabilities over the reference; all sums are of the rounded ones but where they still take
+        // a scale.  The result's bits 14 and 30 are set where one is 2 or more, or NaN.
+        u4 pr[4];
+        const auto weigh = [&](float ref, float& sum) __attribute__((always_inline)) {
+            uint32_t big = 0;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    float e[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        e[j] = __builtin_amdgcn_exp2f(SRC == kCodes ? s[b][i + j] - ref : __builtin_fmaf(s[b][i + j], a.c2, -ref));
+                    if constexpr (SRC == kCodes) {
+                        const f4 v4 = *((const LdsF4*)lds_vs[buf] + 8 * b + i / 2 + h);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            big |= __float_as_uint(e[j]);
+                            sum += e[j];
+                            e[j] *= v4[j];
+                        }
+                    }
+                    const uint32_t lo = narrow<T>(e[0], e[1]), hi = narrow<T>(e[2], e[3]);
+                    pr[2 * b + i / 8][i % 8 / 2] = lo;
+                    pr[2 * b + i / 8][i % 8 / 2 + 1] = hi;
+                    if constexpr (SRC != kCodes) {
+                        big |= lo | hi;
+                        sum = add2<T>(hi, add2<T>(lo, sum));
+                    }
+                }
+            return big;
+        };
+        float sum = l, f = 1.0f;
+        int moved = 0;
+        if (__builtin_expect(__any((weigh(m, sum) & (SRC == kCodes ? 0x40000000u : 0x40004000u)) != 0), 0)) {
+            // the reference follows the largest score, where that has passed it, and the probabilities with it
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
+            if constexpr (SRC != kCodes) top *= a.c2;
+            top = max_halves(top);
+            if (top > m) {
+                f = __builtin_amdgcn_exp2f(m - (top + kAbove));
+                m = top + kAbove;
+            }
+            sum = l * f;
+            weigh(m == -INFINITY ? 0.0f : m, sum);
+            moved = 1;
+        }
+        l = sum;
+        if constexpr (SRC == kCodes) {
+            moved |= uniform(v_fall != 1.0f);
+            f *= v_fall;
+            if (masked) {  // a scale that is not finite
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        pr[t][j] &= (seen(t >> 1, 8 * (t & 1) + 2 * j) ? 0xffffu : 0) | (seen(t >> 1, 8 * (t & 1) + 2 * j + 1) ? 0xffff0000u : 0);
+            }
+        }
+        moved = uniform(moved);
+        asm volatile("" : "+s"(moved));  // a branch of its own
+        if (__builtin_expect(moved, 0)) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        // values of the lane's column of block d, keys as its probabilities lie
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const Lds* at = vb + 16 * t * L::CU * 16 + ((64 * d) ^ v_key);
+                const uint2 lo = read_tr(at), hi = read_tr(at + 8 * L::CU * 16);
+                o[d] = mma32<T>(u4{lo.x, lo.y, hi.x, hi.y}, pr[t], o[d]);
+            }
+        if (__builtin_expect(bad, 0)) {
+            // Values that are not finite: each row adds those that it sees, from memory (see `clean`).
+            constexpr uint32_t inf = T == CHAM_T_F16 ? 0x7c00u : 0x7f80u;
+#pragma unroll 1
+            for (int key = key0; key < min(key0 + kKeysTile, p.nk); ++key) {
+                const bool see = key < lim && !(no_page >> ((key - key0) >> 4) & 1);
+                const char* row;
+                if constexpr (SRC == kPacked) {
+                    row = (const char*)a.v.p + ((int64_t)(p.k0 + key) * a.v.token + (int64_t)hk * a.v.head) * 2;
+                } else {
+                    if (no_page >> ((key - key0) >> 4) & 1) continue;
+                    const int page = a.table[(int64_t)p.seq * a.width + (key >> a.shift)];
+                    const int64_t at = (((int64_t)page * a.Hk + hk) << a.shift) + (key & ((1 << a.shift) - 1));
+                    row = (const char*)a.c.v + at * ldv;
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const int e = 32 * d + 2 * i + 4 * h;
+                        uint2 w = make_uint2(0, 0);
+                        if (e < D) {
+                            if constexpr (SRC == kCodes) {
+                                const uint32_t c = *(const uint32_t*)(row + e);
+                                w = make_uint2(widen2<T, false>(c), widen2<T, true>(c));
+                            } else {
+                                w = *(const uint2*)(row + 2 * e);
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t x = (j < 2 ? w.x : w.y) >> (16 * (j & 1)) & 0xffffu;
+                            // an infinity or a NaN, widened: the exponent is all ones in either type
+                            const uint32_t w32 = (x & 0x8000u) << 16 | 0x7f800000u | ((x & 0x7fffu) > inf ? 0x400000u : 0);
+                            o[d][i + j] += see && (x & 0x7fffu) >= inf ? __uint_as_float(w32) : 0.0f;
+                        }
+                    }
+            }
+        }
+    };
+
+    // Values that are not finite among keys that some of the tile's rows do not see, though they exist: 0
+    // times such a value would be NaN in those rows.  They are taken out of LDS (each wavefront its own 16
+    // keys'), and added apart; the result: whether there are any.
+    const auto clean = [&](Lds* vals) __attribute__((always_inline)) {
+        constexpr uint32_t carry = T == CHAM_T_F16 ? 0x04000400u : 0x00800080u;  // an exponent of ones overflows
+        bool found = false;
+#pragma unroll 1
+        for (int i = 0; i < L::CU / 4; ++i) {
+            LdsU4* at = (LdsU4*)(vals + wave * 16 * L::CU * 16) + lane + kWave * i;
+            u4 w = *at;
+            uint32_t all = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t c = ((w[j] & 0x7fff7fffu) + carry) & 0x80008000u;
+                all |= c;
+                w[j] &= ~((c >> 15) * 0xffffu);
+            }
+            if (all) *at = w;
+            found |= all != 0;
+        }
+        return uniform(__syncthreads_or(found)) != 0;
+    };
+
+    const int lim_first = uniform(limit(row0));
+    int step = p.first;
+    const auto turn = [&](int buf, Lds* kb, Lds* vb, Lds* next_k, Lds* next_v) __attribute__((always_inline)) {
+        __syncthreads();  // this step's keys are there; the other buffer's readers are done
+        no_page = no_page_next;
+        const int key0 = step * kKeysTile;
+        bool bad = false;
+        if (lim_first < min(key0 + kKeysTile, p.nk)) bad = clean(vb);
+        if (step + 1 < end) fetch(step + 1, next_k, next_v);
+        if (live && key0 < lim_hi) compute(key0 + kKeysTile > lim_lo || no_page, bad, step, buf, kb, vb);
+        if (step + 1 < end) store(buf ^ 1, next_k, next_v);
+        ++step;
+    };
+    if (step < end) {
+        if constexpr (SRC != kPacked) pages = page_of(step);
+        fetch(step, (Lds*)k0, (Lds*)v0);
+        store(0, (Lds*)k0, (Lds*)v0);
+    }
+    while (step < end) {
+        turn(0, (Lds*)k0, (Lds*)v0, (Lds*)k1, (Lds*)v1);
+        if (step < end) turn(1, (Lds*)k1, (Lds*)v1, (Lds*)k0, (Lds*)v0);
     }
 
     if (!live || my_row >= rows || (p.pieces > 1 && (unsigned)p.index >= (unsigned)a.most)) return;
     l = add_halves(l);
     const float f = l == 0.0f ? 0.0f : (SRC == kCodes ? vref : 1.0f) / l;
+    m = m == -INFINITY ? 0.0f : m;
     const int64_t o_at = (int64_t)(p.q0 + token) * a.a.o.token + (int64_t)head * a.a.o.head;
     float* po = a.part_o + ((int64_t)p.index * kRowsTile + wave * 32 + col) * D;
 #pragma unroll
@@ -710,7 +815,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(const AttnArgs a) {
         }
         // values of column 16 d + (lane & 15): keys 4 g .. + 3 and 16 + 4 g .. + 3
         __builtin_amdgcn_wave_barrier();
-        const char* at = (const char*)&vl[4 * g + (col >> 2)][0] + (col & 3) * 8;
+        const Lds* at = (const Lds*)&vl[4 * g + (col >> 2)][0] + (col & 3) * 8;
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
             const uint2 lo = read_tr(at + 32 * d), hi = read_tr(at + 32 * d + 16 * L::SV * 16);
