@@ -28,7 +28,6 @@ namespace {
 enum { kPacked, kPages, kCodes };  // where keys and values come from: rows, 16-bit pages, E4M3 pages
 
 constexpr float kLog2e = 1.44269504f;
-constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100, kTrans = 0x400;  // sched_group_barrier's classes
 constexpr float kGrow = 8.0f;    // few_kernel: the reference follows scores more than 2^8 above it
 constexpr float kVGrow = 16.0f;  // and the values' scale follows scales more than 16 times it
 
@@ -45,7 +44,9 @@ struct AttnArgs {
     int G, Hk;
     int shift;            // log2 of the page
     float c2;             // scale log2(e)
-    int slots;            // pieces the whole work is cut into
+    uint32_t group_mul;   // division by G, see by_group
+    int group_shift;
+    float share;          // key heads over the pieces that the whole work is cut into
     int least;            // steps of keys a piece has at least
     int most;             // pieces the workspace holds
     float* part_o;        // [piece][rows][D] outputs of pieces
@@ -92,66 +93,106 @@ CHAM_DEV Seq sequence(const AttnArgs& a, int b) {
     return s;
 }
 
+CHAM_DEV float max_halves(float v) {  // over lanes l and l ^ 32
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+CHAM_DEV float add_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+CHAM_DEV float max_rows16(float v) {  // over lanes l and l ^ 16
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+CHAM_DEV float add_rows16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // a value that all lanes share, in scalar registers
 CHAM_DEV int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-CHAM_DEV int64_t wave_add(int64_t v) {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor((long long)v, d);
-    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+// the sum of all lanes; in binary32, and the same bits in every lane
+CHAM_DEV float wave_total(float v) {
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    v += dpp<0x141>(v);
+    v += dpp<0x140>(v);
+    return add_halves(add_rows16(v));
 }
-CHAM_DEV int wave_scan(int v, int lane) {  // inclusive
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int o = __shfl_up(v, d);
-        v += lane >= d ? o : 0;
-    }
+CHAM_DEV int wave_scan(int v) {  // inclusive
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, true);  // row 0's last into row 1, 2's into 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, true);  // row 1's last into rows 2 and 3
     return v;
 }
 
+// n / G for n < 2^31: with M = ceil(2^(31 + l) / G), 2^(l-1) < G <= 2^l, the error M G - 2^(31 + l) < 2^l
+CHAM_DEV int by_group(const AttnArgs& a, int n) { return (int)((uint64_t)(uint32_t)n * a.group_mul >> a.group_shift); }
+
 // Piece `at` of key head `hk` (every wavefront works it out for itself); false past the last one.
-// With tiles: `at` counts row tiles, and the piece is the tile's first.
-template <int SRC, int BM, int BN>
+// With tiles: `at` counts row tiles, and the piece is the tile's first.  SORT: sequences come in the order
+// of their keys, the longest first, where there are at most 64: what starts last is short.
+template <int SRC, int BM, int BN, bool SORT>
 CHAM_DEV bool find_piece(const AttnArgs& a, int at, int hk, bool tiles, Piece* p) {
     const int lane = threadIdx.x % kWave, B = (int)a.a.B;
-    int64_t work = 0;
+    float work = 0.0f;
+    Seq s{};
+    int nt = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
-        if (b0 + lane < B) {
-            const Seq s = sequence<SRC>(a, b0 + lane);
-            work += (int64_t)((s.nq * a.G + BM - 1) / BM) * ((s.nk + BN - 1) / BN);
-        }
-    }
-    work = wave_add(work) * a.Hk;
-    const int steps = (int)max((work + a.slots - 1) / a.slots, (int64_t)a.least);
-    int before = 0, split_before = 0;
-    for (int b0 = 0; b0 < B; b0 += kWave) {
-        Seq s{};
-        int nt = 0, n = 0;
         if (b0 + lane < B) {
             s = sequence<SRC>(a, b0 + lane);
             nt = (s.nq * a.G + BM - 1) / BM;
-            n = max(1, ((s.nk + BN - 1) / BN + steps - 1) / steps);
+            work += (float)nt * (float)((s.nk + BN - 1) / BN);
         }
+    }
+    // more than its share of all steps, however the sum is rounded
+    const int steps = max(uniform((int)fminf(wave_total(work) * a.share, 1e9f)) + 1, a.least);
+    int before = 0, split_before = 0;
+    for (int b0 = 0; b0 < B; b0 += kWave) {
+        int n = 0;
+        if (B > kWave) {
+            nt = 0;
+            if (b0 + lane < B) {
+                s = sequence<SRC>(a, b0 + lane);
+                nt = (s.nq * a.G + BM - 1) / BM;
+            }
+        }
+        if (b0 + lane < B) n = max(1, (int)(((uint32_t)((s.nk + BN - 1) / BN) + (uint32_t)steps - 1) / (uint32_t)steps));
         const int mine = tiles ? nt : nt * n, split = n > 1 ? nt * n : 0;
-        const int upto = wave_scan(mine, lane), split_upto = wave_scan(split, lane);
-        const uint64_t past = __ballot(before + upto > at);
-        if (past == 0) {
+        int first = 0, split_first = 0;
+        if (SORT && B <= kWave) {
+            for (int j = 0; j < B; ++j) {
+                const int other = __builtin_amdgcn_readlane(s.nk, j);
+                const bool ahead = other > s.nk || (other == s.nk && j < lane);
+                first += ahead ? __builtin_amdgcn_readlane(mine, j) : 0;
+                split_first += ahead ? __builtin_amdgcn_readlane(split, j) : 0;
+            }
+        } else {
+            const int upto = wave_scan(mine), split_upto = wave_scan(split);
+            first = before + upto - mine;
+            split_first = split_before + split_upto - split;
             before += __builtin_amdgcn_readlane(upto, kWave - 1);
             split_before += __builtin_amdgcn_readlane(split_upto, kWave - 1);
-            continue;
         }
-        const int l = __builtin_ctzll(past);
+        const uint64_t here = __ballot(first <= at && at < first + mine);
+        if (here == 0) continue;
+        const int l = __builtin_ctzll(here);
         const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
         p->seq = b0 + l;
         p->q0 = of(s.q0), p->nq = of(s.nq), p->k0 = of(s.k0), p->nk = of(s.nk);
         p->pieces = of(n);
-        const int in = at - before - (of(upto) - of(mine));  // within the sequence
-        const int tile = tiles ? in : in / p->pieces, piece = tiles ? 0 : in - tile * p->pieces;
+        const int in = at - of(first);  // within the sequence
+        const int tile = tiles ? in : (int)((uint32_t)in / (uint32_t)p->pieces), piece = tiles ? 0 : in - tile * p->pieces;
         // the last rows of a causal sequence see the most keys: they come first
         p->tile = of(nt) - 1 - tile;
-        const int blocks = (p->nk + BN - 1) / BN, per = (blocks + p->pieces - 1) / p->pieces;
+        const int blocks = (p->nk + BN - 1) / BN, per = (int)(((uint32_t)blocks + p->pieces - 1) / (uint32_t)p->pieces);
         p->first = piece * per;
         p->end = min(blocks, p->first + per);
-        p->index = (split_before + of(split_upto) - of(split) + tile * p->pieces + piece) * a.Hk + hk;
+        p->index = (of(split_first) + tile * p->pieces + piece) * a.Hk + hk;
         return true;
     }
     return false;
@@ -215,23 +256,6 @@ CHAM_DEV u4 load16(const char* p) { return *(const u4*)p; }
 typedef __attribute__((address_space(3))) uint8_t Lds;
 CHAM_DEV uint2 read_tr(const Lds* p) { return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)p)); }
 
-CHAM_DEV float max_halves(float v) {  // over lanes l and l ^ 32
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-CHAM_DEV float add_halves(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-CHAM_DEV float max_rows16(float v) {  // over lanes l and l ^ 16
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-CHAM_DEV float add_rows16(float v) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 template <int T>
 CHAM_DEV void put4(const cham_heads& o, int64_t at, float a, float b, float c, float d) {
     *(uint2*)((char*)o.p + at * 2) = make_uint2(narrow<T>(a, b), narrow<T>(c, d));
@@ -276,13 +300,13 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     __shared__ __align__(16) float lds_ks[2][kKeysTile], lds_vs[2][kKeysTile];  // kCodes: scales
     const int hk = blockIdx.x % a.Hk;
     Piece p;
-    if (!find_piece<SRC, kRowsTile, kKeysTile>(a, blockIdx.x / a.Hk, hk, false, &p)) return;
+    if (!find_piece<SRC, kRowsTile, kKeysTile, true>(a, blockIdx.x / a.Hk, hk, false, &p)) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane & 31, h = lane >> 5, D = a.a.D;
     const int rows = p.nq * a.G, row0 = p.tile * kRowsTile;
     const bool causal = SRC != kPacked || a.a.causal;
     // keys that a row sees: the first `lim`
-    const auto limit = [&](int row) { return causal ? min(max(p.nk - p.nq + row / a.G + 1, 0), p.nk) : p.nk; };
+    const auto limit = [&](int row) { return causal ? min(max(p.nk - p.nq + by_group(a, row) + 1, 0), p.nk) : p.nk; };
     const int my_row = row0 + wave * 32 + col;
     const bool live = row0 + wave * 32 < rows;
     const int lim = my_row < rows ? limit(my_row) : 0;
@@ -294,7 +318,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
 
     // the queries: second operand of the scores' products
     u4 q[KS];
-    const int token = my_row / a.G, head = hk * a.G + my_row - token * a.G;
+    const int token = by_group(a, my_row), head = hk * a.G + my_row - token * a.G;
     const int64_t q_at = (int64_t)(p.q0 + token) * a.a.q.token + (int64_t)head * a.a.q.head;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -332,21 +356,38 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     float k_scale = 0.0f, v_scale = 0.0f;
     int pages = -1;
     uint32_t no_page = 0, no_page_next = 0;  // which 16 keys of the step have none
-    const auto fetch = [&](int step, Lds* kb, Lds* vb) __attribute__((always_inline)) {
-        const int key0 = step * kKeysTile + 16 * wave;
-        const char *kp, *vp;
-        int left = min(max(p.nk - key0, 0), 16);
+    // What the next step's loads need, kept short: its first key for this wavefront, and the rows' place
+    // (kPacked: the place itself, which moves with the steps; pages: that of page 0's first token).
+    const int row_bytes = D * (SRC == kCodes ? 1 : 2);
+    int key_at = p.first * kKeysTile + 16 * wave;
+    const char* kp = SRC == kPacked ? (const char*)a.k.p + ((int64_t)(p.k0 + key_at) * a.k.token + (int64_t)hk * a.k.head) * 2
+                                    : (const char*)a.c.k + ((int64_t)hk << a.shift) * row_bytes;
+    const char* vp = SRC == kPacked ? (const char*)a.v.p + ((int64_t)(p.k0 + key_at) * a.v.token + (int64_t)hk * a.v.head) * 2
+                                    : (const char*)a.c.v + ((int64_t)hk << a.shift) * row_bytes;
+    const uint32_t page_bytes = SRC == kPacked ? 0 : (uint32_t)row_bytes << a.shift;  // of one head: below 2^24
+    const int full_k = 15 * ldk + row_bytes, full_v = 15 * ldv + row_bytes;
+    __amdgpu_buffer_rsrc_t from_k, from_v;
+    const auto fetch = [&](int step) __attribute__((always_inline)) {
+        const char *k_from = kp, *v_from = vp;
+        int size_k = full_k, size_v = full_v;
+        if (step >= end) {  // the loads behind the last step bring nothing
+            size_k = size_v = 0;
+        } else if (key_at + 16 > p.nk) {  // row r < left lies wholly before `size`, row `left` behind it
+            const int left = p.nk - key_at;
+            size_k = left > 0 ? (left - 1) * ldk + row_bytes : 0;
+            size_v = left > 0 ? (left - 1) * ldv + row_bytes : 0;
+        }
         if constexpr (SRC == kPacked) {
-            kp = (const char*)a.k.p + ((int64_t)(p.k0 + key0) * a.k.token + (int64_t)hk * a.k.head) * 2;
-            vp = (const char*)a.v.p + ((int64_t)(p.k0 + key0) * a.v.token + (int64_t)hk * a.v.head) * 2;
+            kp += (int64_t)kKeysTile * ldk;
+            vp += (int64_t)kKeysTile * ldv;
         } else {
-            const int page = __builtin_amdgcn_readlane(pages, 16 * wave);
+            const int page = __builtin_amdgcn_readlane(pages, 16 * wave), in_page = key_at & ((1 << a.shift) - 1);
             const uint64_t none = __ballot(pages < 0 && step * kKeysTile + lane < p.nk);
             no_page_next = (none & 1) | (none >> 15 & 2) | (none >> 30 & 4) | (none >> 45 & 8);
-            if (page < 0) left = 0;
-            const int64_t at = (((int64_t)max(page, 0) * a.Hk + hk) << a.shift) + (key0 & ((1 << a.shift) - 1));
-            kp = (const char*)a.c.k + at * ldk;
-            vp = (const char*)a.c.v + at * ldv;
+            if (page < 0) size_k = size_v = 0;
+            const uint64_t at = (uint64_t)(uint32_t)max(page, 0) * a.Hk * page_bytes + (uint32_t)(in_page * row_bytes);
+            k_from += at;
+            v_from += at;
             if constexpr (SRC == kCodes) {
                 const int key = step * kKeysTile + lane;
                 const int64_t row = (((int64_t)pages * a.Hk + hk) << a.shift) + (key & ((1 << a.shift) - 1));
@@ -358,21 +399,23 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
             }
             pages = page_of(step + 1);
         }
-        // row r < left lies wholly before `size`, row `left` behind it
-        const int row_bytes = D * (SRC == kCodes ? 1 : 2);
-        const auto size = [&](int ld) { return left > 0 ? (left - 1) * ld + row_bytes : 0; };
-        const __amdgpu_buffer_rsrc_t bk = __builtin_amdgcn_make_buffer_rsrc((void*)kp, (short)0, size(ldk), kBufferFlags);
-        const __amdgpu_buffer_rsrc_t bv = __builtin_amdgcn_make_buffer_rsrc((void*)vp, (short)0, size(ldv), kBufferFlags);
+        key_at += kKeysTile;
+        from_k = __builtin_amdgcn_make_buffer_rsrc((void*)k_from, (short)0, size_k, kBufferFlags);
+        from_v = __builtin_amdgcn_make_buffer_rsrc((void*)v_from, (short)0, size_v, kBufferFlags);
+    };
+    const auto load_k = [&](int i, Lds* kb) __attribute__((always_inline)) {
+        if constexpr (SRC == kCodes) rk[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(from_k, off_k[i], 0, 0));
+        else load_lds(from_k, kb + (wave * L::kLoads + i) * 1024, off_k[i]);
+    };
+    const auto load_v = [&](int i, Lds* vb) __attribute__((always_inline)) {
+        if constexpr (SRC == kCodes) rv[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(from_v, off_v[i], 0, 0));
+        else load_lds(from_v, vb + (wave * L::kLoads + i) * 1024, off_v[i]);
+    };
+    const auto load_all = [&](Lds* kb, Lds* vb) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            if constexpr (SRC == kCodes) {
-                rk[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(bk, off_k[i], 0, 0));
-                rv[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(bv, off_v[i], 0, 0));
-            } else {
-                const int to = (wave * L::kLoads + i) * 1024;
-                load_lds(bk, kb + to, off_k[i]);
-                load_lds(bv, vb + to, off_v[i]);
-            }
+            load_k(i, kb);
+            load_v(i, vb);
         }
     };
     // kCodes: o is the sum over vref, and vs hold the values' scales over it.  All wavefronts see all
@@ -416,24 +459,29 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     const int v_row = 4 * h + ((lane & 15) >> 2);
     const int v_at = v_row * L::CU * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8, v_key = L::key_v(v_row) << 4;
 
-    // The reference is set 2^kAbove above the largest score and stays until one passes it: bfloat16 keeps
-    // every probability's bits; in float16 those below 2^-14 of the reference lose some.
-    constexpr float kAbove = T == CHAM_T_F16 ? 3.0f : 7.0f;
+    // The reference is set kAbove powers of two above the largest score and stays until one passes it.  float16
+    // holds a probability's 11 bits down to 2^-14 of the reference; binary32 sums of bfloat16 ones and values
+    // keep theirs for values down to 2^-78.  Scores that spread over 2^30 (heads of 4096 x 4096 with a standard
+    // deviation of 5 nats) move a reference 2^7 above every few steps: 119 us instead of 91.
+    constexpr float kAbove = T == CHAM_T_F16 ? 6.0f : 24.0f;
 
     // One step's keys against the wavefront's rows; masked: some row does not see all of them.  The
     // outputs' sums are touched in three places only, whatever branch made the probabilities, so that they
     // stay in their registers.
-    const auto compute = [&](bool masked, bool bad, int step, int buf, const Lds* keys, const Lds* vals) __attribute__((always_inline)) {
+    const auto compute = [&](bool masked, bool bad, int step, int buf, const Lds* keys, const Lds* vals, Lds* next_k, Lds* next_v) __attribute__((always_inline)) {
         const int key0 = step * kKeysTile;
         const Lds *kb = keys + k_at, *vb = vals + v_at;
         // the scores of 32 keys; element i: key 32 b + 8 (i / 4) + 4 h + i % 4
         f16v s[2];
+        const auto score = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             s[b] = f16v{};
 #pragma unroll
-            for (int t = 0; t < KS; ++t)
+            for (int t = 0; t < KS; ++t) {
                 s[b] = mma32<T>(*(const LdsU4*)(kb + 32 * b * L::CU * 16 + ((t << 5) ^ k_key)), q[t], s[b]);
+                if (b == 0 && t < kLoads) load_k(t, next_k);
+            }
             if constexpr (SRC == kCodes) {
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
@@ -443,17 +491,11 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                 }
             }
         }
+        };
         const int rel = lim - key0 - 4 * h;
         const auto seen = [&](int b, int i) {
             return 32 * b + 2 * (i & ~3) + (i & 3) < rel && !(no_page >> (2 * b + (i >> 3)) & 1);
         };
-        if (masked) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!seen(b, i)) s[b][i] = -INFINITY;
-        }
         // their probabilities over the reference; all sums are of the rounded ones but where they still take
         // a scale.  The result's bits 14 and 30 are set where one is 2 or more, or NaN.
         u4 pr[4];
@@ -481,14 +523,31 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                     pr[2 * b + i / 8][i % 8 / 2 + 1] = hi;
                     if constexpr (SRC != kCodes) {
                         big |= lo | hi;
-                        sum = add2<T>(hi, add2<T>(lo, sum));
+                        sum += (e[0] + e[1]) + (e[2] + e[3]);
                     }
                 }
             return big;
         };
         float sum = l, f = 1.0f;
         int moved = 0;
-        if (__builtin_expect(__any((weigh(m, sum) & (SRC == kCodes ? 0x40000000u : 0x40004000u)) != 0), 0)) {
+        uint32_t big;
+        if (masked) {
+            asm volatile("; some keys hidden");
+            score();
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!seen(b, i)) s[b][i] = -INFINITY;
+            big = weigh(m, sum);
+            asm volatile("; some keys hidden");
+        } else {
+            asm volatile("; all keys seen");
+            score();
+            big = weigh(m, sum);
+            asm volatile("; all keys seen");
+        }
+        if (__builtin_expect(__any((big & (SRC == kCodes ? 0x40000000u : 0x40004000u)) != 0), 0)) {
             // the reference follows the largest score, where that has passed it, and the probabilities with it
             float top = -INFINITY;
 #pragma unroll
@@ -525,13 +584,15 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         }
         // values of the lane's column of block d, keys as its probabilities lie
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
+            if (t < kLoads) load_v(t, next_v);
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 const Lds* at = vb + 16 * t * L::CU * 16 + ((64 * d) ^ v_key);
                 const uint2 lo = read_tr(at), hi = read_tr(at + 8 * L::CU * 16);
                 o[d] = mma32<T>(u4{lo.x, lo.y, hi.x, hi.y}, pr[t], o[d]);
             }
+        }
         if (__builtin_expect(bad, 0)) {
             // Values that are not finite: each row adds those that it sees, from memory (see `clean`).
             constexpr uint32_t inf = T == CHAM_T_F16 ? 0x7c00u : 0x7f80u;
@@ -604,20 +665,23 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         const int key0 = step * kKeysTile;
         bool bad = false;
         if (lim_first < min(key0 + kKeysTile, p.nk)) bad = clean(vb);
-        if (step + 1 < end) fetch(step + 1, next_k, next_v);
-        if (live && key0 < lim_hi) compute(key0 + kKeysTile > lim_lo || no_page, bad, step, buf, kb, vb);
+        fetch(step + 1);
+        if (live && key0 < lim_hi) compute(key0 + kKeysTile > lim_lo || no_page, bad, step, buf, kb, vb, next_k, next_v);
+        else load_all(next_k, next_v);
         if (step + 1 < end) store(buf ^ 1, next_k, next_v);
         ++step;
     };
     if (step < end) {
         if constexpr (SRC != kPacked) pages = page_of(step);
-        fetch(step, (Lds*)k0, (Lds*)v0);
+        fetch(step);
+        load_all((Lds*)k0, (Lds*)v0);
         store(0, (Lds*)k0, (Lds*)v0);
     }
     while (step < end) {
         turn(0, (Lds*)k0, (Lds*)v0, (Lds*)k1, (Lds*)v1);
         if (step < end) turn(1, (Lds*)k1, (Lds*)v1, (Lds*)k0, (Lds*)v0);
     }
+    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);  // vmcnt(0): no load is under way into LDS that another workgroup gets
 
     if (!live || my_row >= rows || (p.pieces > 1 && (unsigned)p.index >= (unsigned)a.most)) return;
     l = add_halves(l);
@@ -663,7 +727,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(const AttnArgs a) {
     __shared__ L lds;
     const int hk = blockIdx.x % a.Hk;
     Piece p;
-    if (!find_piece<SRC, kRowsFew, kKeysFew>(a, blockIdx.x / a.Hk, hk, false, &p)) return;
+    if (!find_piece<SRC, kRowsFew, kKeysFew, false>(a, blockIdx.x / a.Hk, hk, false, &p)) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane & 15, g = lane >> 4, D = a.a.D;
     const int rows = min(a.G - p.tile * kRowsFew, kRowsFew), head0 = hk * a.G + p.tile * kRowsFew;
@@ -865,35 +929,64 @@ __global__ __launch_bounds__(256, 2) void few_kernel(const AttnArgs a) {
 // ------------------------------------------------------------------------------------
 // joining the pieces of a row tile: o = sum_c w_c o_c / sum_c w_c, w_c = l_c 2^(m_c - max m)
 // ------------------------------------------------------------------------------------
+// A workgroup takes 8 rows, 32 lanes a row (4 elements a lane); where a tile has fewer, several groups of
+// lanes share a row's pieces and are added in their order.
+constexpr int kRowsJoin = 8;
 template <int T, int SRC, int BM, int BN>
 __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
+    __shared__ float4 sums[kRowsJoin][32];
+    __shared__ float2 stats[kRowsJoin];  // reference and total
     const int hk = blockIdx.x % a.Hk;
     Piece p;
-    if (!find_piece<SRC, BM, BN>(a, blockIdx.x / a.Hk, hk, true, &p) || p.pieces == 1) return;
+    if (!find_piece<SRC, BM, BN, BM == kRowsTile>(a, blockIdx.x / a.Hk, hk, true, &p) || p.pieces == 1) return;
     if ((unsigned)(p.index + (p.pieces - 1) * a.Hk) >= (unsigned)a.most) return;
-    const int D = a.a.D, rows = min(p.nq * a.G - p.tile * BM, BM);
-    for (int u = threadIdx.x; u < rows * (D / 4); u += 256) {
-        const int row = u / (D / 4), e = u % (D / 4) * 4;
-        float top = -INFINITY;
-        for (int c = 0; c < p.pieces; ++c) {
-            const float2 s = *(const float2*)(a.part_s + ((int64_t)(p.index + c * a.Hk) * BM + row) * 2);
-            if (s.y != 0.0f) top = fmaxf(top, s.x);
+    const int D = a.a.D, row0 = blockIdx.y * kRowsJoin, rows = min(min(p.nq * a.G - p.tile * BM, BM) - row0, kRowsJoin);
+    if (rows <= 0) return;
+    const int shift = rows > 4 ? 3 : rows > 2 ? 2 : rows > 1 ? 1 : 0;  // lane groups: 2^shift rows, the rest shares pieces
+    const int group = threadIdx.x / 32, e = threadIdx.x % 32 * 4, row = group & ((1 << shift) - 1), part = group >> shift;
+    const int parts = 8 >> shift;
+    const bool live = row < rows && e < D;
+    const int64_t at = (int64_t)p.index * BM + row0 + row, stride = (int64_t)a.Hk * BM;
+    float top = -INFINITY, total = 0.0f;
+    f4 sum = {};
+    if (live) {
+#pragma unroll 4
+        for (int c = part; c < p.pieces; c += parts) {
+            const float2 s = *(const float2*)(a.part_s + (at + c * stride) * 2);
+            top = s.y != 0.0f ? fmaxf(top, s.x) : top;
         }
-        f4 sum = {};
-        float total = 0.0f;
-        for (int c = 0; c < p.pieces; ++c) {
-            const int64_t r = (int64_t)(p.index + c * a.Hk) * BM + row;
-            const float2 s = *(const float2*)(a.part_s + r * 2);
-            if (s.y == 0.0f) continue;  // saw no key
-            const float w = s.y * __builtin_amdgcn_exp2f(s.x - top);
+#pragma unroll 4
+        for (int c = part; c < p.pieces; c += parts) {
+            const float2 s = *(const float2*)(a.part_s + (at + c * stride) * 2);
+            const f4 v = *(const f4*)(a.part_o + (at + c * stride) * D + e);
+            const float w = s.y == 0.0f ? 0.0f : s.y * __builtin_amdgcn_exp2f(s.x - top);  // 0: saw no key, its output is 0
             total += w;
-            sum += w * *(const f4*)(a.part_o + r * D + e);
+            sum += w * v;
         }
-        sum *= total == 0.0f ? 0.0f : 1.0f / total;
-        const int at = p.tile * BM + row, token = at / a.G;
-        put4<T>(a.a.o, (int64_t)(p.q0 + token) * a.a.o.token + (int64_t)(hk * a.G + at - token * a.G) * a.a.o.head + e, sum[0],
-                sum[1], sum[2], sum[3]);
     }
+    if (parts > 1) {  // a group's sums are over its own largest reference
+        sums[group][threadIdx.x % 32] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        if (threadIdx.x % 32 == 0) stats[group] = make_float2(top, total);
+        __syncthreads();
+        if (part > 0) return;
+        for (int c = 0; c < parts; ++c) top = fmaxf(top, stats[row + (c << shift)].x);
+        total = 0.0f;
+        sum = f4{};
+        for (int c = 0; c < parts; ++c) {
+            const int g = row + (c << shift);
+            const float2 s = stats[g];
+            const float4 v = sums[g][threadIdx.x % 32];
+            const float w = s.x == top || s.y != s.y ? 1.0f : __builtin_amdgcn_exp2f(s.x - top);
+            if (s.y == 0.0f) continue;
+            total += w * s.y;
+            sum += w * f4{v.x, v.y, v.z, v.w};
+        }
+    }
+    if (!live) return;
+    sum *= total == 0.0f ? 0.0f : 1.0f / total;
+    const int in = p.tile * BM + row0 + row, token = by_group(a, in);
+    put4<T>(a.a.o, (int64_t)(p.q0 + token) * a.a.o.token + (int64_t)(hk * a.G + in - token * a.G) * a.a.o.head + e, sum[0], sum[1],
+            sum[2], sum[3]);
 }
 
 // ------------------------------------------------------------------------------------
@@ -937,20 +1030,20 @@ int attn_check(const cham_attn* a, int32_t Hk) {
 // Grid of the pieces: every tile is a piece, and the cuts make at most `slots` more.
 template <int T, int SRC, int KS, int DB, int ND>
 int launch(AttnArgs& a, bool few, int64_t tiles, bool may_split, hipStream_t s) {
-    const int64_t all = tiles * a.Hk, grid = may_split ? all + a.slots : all;
-    if (!cham_launchable(grid, 256)) return CHAM_ESHAPE;
+    const int64_t all = tiles * a.Hk, grid = may_split ? all + slots_of(few) : all;
+    if (!cham_launchable(may_split ? std::max(grid, all * (few ? kRowsFew : kRowsTile) / kRowsJoin) : grid, 256)) return CHAM_ESHAPE;
     if constexpr (SRC != kPacked) {
         if (few) {
             hipLaunchKernelGGL((few_kernel<T, ND, SRC>), dim3((unsigned)grid), dim3(256), 0, s, a);
             CHAM_CHECK_LAUNCH();
-            if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsFew, kKeysFew>), dim3((unsigned)all), dim3(256), 0, s, a);
+            if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsFew, kKeysFew>), dim3((unsigned)all, kRowsFew / kRowsJoin), dim3(256), 0, s, a);
             CHAM_CHECK_LAUNCH();
             return CHAM_OK;
         }
     }
     hipLaunchKernelGGL((tile_kernel<T, KS, DB, SRC>), dim3((unsigned)grid), dim3(256), 0, s, a);
     CHAM_CHECK_LAUNCH();
-    if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsTile, kKeysTile>), dim3((unsigned)all), dim3(256), 0, s, a);
+    if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsTile, kKeysTile>), dim3((unsigned)all, kRowsTile / kRowsJoin), dim3(256), 0, s, a);
     CHAM_CHECK_LAUNCH();
     return CHAM_OK;
 }
@@ -976,7 +1069,11 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     a.G = a.a.q.H / a.Hk;
     a.nq = (int)(a.a.T / a.a.B);
     a.c2 = a.a.scale * kLog2e;
-    a.slots = slots_of(few);
+    a.share = (float)a.Hk / (float)slots_of(few) * 1.001f;
+    int l = 0;
+    while ((1 << l) < a.G) ++l;
+    a.group_shift = 31 + l;
+    a.group_mul = (uint32_t)((((uint64_t)1 << a.group_shift) + a.G - 1) / a.G);
     a.least = few ? 1 : 4;
     a.most = (int)sp.pieces;
     a.part_o = (float*)ws;
@@ -984,8 +1081,15 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     const int64_t tiles = a.a.cu_q ? a.a.T * a.G / BM + a.a.B : a.a.B * up((int64_t)a.nq * a.G, BM);
     const int64_t blocks = up(nk_most, BN);
     bool may_split = blocks > a.least;
+    // Tiles that fill the card are not cut: the long ones start first, and what a cut saves at the end is less
+    // than the partial outputs and the second launch cost (8101 tokens, 2056 tiles: 5 us with nothing to join).
+    // A cache's sequences may be far longer than others: theirs are cut up to four such fillings.
+    if (!few && a.a.T * a.G / BM * a.Hk >= (int64_t)slots_of(few) * (SRC == kPacked ? 1 : 4)) {
+        may_split = false;
+        a.least = INT32_MAX / 2;
+    }
     if (SRC == kPacked && !a.a.cu_q && !a.cu_k)  // every length is known here
-        may_split = may_split && blocks > up(tiles * blocks * a.Hk, a.slots);
+        may_split = may_split && blocks > up(tiles * blocks * a.Hk, slots_of(few));
     if (a.a.q.type == CHAM_T_F16) return launch_d<CHAM_T_F16, SRC>(a, few, tiles, may_split, s);
     return launch_d<CHAM_T_BF16, SRC>(a, few, tiles, may_split, s);
 }

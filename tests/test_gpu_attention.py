@@ -346,8 +346,8 @@ def _attended(q, k, v, scale, causal, seen=None, vstep=None):
     2 |ref|), the exponential by 2^-22.  p is rounded to 16 bits (and, with codes, takes the scale in two
     binary32 roundings), and so in the sum l, whose quotient then is off by as much again: (sum p (1 + d) v) /
     (sum p (1 + d)) lies within u sum p |v| + u |o| of o.  Below the type's normal range p is rounded by half a
-    subnormal step, in units of the reference, which lies up to 2^3 above the largest score in float16 (bfloat16:
-    2^7; with codes, in units of the largest scale: vstep), so against l >= 1 as here by 8 (128) of
+    subnormal step, in units of the reference, which lies up to 2^6 above the largest score in float16 (bfloat16:
+    2^24; with codes, in units of the largest scale: vstep), so against l >= 1 as here by 2^6 (2^24) of
     those.  Sums of n terms take n 2^-24."""
     nq, Hq, D = q.shape
     nk, Hk = k.shape[:2]
@@ -378,7 +378,7 @@ def _attended(q, k, v, scale, causal, seen=None, vstep=None):
         a = p @ vz.abs()
         vs = vz.abs() if vstep is None else vstep[:, j:j + 1].expand(-1, D) * (vz != 0)
         bound[:, h] = (p * off) @ vz.abs() + a * (u + 4 * U + nk * 2 * U) + o[:, h].abs() * ((p * off).sum(1, keepdim=True) + nk * U + 8 * U)
-        bound[:, h] += u * o[:, h].abs() + (8 if dt == torch.float16 else 128) * TINY[dt] * vs.sum(0, keepdim=True) / l
+        bound[:, h] += u * o[:, h].abs() + (2.0 ** 6 if dt == torch.float16 else 2.0 ** 24) * TINY[dt] * vs.sum(0, keepdim=True) / l
         bound[:, h] += TINY[dt] + u * (o[:, h].abs() + bound[:, h])
     return o, bound * 1.02 + 1e-40
 
