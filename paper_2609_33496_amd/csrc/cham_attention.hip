@@ -230,13 +230,6 @@ CHAM_DEV uint32_t widen2(uint32_t w) {
     if constexpr (T == CHAM_T_F16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
 }
-// c plus two 16-bit values
-template <int T>
-CHAM_DEV float add2(uint32_t w, float c) {
-    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-    if constexpr (T == CHAM_T_F16) return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, w), half2v{(_Float16)1, (_Float16)1}, c, false);
-    else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, w), bf2{(__bf16)1.0f, (__bf16)1.0f}, c, false);
-}
 template <int T>
 CHAM_DEV u4 widen8(uint32_t lo, uint32_t hi) {
     return u4{widen2<T, false>(lo), widen2<T, true>(lo), widen2<T, false>(hi), widen2<T, true>(hi)};
@@ -345,16 +338,15 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
             off_v[i] = 8 * cv < D ? (uint32_t)(row * ldv + cv * 16) : kOutside;
         }
     }
-    // pages of the next step's keys (one a lane), a step ahead of their use; -1: none
-    const auto page_of = [&](int step) {
-        const int key = step * kKeysTile + lane;
-        int page = -1;
-        if (key < p.nk) page = a.table[(int64_t)p.seq * a.width + (key >> a.shift)];
-        return page >= 0 && page < a.c.pages ? page : -1;
-    };
+    // pages of the next step's keys (one a lane), a step ahead of their use.  No branch guards this load or
+    // the scales' (what lies behind the last key is read from the last one's place): at a branch's end the
+    // compiler would wait for them.
+    const int32_t* table = SRC == kPacked ? nullptr : a.table + (int64_t)p.seq * a.width;
+    const auto page_of = [&](int step) { return table[min(step * kKeysTile + lane, p.nk - 1) >> a.shift]; };
     u4 rk[SRC == kCodes ? kLoads : 1], rv[SRC == kCodes ? kLoads : 1];
     float k_scale = 0.0f, v_scale = 0.0f;
     int pages = -1;
+    bool held = false;  // the lane's key of the step that is brought has a place
     uint32_t no_page = 0, no_page_next = 0;  // which 16 keys of the step have none
     // What the next step's loads need, kept short: its first key for this wavefront, and the rows' place
     // (kPacked: the place itself, which moves with the steps; pages: that of page 0's first token).
@@ -381,21 +373,20 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
             kp += (int64_t)kKeysTile * ldk;
             vp += (int64_t)kKeysTile * ldv;
         } else {
-            const int page = __builtin_amdgcn_readlane(pages, 16 * wave), in_page = key_at & ((1 << a.shift) - 1);
-            const uint64_t none = __ballot(pages < 0 && step * kKeysTile + lane < p.nk);
+            const int key = step * kKeysTile + lane, in_page = key_at & ((1 << a.shift) - 1);
+            const bool there = (uint32_t)pages < (uint32_t)a.c.pages;
+            held = there && key < p.nk;
+            const uint64_t none = __ballot(!there && key < p.nk);
             no_page_next = (none & 1) | (none >> 15 & 2) | (none >> 30 & 4) | (none >> 45 & 8);
+            const int page = __builtin_amdgcn_readlane(there ? pages : -1, 16 * wave);
             if (page < 0) size_k = size_v = 0;
             const uint64_t at = (uint64_t)(uint32_t)max(page, 0) * a.Hk * page_bytes + (uint32_t)(in_page * row_bytes);
             k_from += at;
             v_from += at;
             if constexpr (SRC == kCodes) {
-                const int key = step * kKeysTile + lane;
-                const int64_t row = (((int64_t)pages * a.Hk + hk) << a.shift) + (key & ((1 << a.shift) - 1));
-                k_scale = v_scale = 0.0f;
-                if (pages >= 0) {
-                    v_scale = a.c.vs[row];
-                    if (wave == 0) k_scale = a.c.ks[row];
-                }
+                const int64_t row = (((int64_t)(there ? pages : 0) * a.Hk + hk) << a.shift) + (key & ((1 << a.shift) - 1));
+                k_scale = a.c.ks[row];
+                v_scale = a.c.vs[row];
             }
             pages = page_of(step + 1);
         }
@@ -434,7 +425,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                     *(LdsU4*)(vb + 16 * (row + ((c + 1) ^ L::key_v(in)))) = widen8<T>(rv[i][2], rv[i][3]);
                 }
             }
-            uint32_t m = __float_as_uint(v_scale) & 0x7fffffffu;
+            const float kx = held ? k_scale : 0.0f, vx = held ? v_scale : 0.0f;
+            uint32_t m = __float_as_uint(vx) & 0x7fffffffu;
             m = m < kInfBits ? m : 0;
             m = dpp_maxu<0x140>(dpp_maxu<0x141>(dpp_maxu<0x4E>(dpp_maxu<0xB1>(m))));
             const float vm = __uint_as_float(uniform(__float_as_uint(max_halves(max_rows16(__uint_as_float(m))))));
@@ -445,8 +437,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                 vref = next;
                 vinv = 1.0f / next;
             }
-            if (wave == 0) *((LdsFloat*)lds_ks[buf] + lane) = k_scale * a.c2;
-            if (wave == 1) *((LdsFloat*)lds_vs[buf] + lane) = v_scale * vinv;
+            if (wave == 0) *((LdsFloat*)lds_ks[buf] + lane) = kx * a.c2;
+            if (wave == 1) *((LdsFloat*)lds_vs[buf] + lane) = vx * vinv;
         }
     };
 
@@ -459,7 +451,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     const int v_row = 4 * h + ((lane & 15) >> 2);
     const int v_at = v_row * L::CU * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8, v_key = L::key_v(v_row) << 4;
 
-    // The reference is set kAbove powers of two above the largest score and stays until one passes it.  float16
+    // The reference is set kAbove powers of two above the largest score and stays until a lane's 32
+    // probabilities add up to 2: where none has, none is as large.  float16
     // holds a probability's 11 bits down to 2^-14 of the reference; binary32 sums of bfloat16 ones and values
     // keep theirs for values down to 2^-78.  Scores that spread over 2^30 (heads of 4096 x 4096 with a standard
     // deviation of 5 nats) move a reference 2^7 above every few steps: 119 us instead of 91.
@@ -480,7 +473,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
 #pragma unroll
             for (int t = 0; t < KS; ++t) {
                 s[b] = mma32<T>(*(const LdsU4*)(kb + 32 * b * L::CU * 16 + ((t << 5) ^ k_key)), q[t], s[b]);
-                if (b == 0 && t < kLoads) load_k(t, next_k);
+                if (SRC != kCodes && b == 0 && t < kLoads) load_k(t, next_k);
             }
             if constexpr (SRC == kCodes) {
 #pragma unroll
@@ -496,73 +489,64 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         const auto seen = [&](int b, int i) {
             return 32 * b + 2 * (i & ~3) + (i & 3) < rel && !(no_page >> (2 * b + (i >> 3)) & 1);
         };
-        // their probabilities over the reference; all sums are of the rounded ones but where they still take
-        // a scale.  The result's bits 14 and 30 are set where one is 2 or more, or NaN.
+        // their probabilities over the reference, and the lane's sum of them
         u4 pr[4];
-        const auto weigh = [&](float ref, float& sum) __attribute__((always_inline)) {
-            uint32_t big = 0;
+        const auto weigh = [&](float ref) __attribute__((always_inline)) {
+            float sum[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                     float e[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < 4; ++j) {
                         e[j] = __builtin_amdgcn_exp2f(SRC == kCodes ? s[b][i + j] - ref : __builtin_fmaf(s[b][i + j], a.c2, -ref));
+                        sum[j & 1] += e[j];
+                    }
                     if constexpr (SRC == kCodes) {
                         const f4 v4 = *((const LdsF4*)lds_vs[buf] + 8 * b + i / 2 + h);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            big |= __float_as_uint(e[j]);
-                            sum += e[j];
-                            e[j] *= v4[j];
-                        }
+                        for (int j = 0; j < 4; ++j) e[j] *= v4[j];
                     }
-                    const uint32_t lo = narrow<T>(e[0], e[1]), hi = narrow<T>(e[2], e[3]);
-                    pr[2 * b + i / 8][i % 8 / 2] = lo;
-                    pr[2 * b + i / 8][i % 8 / 2 + 1] = hi;
-                    if constexpr (SRC != kCodes) {
-                        big |= lo | hi;
-                        sum += (e[0] + e[1]) + (e[2] + e[3]);
-                    }
+                    pr[2 * b + i / 8][i % 8 / 2] = narrow<T>(e[0], e[1]);
+                    pr[2 * b + i / 8][i % 8 / 2 + 1] = narrow<T>(e[2], e[3]);
                 }
-            return big;
+            return sum[0] + sum[1];
         };
-        float sum = l, f = 1.0f;
+        float sum, f = 1.0f;
         int moved = 0;
-        uint32_t big;
         if (masked) {
-            asm volatile("; some keys hidden");
+            asm volatile("; some keys hidden");  // two forms, which the compiler is not to join again
             score();
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (!seen(b, i)) s[b][i] = -INFINITY;
-            big = weigh(m, sum);
+            sum = weigh(m);
             asm volatile("; some keys hidden");
         } else {
             asm volatile("; all keys seen");
             score();
-            big = weigh(m, sum);
+            sum = weigh(m);
             asm volatile("; all keys seen");
         }
-        if (__builtin_expect(__any((big & (SRC == kCodes ? 0x40000000u : 0x40004000u)) != 0), 0)) {
-            // the reference follows the largest score, where that has passed it, and the probabilities with it
+        if (__builtin_expect(__any(!(sum < 2.0f)), 0)) {  // a probability may be large, or there is no reference yet
+            // every row's reference follows its largest score, and its probabilities with it
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
             if constexpr (SRC != kCodes) top *= a.c2;
-            top = max_halves(top);
-            if (top > m) {
-                f = __builtin_amdgcn_exp2f(m - (top + kAbove));
-                m = top + kAbove;
-            }
-            sum = l * f;
-            weigh(m == -INFINITY ? 0.0f : m, sum);
+            // (a row's own sums decide, so that no other row's keys change how it rounds)
+            const bool mine = max_halves(sum < 2.0f ? 0.0f : 1.0f) > 0.0f;
+            const float next = mine ? fmaxf(m, max_halves(top) + kAbove) : m;
+            f = next > m ? __builtin_amdgcn_exp2f(m - next) : 1.0f;
+            m = next;
+            l *= f;
+            sum = weigh(m == -INFINITY ? 0.0f : m);
             moved = 1;
         }
-        l = sum;
+        l += sum;
         if constexpr (SRC == kCodes) {
             moved |= uniform(v_fall != 1.0f);
             f *= v_fall;
@@ -585,7 +569,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         // values of the lane's column of block d, keys as its probabilities lie
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            if (t < kLoads) load_v(t, next_v);
+            if (SRC != kCodes && t < kLoads) load_v(t, next_v);
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 const Lds* at = vb + 16 * t * L::CU * 16 + ((64 * d) ^ v_key);
@@ -666,9 +650,9 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         bool bad = false;
         if (lim_first < min(key0 + kKeysTile, p.nk)) bad = clean(vb);
         fetch(step + 1);
+        if constexpr (SRC == kCodes) load_all(next_k, next_v);  // into registers: no branch between them and their use
         if (live && key0 < lim_hi) compute(key0 + kKeysTile > lim_lo || no_page, bad, step, buf, kb, vb, next_k, next_v);
-        else load_all(next_k, next_v);
-        if (step + 1 < end) store(buf ^ 1, next_k, next_v);
+        else if constexpr (SRC != kCodes) load_all(next_k, next_v);
         ++step;
     };
     if (step < end) {
@@ -679,7 +663,15 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     }
     while (step < end) {
         turn(0, (Lds*)k0, (Lds*)v0, (Lds*)k1, (Lds*)v1);
-        if (step < end) turn(1, (Lds*)k1, (Lds*)v1, (Lds*)k0, (Lds*)v0);
+        if constexpr (SRC == kCodes) {
+            if (step >= end) break;
+            store(1, (Lds*)k1, (Lds*)v1);
+            turn(1, (Lds*)k1, (Lds*)v1, (Lds*)k0, (Lds*)v0);
+            if (step >= end) break;
+            store(0, (Lds*)k0, (Lds*)v0);
+        } else if (step < end) {
+            turn(1, (Lds*)k1, (Lds*)v1, (Lds*)k0, (Lds*)v0);
+        }
     }
     __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);  // vmcnt(0): no load is under way into LDS that another workgroup gets
 
@@ -996,7 +988,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
 bool few_rows(const cham_attn* a) { return !a->cu_q && a->T == a->B; }
 
 // Pieces the work is cut into: what the card holds at once.
-int slots_of(bool few) { return cham_device_cus() * (few ? 4 : 2); }
+int slots_of(bool few) { return cham_device_cus() * 4; }
 
 struct Space {
     int64_t pieces, rows, bytes;
