@@ -588,9 +588,10 @@ typedef struct cham_heads {
 
 /* y = x / sqrt(mean_D(x^2) + eps) * g (norm), then the pairs (a, b), i = 0 .. R/2 - 1, of the first
  * R elements turn by the angle t = pos freq[i]: (a cos t - b sin t, b cos t + a sin t) * amp.
- * The squares, their sum and the root are binary64 (every finite row has its norm); angles are
- * binary64 up to their reduction by pi/2, so far positions keep their angle (absolute error below
- * 2^-53 |t| + 2^-24); the rest is binary32, rounded once to the output's type. */
+ * The squares, their sum and the root are binary64 for binary32 elements and where a row's mean square lies
+ * outside 2^-60 .. 2^100, else binary32 (y within 2^-20): every finite row has its norm.  Angles are binary64
+ * up to their reduction by pi/2, so far positions keep their angle (absolute error below 2^-53 |t| + 2^-24);
+ * the rest is binary32, rounded once to the output's type. */
 typedef struct cham_rotate {
     int64_t T;             /* tokens                                                          */
     int32_t D;

@@ -35,6 +35,13 @@ CHAM_DEV double vector_sum(double v) {
     return LP == 16 ? dpp_add<0x140>(v) : v;
 }
 template <int LP>
+CHAM_DEV float vector_sum(float v) {
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    v += dpp<0x141>(v);
+    return LP == 16 ? v + dpp<0x140>(v) : v;
+}
+template <int LP>
 CHAM_DEV uint32_t vector_max(uint32_t v) {
     v = dpp_maxu<0x141>(dpp_maxu<0x4E>(dpp_maxu<0xB1>(v)));
     return LP == 16 ? dpp_maxu<0x140>(v) : v;
@@ -82,112 +89,173 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const RowsArgs a) {
     const int64_t t0 = (int64_t)blockIdx.x * a.tok;
     const int nt = (int)min((int64_t)a.tok, a.r.T - t0);
     const int first = blockIdx.y * a.per, per = min(a.per, a.nv - first);
-    const int items = nt * per;
     const bool live = d0 < D;
 
+    // A group of lanes takes vectors first + group, + kGroups, ... of each token, a few tokens' loads at a
+    // time, the first before the angles.
+    constexpr int kBatch = XT == CHAM_T_F32 ? 2 : 4, kSize = XT == CHAM_T_F32 ? 4 : 2;
+    Raw<XT> raw[kBatch];
+    int which = 0, head = 0;
+    const char* from = nullptr;
+    int64_t step = 0;  // bytes from token to token
+    const auto vector = [&](int vec) {
+        const int hq = a.in[0].H, hk = a.in[1].H;
+        which = vec < hq ? 0 : vec < hq + hk ? 1 : 2;
+        head = vec - (which == 0 ? 0 : which == 1 ? hq : hq + hk);
+        const cham_heads& h = which == 0 ? a.in[0] : which == 1 ? a.in[1] : a.in[2];
+        step = h.token * kSize;
+        from = (const char*)h.p + (t0 * h.token + (int64_t)head * h.head + d0) * kSize;
+    };
+    const auto fetch = [&](int tok) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            raw[i] = Raw<XT>{};
+            if (live && tok + i < nt) raw[i] = load8<XT>(from + (tok + i) * step, 0);
+        }
+    };
+    if (group < per) {
+        vector(first + group);
+        fetch(0);
+    }
     if (half > 0) {
         for (int i = threadIdx.x; i < nt * kMaxHalf; i += kThreads) {
             const int k = i % kMaxHalf;
+            float2 v = make_float2(1.0f, 0.0f);  // pairs behind R stay as they are
             if (k < half) {
-                const float2 v = cos_sin((double)a.r.pos[t0 + i / kMaxHalf] * a.r.freq[k]);
-                cs[i / kMaxHalf][0][k] = v.x * a.r.amp;
-                cs[i / kMaxHalf][1][k] = v.y * a.r.amp;
+                v = cos_sin((double)a.r.pos[t0 + i / kMaxHalf] * a.r.freq[k]);
+                v.x *= a.r.amp;
+                v.y *= a.r.amp;
             }
+            cs[i / kMaxHalf][0][k] = v.x;
+            cs[i / kMaxHalf][1][k] = v.y;
         }
     }
-    struct At {
-        int which, head, tok;
-    };
-    const auto at = [&](int item) {
-        const int tok = per == 1 ? item : item / per, vec = item - tok * per + first;
-        const int hq = a.in[0].H, hk = a.in[1].H;
-        return vec < hq ? At{0, vec, tok} : vec < hq + hk ? At{1, vec - hq, tok} : At{2, vec - hq - hk, tok};
-    };
-    const auto fetch = [&](const At& p) {
-        const cham_heads& h = p.which == 0 ? a.in[0] : p.which == 1 ? a.in[1] : a.in[2];
-        Raw<XT> r{};
-        if (live) r = load8<XT>(h.p, (t0 + p.tok) * h.token + (int64_t)p.head * h.head + d0);
-        return r;
-    };
-    Raw<XT> next{};
-    if (group < items) next = fetch(at(group));
     __syncthreads();
 
-    for (int item = group; item < items; item += kGroups) {
-        const At p = at(item);
-        float y[kChunk];
-        widen<XT>(next, y);
-        if (item + kGroups < items) next = fetch(at(item + kGroups));
-        if (p.which < 2) {
-            if (a.r.norm) {
-                double s = 0.0;
+    for (int vec = group; vec < per; vec += kGroups) {
+        if (vec != group) vector(first + vec);
+        const cham_heads& out = which == 0 ? a.out[0] : a.out[1];
+        char* const to = (char*)out.p + (t0 * out.token + (int64_t)head * out.head + d0) * kSize;
+        const int64_t to_step = out.token * kSize;
+        float w[kChunk];  // the norm's weights
+        if (a.r.norm && which < 2) {
+            const void* g = which == 0 ? a.r.qg : a.r.kg;
 #pragma unroll
-                for (int j = 0; j < kChunk; ++j) s = __builtin_fma((double)y[j], (double)y[j], s);
-                s = __builtin_fma(vector_sum<LP>(s), a.inv_d, (double)a.r.eps);
-                // 1 / sqrt(s): binary32's estimate for s brought into its range by a power of four,
-                // one Newton step in binary64; an infinite s gives 0
-                const int e = (__builtin_amdgcn_frexp_exp(s) + 1) & ~1;
-                const double m = __builtin_amdgcn_ldexp(s, -e);
-                double q = (double)__builtin_amdgcn_rsqf((float)m);
-                if (q != 0.0) q = __builtin_amdgcn_ldexp(q * __builtin_fma(-0.5 * m * q, q, 1.5), -e / 2);
-                const void* g = p.which == 0 ? a.r.qg : a.r.kg;
-                float w[kChunk];
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) w[j] = 1.0f;
-                if (g && live) load_g(g, p.which == 0 ? a.r.qg_type : a.r.kg_type, d0, w);
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) y[j] = (float)((double)y[j] * q) * w[j];
-            }
-            if (half > 0) {
-                const float *co = cs[p.tok][0], *si = cs[p.tok][1];
-                if (a.r.layout == CHAM_ROT_PAIRS) {
-#pragma unroll
-                    for (int j = 0; j < kChunk; j += 2) {
-                        const int i = (d0 + j) >> 1;
-                        if (i < half) {
-                            const float c = co[i], s = si[i], u = y[j], v = y[j + 1];
-                            y[j] = u * c - v * s;
-                            y[j + 1] = v * c + u * s;
-                        }
-                    }
-                } else {
-                    // partners lie R/2 elements apart, in another lane and, for odd R/2, at
-                    // another place: through LDS, within the wavefront
-                    float* row = rows[group];
-                    *(float4*)(row + d0) = make_float4(y[0], y[1], y[2], y[3]);
-                    *(float4*)(row + d0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
-                    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                    for (int j = 0; j < kChunk; ++j) {
-                        const int d = d0 + j;
-                        if (d < 2 * half) {
-                            const bool low = d < half;
-                            const int i = low ? d : d - half;
-                            const float o = row[low ? d + half : i], s = si[i];
-                            y[j] = y[j] * co[i] + (low ? -o : o) * s;
-                        }
-                    }
-                    __builtin_amdgcn_wave_barrier();
-                }
-            }
+            for (int j = 0; j < kChunk; ++j) w[j] = 1.0f;
+            if (g && live) load_g(g, which == 0 ? a.r.qg_type : a.r.kg_type, d0, w);
         }
-        if (CT < 0 || p.which == 0) {
-            const cham_heads& h = p.which == 0 ? a.out[0] : a.out[1];
-            if (live) put8<XT>(h.p, (t0 + p.tok) * h.token + (int64_t)p.head * h.head + d0, y);
-        } else if constexpr (CT >= 0) {
-            const int32_t slot = a.slots[t0 + p.tok];
-            const bool in = slot >= 0 && slot < a.c.pages * a.c.page;
-            const int64_t row = in ? ((int64_t)(slot / a.c.page) * a.c.H + p.head) * a.c.page + slot % a.c.page : 0;
-            void* to = p.which == 1 ? a.c.k : a.c.v;
-            if constexpr (CT == CHAM_T_E4M3) {
-                uint32_t stored;
-                const float r = block_scale(vector_max<LP>(live ? chunk_amax(y) : 0u), false, &stored);
-                if (in && live) {
-                    *(uint2*)((uint8_t*)to + row * D + d0) = codes8_e4m3(y, r);
-                    if (lane == 0) ((uint32_t*)(p.which == 1 ? a.c.ks : a.c.vs))[row] = stored;
+        for (int tok0 = 0; tok0 < nt; tok0 += kBatch) {
+            if (vec != group || tok0 > 0) fetch(tok0);
+#pragma unroll
+            for (int v = 0; v < kBatch; ++v) {
+                const int tok = tok0 + v;
+                if (tok >= nt) break;
+                float y[kChunk];
+                widen<XT>(raw[v], y);
+                if (which < 2) {
+                    if (a.r.norm) {
+                        // 16-bit elements: binary32 where the sum is far from its ends (twelve roundings, halved by the
+                        // root: 6 2^-24); else, and for binary32 elements, binary64
+                        float q32 = 0.0f;
+                        bool wide = XT == CHAM_T_F32;
+                        if constexpr (XT != CHAM_T_F32) {
+                            float s = 0.0f;
+#pragma unroll
+                            for (int j = 0; j < kChunk; ++j) s = __builtin_fmaf(y[j], y[j], s);
+                            s = __builtin_fmaf(vector_sum<LP>(s), (float)a.inv_d, a.r.eps);
+                            q32 = __builtin_amdgcn_rsqf(s);
+                            q32 = q32 * __builtin_fmaf(-0.5f * s * q32, q32, 1.5f);
+                            wide = !(s > 0x1p-60f && s < 0x1p+100f);
+                        }
+                            if (wide) {
+                            double s = 0.0;
+#pragma unroll
+                            for (int j = 0; j < kChunk; ++j) s = __builtin_fma((double)y[j], (double)y[j], s);
+                            s = __builtin_fma(vector_sum<LP>(s), a.inv_d, (double)a.r.eps);
+                            // 1 / sqrt(s): binary32's estimate for s brought into its range by a power of four,
+                            // one Newton step in binary64; an infinite s gives 0
+                            const int e = (__builtin_amdgcn_frexp_exp(s) + 1) & ~1;
+                            const double m = __builtin_amdgcn_ldexp(s, -e);
+                            double q = (double)__builtin_amdgcn_rsqf((float)m);
+                            if (q != 0.0) q = __builtin_amdgcn_ldexp(q * __builtin_fma(-0.5 * m * q, q, 1.5), -e / 2);
+#pragma unroll
+                            for (int j = 0; j < kChunk; ++j) y[j] = (float)((double)y[j] * q) * w[j];
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < kChunk; ++j) y[j] = y[j] * q32 * w[j];
+                        }
+                    }
+                    if (half > 0) {
+                        const float *co = cs[tok][0], *si = cs[tok][1];
+                        if (a.r.layout == CHAM_ROT_PAIRS) {
+                            const float4 c4 = *(const float4*)(co + d0 / 2), s4 = *(const float4*)(si + d0 / 2);
+                            const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float u = y[2 * j], v = y[2 * j + 1];
+                                y[2 * j] = u * c[j] - v * s[j];
+                                y[2 * j + 1] = v * c[j] + u * s[j];
+                            }
+                        } else if (half % kChunk == 0) {
+                            // a partner is another lane's element of the same place
+                            const bool low = d0 < half, turned = d0 < 2 * half;
+                            const int i = turned ? (low ? d0 : d0 - half) : 0, from = turned ? (low ? d0 + half : i) : 0;
+                            float* row = rows[group];
+                            *(float4*)(row + d0) = make_float4(y[0], y[1], y[2], y[3]);
+                            *(float4*)(row + d0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
+                            __builtin_amdgcn_wave_barrier();
+                            float4 o4[2], c4[2], s4[2];
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                o4[j] = *(const float4*)(row + from + 4 * j);
+                                c4[j] = *(const float4*)(co + i + 4 * j);
+                                s4[j] = *(const float4*)(si + i + 4 * j);
+                            }
+                            __builtin_amdgcn_wave_barrier();
+                            const float *o = (const float*)o4, *c = (const float*)c4, *s = (const float*)s4;
+                            if (turned) {
+#pragma unroll
+                                for (int j = 0; j < kChunk; ++j) y[j] = y[j] * c[j] + (low ? -o[j] : o[j]) * s[j];
+                            }
+                        } else {
+                            // partners lie R/2 elements apart, in another lane and, for odd R/2, at
+                            // another place: through LDS, within the wavefront
+                            float* row = rows[group];
+                            *(float4*)(row + d0) = make_float4(y[0], y[1], y[2], y[3]);
+                            *(float4*)(row + d0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
+                            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                            for (int j = 0; j < kChunk; ++j) {
+                                const int d = d0 + j;
+                                if (d < 2 * half) {
+                                    const bool low = d < half;
+                                    const int i = low ? d : d - half;
+                                    const float o = row[low ? d + half : i], s = si[i];
+                                    y[j] = y[j] * co[i] + (low ? -o : o) * s;
+                                }
+                            }
+                            __builtin_amdgcn_wave_barrier();
+                        }
+                    }
                 }
-            } else if (in && live) {
-                put8<CT>(to, row * D + d0, y);
+                if (CT < 0 || which == 0) {
+                    if (live) put8<XT>(to + tok * to_step, 0, y);
+                } else if constexpr (CT >= 0) {
+                    const int32_t slot = a.slots[t0 + tok];
+                    const bool in = slot >= 0 && slot < a.c.pages * a.c.page;
+                    const int64_t row = in ? ((int64_t)(slot / a.c.page) * a.c.H + head) * a.c.page + slot % a.c.page : 0;
+                    void* to = which == 1 ? a.c.k : a.c.v;
+                    if constexpr (CT == CHAM_T_E4M3) {
+                        uint32_t stored;
+                        const float r = block_scale(vector_max<LP>(live ? chunk_amax(y) : 0u), false, &stored);
+                        if (in && live) {
+                            *(uint2*)((uint8_t*)to + row * D + d0) = codes8_e4m3(y, r);
+                            if (lane == 0) ((uint32_t*)(which == 1 ? a.c.ks : a.c.vs))[row] = stored;
+                        }
+                    } else if (in && live) {
+                        put8<CT>(to, row * D + d0, y);
+                    }
+                }
             }
         }
     }
@@ -238,27 +306,46 @@ __global__ __launch_bounds__(kThreads) void read_kernel(const ReadArgs a) {
     }
     __syncthreads();
     if (d0 >= a.c.D) return;
-    for (int item = group; item < nt * per; item += kGroups) {
-        const int tok = item / per, vec = item - tok * per + first;
-        const bool v = vec >= a.c.H;
-        const int head = v ? vec - a.c.H : vec, page = page_of[tok];
-        if (page == -2) continue;
-        float y[kChunk] = {};
-        if (page >= 0) {
-            const int64_t row = ((int64_t)page * a.c.H + head) * a.c.page + place[tok];
+    // four vectors' loads are under way at a time
+    for (int item0 = group; item0 < nt * per; item0 += 4 * kGroups) {
+        Raw<CT == CHAM_T_E4M3 ? CHAM_T_BF16 : CT> raw[4];
+        float scale[4];
+        int page[4];
+        int64_t to[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int item = min(item0 + i * kGroups, nt * per - 1);
+            const int tok = (int)((uint32_t)item / (uint32_t)per), vec = item - tok * per + first;
+            const bool v = vec >= a.c.H;
+            const int head = v ? vec - a.c.H : vec;
+            page[i] = item0 + i * kGroups < nt * per ? page_of[tok] : -2;
+            const int64_t row = ((int64_t)max(page[i], 0) * a.c.H + head) * a.c.page + (page[i] >= 0 ? place[tok] : 0);
             const void* from = v ? a.c.v : a.c.k;
             if constexpr (CT == CHAM_T_E4M3) {
                 const uint2 w = *(const uint2*)((const uint8_t*)from + row * a.c.D + d0);
-                decode8_e4m3(w, y);
-                const float s = (v ? a.c.vs : a.c.ks)[row];
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) y[j] *= s;
+                raw[i].a = make_uint4(w.x, w.y, 0, 0);
+                scale[i] = (v ? a.c.vs : a.c.ks)[row];
             } else {
-                widen<CT>(load8<CT>(from, row * a.c.D + d0), y);
+                raw[i] = load8<CT>(from, row * a.c.D + d0);
             }
+            const cham_heads& h = v ? a.vo : a.ko;
+            to[i] = (int64_t)(uintptr_t)h.p + ((t0 + tok) * h.token + (int64_t)head * h.head + d0) * (YT == CHAM_T_F32 ? 4 : 2);
         }
-        const cham_heads& h = v ? a.vo : a.ko;
-        put8<YT>(h.p, (t0 + tok) * h.token + (int64_t)head * h.head + d0, y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (page[i] == -2) continue;
+            float y[kChunk] = {};
+            if (page[i] >= 0) {
+                if constexpr (CT == CHAM_T_E4M3) {
+                    decode8_e4m3(make_uint2(raw[i].a.x, raw[i].a.y), y);
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) y[j] *= scale[i];
+                } else {
+                    widen<CT>(raw[i], y);
+                }
+            }
+            put8<YT>((void*)(uintptr_t)to[i], 0, y);
+        }
     }
 }
 
@@ -274,7 +361,7 @@ void rows_plan(int64_t T, int nv, int groups, int* tok, int* split) {
         *tok = 1;
         *split = one;
     } else {
-        *tok = std::max(1, std::min(kMaxTok, 4 * groups / nv));
+        *tok = std::max(1, std::min(kMaxTok, 8 * groups / nv));
         *split = 1;
     }
 }

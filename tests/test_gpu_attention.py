@@ -61,7 +61,9 @@ def _within(got, want, bound):
 def _rotated(x, w, eps, norm, pos, freq, layout, amp):
     """(y, bound) in 64 bits: the bound counts the chain's binary32 roundings, not the output's.
 
-    Norm: two roundings (the product with the root's reciprocal, the weight).  A pair's sum takes cos and
+    Norm: two roundings (the product with the root's reciprocal, the weight); of 16-bit elements, whose squares
+    are added in binary32, 12 in all: eight squares in a lane and four steps over lanes (halved by the root: 6),
+    the mean and eps (1), the reciprocal root and its step (3).  A pair's sum takes cos and
     sin within 2^-23 (a remainder rounded to 2^-26, the series' seven roundings below 2^-24 each of
     terms that fall fast, and the reduction's 2^-53 |t|), amp one rounding, two products and their sum."""
     y = x.double()
@@ -69,7 +71,7 @@ def _rotated(x, w, eps, norm, pos, freq, layout, amp):
         y = y / torch.sqrt((y * y).mean(2, keepdim=True) + eps)
         if w is not None:
             y = y * w.double()
-    bound = y.abs() * (3 * U if norm else 0.0)
+    bound = y.abs() * ((3 * U if x.dtype == torch.float32 else 12 * U) if norm else 0.0)
     if freq is None:
         return y, bound
     n = freq.numel()
@@ -79,7 +81,7 @@ def _rotated(x, w, eps, norm, pos, freq, layout, amp):
     i, j = (torch.arange(n, device=DEV) * 2, torch.arange(n, device=DEV) * 2 + 1) if layout == cham.ROT_PAIRS else \
         (torch.arange(n, device=DEV), torch.arange(n, device=DEV) + n)
     a, b = y[..., i], y[..., j]
-    err = (a.abs() + b.abs()) * abs(amp) * (angle + 7 * U)
+    err = (a.abs() + b.abs()) * abs(amp) * (angle + (7 if x.dtype == torch.float32 else 16) * U)
     y, bound = y.clone(), bound.clone()
     y[..., i], y[..., j] = a * c - b * s, b * c + a * s
     bound[..., i] = err
