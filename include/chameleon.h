@@ -660,7 +660,8 @@ typedef struct cham_attn {
     int32_t pad;
     const int32_t* cu_q;   /* [B + 1] first rows, ascending from 0 to at most T: rows behind the
                               last sequence are left as they are.  NULL: B sequences of T / B   */
-    cham_heads q, o;       /* CHAM_T_F16 or CHAM_T_BF16, one type; o overlaps no input        */
+    cham_heads q, o;       /* CHAM_T_F16 or CHAM_T_BF16, one type; o overlaps no input (o.p ==
+                              q.p is refused)                                                 */
 } cham_attn;
 
 /* Attention over packed keys and values k, v [Tk][Hk][D] of q's type: cu_k as cu_q, NULL: B
@@ -674,7 +675,7 @@ int cham_attention(const cham_attn* a, const cham_heads* k, const cham_heads* v,
 /* Attention of each sequence's newest tokens over its tokens in a cache: lens[b] (device) counts
  * sequence b's tokens, the queries' own among them, which have been written before; table [B][width] as
  * in cham_cache_read.  Always causal.  A token without a page is seen by no query; lens beyond
- * width * page count as that.  c's type is q's, or E4M3.  ws and errors as cham_attention. */
+ * width * page (or 2^31 - 2^16) count as that.  c's type is q's, or E4M3.  ws and errors as cham_attention. */
 int cham_cache_attention(const cham_attn* a, const cham_cache* c, const int32_t* table, int64_t width,
                          const int32_t* lens, void* ws, size_t ws_bytes, void* stream);
 

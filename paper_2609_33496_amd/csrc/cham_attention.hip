@@ -88,7 +88,7 @@ CHAM_DEV Seq sequence(const AttnArgs& a, int b) {
         }
     } else {
         s.k0 = 0;
-        s.nk = (int)min((int64_t)max(a.lens[b], 0), a.width << a.shift);
+        s.nk = (int)min(min((int64_t)max(a.lens[b], 0), a.width << a.shift), kMaxRows);
     }
     return s;
 }
@@ -677,7 +677,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
 
     if (!live || my_row >= rows || (p.pieces > 1 && (unsigned)p.index >= (unsigned)a.most)) return;
     l = add_halves(l);
-    const float f = l == 0.0f ? 0.0f : (SRC == kCodes ? vref : 1.0f) / l;
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;  // before the values' scale: the product stays in range
     m = m == -INFINITY ? 0.0f : m;
     const int64_t o_at = (int64_t)(p.q0 + token) * a.a.o.token + (int64_t)head * a.a.o.head;
     float* po = a.part_o + ((int64_t)p.index * kRowsTile + wave * 32 + col) * D;
@@ -687,8 +687,11 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         for (int i = 0; i < 16; i += 4) {
             const int e = 32 * d + 2 * i + 4 * h;
             if (e >= D) continue;
-            if (p.pieces == 1) put4<T>(a.a.o, o_at + e, o[d][i] * f, o[d][i + 1] * f, o[d][i + 2] * f, o[d][i + 3] * f);
-            else *(f4*)(po + e) = f4{o[d][i] * f, o[d][i + 1] * f, o[d][i + 2] * f, o[d][i + 3] * f};
+            float r[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = o[d][i + j] * f * (SRC == kCodes ? vref : 1.0f);
+            if (p.pieces == 1) put4<T>(a.a.o, o_at + e, r[0], r[1], r[2], r[3]);
+            else *(f4*)(po + e) = f4{r[0], r[1], r[2], r[3]};
         }
     if (p.pieces > 1 && h == 0)
         *(float2*)(a.part_s + ((int64_t)p.index * kRowsTile + wave * 32 + col) * 2) = make_float2(m, l);
@@ -697,29 +700,30 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
 // ------------------------------------------------------------------------------------
 // the kernel of single tokens: up to 16 rows (heads of one token), over pages
 // ------------------------------------------------------------------------------------
-// The cache's bytes bound it.  Each of 4 wavefronts takes every fourth 32 keys of the piece, with no
+// The cache's bytes bound it.  Each of NW wavefronts takes every NW-th 32 keys of the piece, with no
 // wait for the others: keys go from memory into the products' operand as they lie (a lane's 16 bytes
 // of a row are a run of D, which only fixes the order of the sum), values through the wavefront's own
 // LDS for the transposing read; the next 32 keys' loads are under way meanwhile.  At the end
-// the four join through LDS.
-template <int ND, int SRC>
+// they join through LDS.
+template <int ND, int SRC, int NW>
 struct Few {
     // rows of values 2 mod 4 chunks apart: 8 rows of 32 bytes fall on different banks
     static constexpr int SV = ND <= 5 ? 10 : ND == 6 ? 14 : 18;
     static constexpr int kKLoads = SRC == kCodes ? (ND + 3) / 4 : (ND + 1) / 2;  // of 16 keys
     static constexpr int kUnits = SRC == kCodes ? ND : 2 * ND;                   // chunks of a row of values
     static constexpr int kVLoads = (32 * kUnits + kWave - 1) / kWave;
-    u4 v[4][32][SV];
-    float m[4][kRowsFew], l[4][kRowsFew];
+    u4 v[NW][32][SV];
+    float m[NW][kRowsFew], l[NW][kRowsFew], vref[NW];
 };
 
-template <int T, int ND, int SRC>
-__global__ __launch_bounds__(256, 2) void few_kernel(const AttnArgs a) {
-    using L = Few<ND, SRC>;
+template <int T, int ND, int SRC, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
+    using L = Few<ND, SRC, NW>;
+    constexpr int kKeys = 32 * NW;
     __shared__ L lds;
     const int hk = blockIdx.x % a.Hk;
     Piece p;
-    if (!find_piece<SRC, kRowsFew, kKeysFew, false>(a, blockIdx.x / a.Hk, hk, false, &p)) return;
+    if (!find_piece<SRC, kRowsFew, kKeys, false>(a, blockIdx.x / a.Hk, hk, false, &p)) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane & 15, g = lane >> 4, D = a.a.D;
     const int rows = min(a.G - p.tile * kRowsFew, kRowsFew), head0 = hk * a.G + p.tile * kRowsFew;
@@ -780,11 +784,11 @@ __global__ __launch_bounds__(256, 2) void few_kernel(const AttnArgs a) {
     float m = 0.0f, l = 0.0f, vref = 0.0f, vinv = 0.0f;
     bool any = false;
     u4(&vl)[32][L::SV] = lds.v[wave];
-    const int end = min(p.end * kKeysFew, p.nk);
-    int key0 = p.first * kKeysFew + 32 * wave;
+    const int end = min(p.end * kKeys, p.nk);
+    int key0 = p.first * kKeys + 32 * wave;
     Loads now{};
     if (key0 < end) fetch(key0, now);
-    for (; key0 < end; key0 += kKeysFew) {
+    for (; key0 < end; key0 += kKeys) {
         // values into LDS, and the scores, from this step's registers; then the next step's loads
 #pragma unroll
         for (int i = 0; i < L::kVLoads; ++i) {
@@ -820,7 +824,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(const AttnArgs a) {
                 vs[t][i] = SRC == kCodes ? now.vs[t][i] : 1.0f;
                 if (!now.page[t] || key0 + 16 * t + 4 * g + i >= p.nk) s[t][i] = -INFINITY;
             }
-        if (key0 + kKeysFew < end) fetch(key0 + kKeysFew, now);
+        if (key0 + kKeys < end) fetch(key0 + kKeys, now);
         float top = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -883,31 +887,33 @@ __global__ __launch_bounds__(256, 2) void few_kernel(const AttnArgs a) {
     // the wavefronts' sums, each over its own reference: element i of block d is o[4 g + i of block d]
     l = add_halves(add_rows16(l));
     float* mine = (float*)&lds.v[wave][0][0];
-    const float back = SRC == kCodes ? vref : 1.0f;
 #pragma unroll
-    for (int d = 0; d < ND; ++d) *(f4*)(mine + col * (16 * ND) + 16 * d + 4 * g) = o[d] * back;
+    for (int d = 0; d < ND; ++d) *(f4*)(mine + col * (16 * ND) + 16 * d + 4 * g) = o[d];
+    if (lane == 0) lds.vref[wave] = SRC == kCodes ? vref : 1.0f;
     if (g == 0) {
         lds.m[wave][col] = any ? m : -INFINITY;
         lds.l[wave][col] = l;
     }
     __syncthreads();
     if (p.pieces > 1 && (unsigned)p.index >= (unsigned)a.most) return;
-    for (int u = threadIdx.x; u < rows * (D / 4); u += 256) {
+    for (int u = threadIdx.x; u < rows * (D / 4); u += 64 * NW) {
         const int row = u / (D / 4), e = u % (D / 4) * 4;
         float top = lds.m[0][row];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) top = fmaxf(top, lds.m[w][row]);
-        f4 sum = {};
-        float total = 0.0f;
+        for (int w = 1; w < NW; ++w) top = fmaxf(top, lds.m[w][row]);
+        float weight[NW], total = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = lds.m[w][row] > -INFINITY ? __builtin_amdgcn_exp2f(lds.m[w][row] - top) : 0.0f;
-            if (lds.m[w][row] == -INFINITY && !(lds.l[w][row] != lds.l[w][row])) continue;  // saw no key
-            total += f * lds.l[w][row];
-            sum += f * *(const f4*)((const float*)&lds.v[w][0][0] + row * (16 * ND) + e);
+        for (int w = 0; w < NW; ++w) {
+            const float mw = lds.m[w][row], lw = lds.l[w][row];
+            weight[w] = mw > -INFINITY ? __builtin_amdgcn_exp2f(mw - top) : lw != lw ? lw : 0.0f;  // 0: saw no key
+            total += weight[w] > 0.0f || weight[w] != weight[w] ? weight[w] * lw : 0.0f;
         }
         const float f = total == 0.0f ? 0.0f : 1.0f / total;
-        sum *= f;
+        f4 sum = {};
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            if (weight[w] != 0.0f)
+                sum += weight[w] * f * *(const f4*)((const float*)&lds.v[w][0][0] + row * (16 * ND) + e) * lds.vref[w];
         if (p.pieces == 1) {
             put4<T>(a.a.o, (int64_t)p.q0 * a.a.o.token + (int64_t)(head0 + row) * a.a.o.head + e, sum[0], sum[1], sum[2], sum[3]);
         } else {
@@ -1016,6 +1022,7 @@ int attn_check(const cham_attn* a, int32_t Hk) {
     if (rc == CHAM_OK) rc = heads_check(&a->o, a->T, a->D);
     if (rc != CHAM_OK) return rc;
     if (a->T * (a->q.H / Hk) >= kMaxRows) return CHAM_ESHAPE;
+    if (a->T > 0 && a->o.p == a->q.p) return CHAM_EINVAL;  // several workgroups read a row of q
     return CHAM_OK;
 }
 
@@ -1023,12 +1030,13 @@ int attn_check(const cham_attn* a, int32_t Hk) {
 template <int T, int SRC, int KS, int DB, int ND>
 int launch(AttnArgs& a, bool few, int64_t tiles, bool may_split, hipStream_t s) {
     const int64_t all = tiles * a.Hk, grid = may_split ? all + slots_of(few) : all;
-    if (!cham_launchable(may_split ? std::max(grid, all * (few ? kRowsFew : kRowsTile) / kRowsJoin) : grid, 256)) return CHAM_ESHAPE;
+    if (!cham_launchable(may_split ? std::max(grid, all * (few ? kRowsFew : kRowsTile) / kRowsJoin) : grid, few && !may_split ? 512 : 256)) return CHAM_ESHAPE;
     if constexpr (SRC != kPacked) {
         if (few) {
-            hipLaunchKernelGGL((few_kernel<T, ND, SRC>), dim3((unsigned)grid), dim3(256), 0, s, a);
+            if (may_split) hipLaunchKernelGGL((few_kernel<T, ND, SRC, 4>), dim3((unsigned)grid), dim3(256), 0, s, a);
+            else hipLaunchKernelGGL((few_kernel<T, ND, SRC, 8>), dim3((unsigned)grid), dim3(512), 0, s, a);
             CHAM_CHECK_LAUNCH();
-            if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsFew, kKeysFew>), dim3((unsigned)all, kRowsFew / kRowsJoin), dim3(256), 0, s, a);
+            if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsFew, kKeysFew>), dim3((unsigned)all, a.G > kRowsJoin ? kRowsFew / kRowsJoin : 1), dim3(256), 0, s, a);
             CHAM_CHECK_LAUNCH();
             return CHAM_OK;
         }
@@ -1080,6 +1088,13 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
         may_split = false;
         a.least = INT32_MAX / 2;
     }
+    // Up to 1024 keys are one piece, of eight wavefronts: a step of theirs takes about 1.7 us, a second launch
+    // 4 and 3 more on the host (one sequence of 700
+    // tokens, 8 key heads, 16-bit pages of 16: 12.3 us, in pieces 7.2 and 4.2).
+    if (few && blocks <= 8) {
+        may_split = false;
+        a.least = INT32_MAX / 2;
+    }
     if (SRC == kPacked && !a.a.cu_q && !a.cu_k)  // every length is known here
         may_split = may_split && blocks > up(tiles * blocks * a.Hk, slots_of(few));
     if (a.a.q.type == CHAM_T_F16) return launch_d<CHAM_T_F16, SRC>(a, few, tiles, may_split, s);
@@ -1114,6 +1129,7 @@ extern "C" int cham_attention(const cham_attn* a, const cham_heads* k, const cha
     args.a = *a;
     args.k = *k;
     args.v = *v;
+    if (Tk <= 1) args.k.token = args.v.token = a->D;  // a single row's stride says nothing
     args.cu_k = cu_k;
     args.Tk = Tk;
     args.nk = a->B > 0 ? (int)(Tk / a->B) : 0;

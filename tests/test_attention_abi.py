@@ -31,7 +31,7 @@ def _cache(**kw):
 
 
 def _attn(**kw):
-    d = dict(B=1, T=3, D=64, causal=1, scale=0.125, pad=0, cu_q=None, q=_heads(), o=_heads())
+    d = dict(B=1, T=3, D=64, causal=1, scale=0.125, pad=0, cu_q=None, q=_heads(), o=_heads(p=4096))
     d.update(kw)
     return cham._Attn(*[d[k] for k, _ in cham._Attn._fields_])
 
@@ -138,6 +138,7 @@ def test_attention_other_refusals():
     assert L.cham_attention(a, h, h, 3, None, None, need, None) == cham.EWORKSPACE
     assert L.cham_attention(a, h, h, 3, None, 320, need, None) == cham.EWORKSPACE
     assert L.cham_attention(_attn(T=1), h, h, 3, None, 256, 0, None) == cham.EWORKSPACE
+    assert L.cham_attention(_attn(o=_heads()), h, h, 3, None, 256, need, None) == cham.EINVAL  # over its queries
     c = _cache()
     assert L.cham_cache_attention(a, c, None, 2, 64, 256, need, None) == cham.EINVAL
     assert L.cham_cache_attention(a, c, 64, 2, None, 256, need, None) == cham.EINVAL

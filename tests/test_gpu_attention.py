@@ -616,6 +616,75 @@ def test_cache_attention_scales_of_every_size(dt, chunk):
     assert bool((cham.cache_attention(q, c, table, _ints([n]), _starts(lq) if chunk else None) == 0).all())
 
 
+@pytest.mark.parametrize("chunk", [False, True])
+@pytest.mark.parametrize("n", [40, 3000])
+def test_cache_attention_values_near_the_largest(chunk, n):
+    """Scales of 2^110 in bfloat16: outputs of 2^118 are within its range, their sums over a reference far
+    above or below the scores have to be too.  And scales of 2^-118, whose outputs are normal numbers."""
+    case(f"cache_attention large values chunk={chunk} n={n}")
+    lq = [9] if chunk else [1]
+    for size in (2.0 ** 110, 2.0 ** -118):
+        q, c, table = _cached_case(8, lq, [n], 4, 1, 64, 16, torch.bfloat16, E4)
+        c.v_scale.fill_(size)
+        o = cham.cache_attention(q, c, table, _ints([n]), _starts(lq) if chunk else None)
+        assert bool(o.isfinite().all())
+        _check_cached(o, q, c, table, lq, [n])
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+def test_attention_rows_do_not_change_one_another(dt):
+    """A row's result has the same bits whatever queries lie beside it in its tile."""
+    case(f"attention rows apart {dt}")
+    q, k, v = _qkv(12, 128, 500, 2, 1, 64, dt)
+    want = cham.attention(q, k, v)
+    other = q.clone()
+    other[1::2] *= 30.0
+    other[64] = INF
+    got = cham.attention(other, k, v)
+    keep = torch.arange(0, 128, 2, device=DEV)
+    keep = keep[keep != 64]
+    assert torch.equal(got[keep], want[keep])
+
+
+def test_single_rows_strides_say_nothing():
+    """One key, one query: their row strides may be anything."""
+    case("single rows")
+    q, k, v = _qkv(13, 1, 1, 4, 2, 72, torch.bfloat16)
+    want = cham.attention(q, k, v)
+    wide = [torch.as_strided(t.contiguous(), t.shape, (0, 72, 1)) for t in (q, k, v)]
+    assert torch.equal(cham.attention(*wide), want)
+    qo, ko = cham.norm_rotate(wide[0], wide[1])
+    assert torch.equal(qo, cham.norm_rotate(q, k)[0]) and torch.equal(ko, cham.norm_rotate(q, k)[1])
+    # many queries over one key, which only the last sees
+    q = _rows(14, 200, 4, 72, torch.bfloat16)
+    o = cham.attention(q, wide[1], wide[2], causal=True)
+    assert bool((o[:-1] == 0).all()) and torch.equal(o[-1], want[0].new_empty(4, 72).copy_(wide[2][0].repeat_interleave(2, 0)))
+    none = cham.attention(q, k[:0], v[:0])
+    assert bool((none == 0).all())
+
+
+def test_cache_past_four_gib():
+    """Pages whose bytes lie beyond 32-bit offsets: written, read back and attended like the first ones."""
+    case("cache of 2 x 4.3 GB")
+    H, page, D, pages = 8, 64, 128, 65700
+    c = cham.Cache(*[torch.empty((pages, H, page, D), dtype=E4, device=DEV) for _ in range(2)],
+                   *[torch.empty((pages, H, page), device=DEV) for _ in range(2)])
+    n = 150
+    x = _rows(3, n, 16 + 2 * H, D, torch.bfloat16)
+    q, k, v = x[:, :16], x[:, 16:16 + H], x[:, 16 + H:]
+    t = torch.arange(n, device=DEV)
+    res = []
+    for ids in ([0, 1, 2], [65699, 65536, 65698]):
+        table = _ints([ids])
+        slots = (table[0, t // page] * page + t % page).to(torch.int32)
+        cham.cache_write(c, slots, k, v, norm=False)
+        res.append([*cham.cache_read(c, table, _ints([0, n]), n), cham.cache_attention(q[-1:], c, table, _ints([n])),
+                    cham.cache_attention(q, c, table, _ints([n]), _ints([0, n]))])
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+    assert torch.equal(res[0][0], _gather(cham.Cache(c.k[:3], c.v[:3], c.k_scale[:3], c.v_scale[:3]), _ints([[0, 1, 2]]), 0, n, "k")[0].bfloat16())
+
+
 # ---------------------------------------------------------------------------------------------
 # together, streams, graphs
 # ---------------------------------------------------------------------------------------------
