@@ -649,8 +649,8 @@ int cham_cache_read(const cham_cache* c, const int32_t* table, int64_t width, co
 /* o_i = sum_j p_ij v_j, p_i the softmax over the keys j that query i sees of scale <q_i, k_j>.
  * causal: query i of a sequence's nq sees its first nk - nq + i + 1 of nk keys (the last query sees all
  * of them); else all.  A query that sees none gets zeros; keys that are not seen have no influence,
- * whatever they hold.  Products in 16 bits (q, k, v as they are; p rounded to their type), sums,
- * maxima and statistics in binary32, one rounding at the end.  Results are bitwise reproducible. */
+ * whatever they hold.  Products in 16 bits (q, k, v as they are; p rounded to their type, to
+ * binary16 over E4M3 values), sums, maxima and statistics in binary32, one rounding at the end.  Results are bitwise reproducible. */
 typedef struct cham_attn {
     int64_t B;             /* sequences, < 2^24                                               */
     int64_t T;             /* rows of q and o                                                 */

@@ -25,7 +25,13 @@
 namespace cham {
 namespace {
 
-enum { kPacked, kPages, kCodes };  // where keys and values come from: rows, 16-bit pages, E4M3 pages
+// Where keys and values come from: rows, 16-bit pages, E4M3 pages.  Probabilities are rounded to 16 bits for
+// their product with the values.  Beside 16-bit values they take those's type, and their sum adds the rounded
+// ones, so that a key that outweighs the others comes out as it is (bfloat16 errors against 64 bits stay below 1.5
+// times those of a binary32 form, 0.0017).  E4M3 values are exact in float16, so there they take
+// float16 whatever the queries' type, after the values' scale over the largest of them, which keeps them in
+// its range; the sum adds them unrounded.
+enum { kPacked, kPages, kCodes };
 
 constexpr float kLog2e = 1.44269504f;
 constexpr float kGrow = 8.0f;    // few_kernel: the reference follows scores more than 2^8 above it
@@ -230,6 +236,13 @@ CHAM_DEV uint32_t widen2(uint32_t w) {
     if constexpr (T == CHAM_T_F16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
     else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
 }
+// c plus two 16-bit values
+template <int T>
+CHAM_DEV float add2(uint32_t w, float c) {
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    if constexpr (T == CHAM_T_F16) return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, w), half2v{(_Float16)1, (_Float16)1}, c, false);
+    else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, w), bf2{(__bf16)1.0f, (__bf16)1.0f}, c, false);
+}
 template <int T>
 CHAM_DEV u4 widen8(uint32_t lo, uint32_t hi) {
     return u4{widen2<T, false>(lo), widen2<T, true>(lo), widen2<T, false>(hi), widen2<T, true>(hi)};
@@ -287,6 +300,7 @@ struct Tile {
 template <int T, int KS, int DB, int SRC>
 __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     using L = Tile<KS, DB>;
+    constexpr int VT = SRC == kCodes ? CHAM_T_F16 : T;  // of the values' products, see kPacked
     // each buffer a variable of its own: the compiler then knows that a step's reads do not touch what
     // the loads under way write, and does not wait for them
     __shared__ __align__(1024) uint8_t k0[L::kBytes], k1[L::kBytes], v0[L::kBytes], v1[L::kBytes];
@@ -421,8 +435,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                     const int row = (16 * wave + in) * L::CU;
                     *(LdsU4*)(kb + 16 * (row + (c ^ L::key_k(in)))) = widen8<T>(rk[i][0], rk[i][1]);
                     *(LdsU4*)(kb + 16 * (row + ((c + 1) ^ L::key_k(in)))) = widen8<T>(rk[i][2], rk[i][3]);
-                    *(LdsU4*)(vb + 16 * (row + (c ^ L::key_v(in)))) = widen8<T>(rv[i][0], rv[i][1]);
-                    *(LdsU4*)(vb + 16 * (row + ((c + 1) ^ L::key_v(in)))) = widen8<T>(rv[i][2], rv[i][3]);
+                    *(LdsU4*)(vb + 16 * (row + (c ^ L::key_v(in)))) = widen8<VT>(rv[i][0], rv[i][1]);
+                    *(LdsU4*)(vb + 16 * (row + ((c + 1) ^ L::key_v(in)))) = widen8<VT>(rv[i][2], rv[i][3]);
                 }
             }
             const float kx = held ? k_scale : 0.0f, vx = held ? v_scale : 0.0f;
@@ -452,11 +466,13 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     const int v_at = v_row * L::CU * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8, v_key = L::key_v(v_row) << 4;
 
     // The reference is set kAbove powers of two above the largest score and stays until a lane's 32
-    // probabilities add up to 2: where none has, none is as large.  float16
-    // holds a probability's 11 bits down to 2^-14 of the reference; binary32 sums of bfloat16 ones and values
-    // keep theirs for values down to 2^-78.  Scores that spread over 2^30 (heads of 4096 x 4096 with a standard
-    // deviation of 5 nats) move a reference 2^7 above every few steps: 119 us instead of 91.
-    constexpr float kAbove = T == CHAM_T_F16 ? 6.0f : 24.0f;
+    // probabilities add up to kBig: where none has, none is as large.  float16 holds a probability's 11 bits
+    // between 2^-14 and 2^16 (2^12 before the values' scale, which may be kVGrow times the reference's); binary32
+    // sums of bfloat16 ones and values hold 24 bits for values from 2^-78 up and stay finite for the largest.  So
+    // a reference moves where scores grow by 2^20 (2^16, 2^25).  4096 x 4096, scores of 5 nats' standard deviation:
+    // 119 us a piece where it moves at 2^8, which is every few steps, 91 so.
+    constexpr float kAbove = VT == CHAM_T_F16 ? 6.0f : 24.0f;
+    constexpr float kBig = SRC == kCodes ? 1024.0f : T == CHAM_T_F16 ? 16384.0f : 2.0f;
 
     // One step's keys against the wavefront's rows; masked: some row does not see all of them.  The
     // outputs' sums are touched in three places only, whatever branch made the probabilities, so that they
@@ -501,15 +517,17 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         e[j] = __builtin_amdgcn_exp2f(SRC == kCodes ? s[b][i + j] - ref : __builtin_fmaf(s[b][i + j], a.c2, -ref));
-                        sum[j & 1] += e[j];
+                        if (SRC == kCodes) sum[j & 1] += e[j];
                     }
                     if constexpr (SRC == kCodes) {
                         const f4 v4 = *((const LdsF4*)lds_vs[buf] + 8 * b + i / 2 + h);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) e[j] *= v4[j];
                     }
-                    pr[2 * b + i / 8][i % 8 / 2] = narrow<T>(e[0], e[1]);
-                    pr[2 * b + i / 8][i % 8 / 2 + 1] = narrow<T>(e[2], e[3]);
+                    const uint32_t lo = narrow<VT>(e[0], e[1]), hi = narrow<VT>(e[2], e[3]);
+                    if constexpr (SRC != kCodes) sum[0] = add2<T>(hi, add2<T>(lo, sum[0]));
+                    pr[2 * b + i / 8][i % 8 / 2] = lo;
+                    pr[2 * b + i / 8][i % 8 / 2 + 1] = hi;
                 }
             return sum[0] + sum[1];
         };
@@ -531,14 +549,14 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
             sum = weigh(m);
             asm volatile("; all keys seen");
         }
-        if (__builtin_expect(__any(!(sum < 2.0f)), 0)) {  // a probability may be large, or there is no reference yet
+        if (__builtin_expect(__any(!(sum < kBig)), 0)) {  // a probability may be large, or there is no reference yet
             // every row's reference follows its largest score, and its probabilities with it
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
             if constexpr (SRC != kCodes) top *= a.c2;
             // (a row's own sums decide, so that no other row's keys change how it rounds)
-            const bool mine = max_halves(sum < 2.0f ? 0.0f : 1.0f) > 0.0f;
+            const bool mine = max_halves(sum < kBig ? 0.0f : 1.0f) > 0.0f;
             const float next = mine ? fmaxf(m, max_halves(top) + kAbove) : m;
             f = next > m ? __builtin_amdgcn_exp2f(m - next) : 1.0f;
             m = next;
@@ -574,12 +592,12 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
             for (int d = 0; d < DB; ++d) {
                 const Lds* at = vb + 16 * t * L::CU * 16 + ((64 * d) ^ v_key);
                 const uint2 lo = read_tr(at), hi = read_tr(at + 8 * L::CU * 16);
-                o[d] = mma32<T>(u4{lo.x, lo.y, hi.x, hi.y}, pr[t], o[d]);
+                o[d] = mma32<VT>(u4{lo.x, lo.y, hi.x, hi.y}, pr[t], o[d]);
             }
         }
         if (__builtin_expect(bad, 0)) {
             // Values that are not finite: each row adds those that it sees, from memory (see `clean`).
-            constexpr uint32_t inf = T == CHAM_T_F16 ? 0x7c00u : 0x7f80u;
+            constexpr uint32_t inf = VT == CHAM_T_F16 ? 0x7c00u : 0x7f80u;
 #pragma unroll 1
             for (int key = key0; key < min(key0 + kKeysTile, p.nk); ++key) {
                 const bool see = key < lim && !(no_page >> ((key - key0) >> 4) & 1);
@@ -601,7 +619,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                         if (e < D) {
                             if constexpr (SRC == kCodes) {
                                 const uint32_t c = *(const uint32_t*)(row + e);
-                                w = make_uint2(widen2<T, false>(c), widen2<T, true>(c));
+                                w = make_uint2(widen2<VT, false>(c), widen2<VT, true>(c));
                             } else {
                                 w = *(const uint2*)(row + 2 * e);
                             }
@@ -622,7 +640,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     // times such a value would be NaN in those rows.  They are taken out of LDS (each wavefront its own 16
     // keys'), and added apart; the result: whether there are any.
     const auto clean = [&](Lds* vals) __attribute__((always_inline)) {
-        constexpr uint32_t carry = T == CHAM_T_F16 ? 0x04000400u : 0x00800080u;  // an exponent of ones overflows
+        constexpr uint32_t carry = VT == CHAM_T_F16 ? 0x04000400u : 0x00800080u;  // an exponent of ones overflows
         bool found = false;
 #pragma unroll 1
         for (int i = 0; i < L::CU / 4; ++i) {
@@ -719,6 +737,7 @@ struct Few {
 template <int T, int ND, int SRC, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
     using L = Few<ND, SRC, NW>;
+    constexpr int VT = SRC == kCodes ? CHAM_T_F16 : T;
     constexpr int kKeys = 32 * NW;
     __shared__ L lds;
     const int hk = blockIdx.x % a.Hk;
@@ -795,8 +814,8 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
             const int u = lane + kWave * i, row = u / L::kUnits, c = u % L::kUnits;
             if (32 * L::kUnits % kWave == 0 || row < 32) {
                 if constexpr (SRC == kCodes) {
-                    vl[row][2 * c] = widen8<T>(now.v[i][0], now.v[i][1]);
-                    vl[row][2 * c + 1] = widen8<T>(now.v[i][2], now.v[i][3]);
+                    vl[row][2 * c] = widen8<VT>(now.v[i][0], now.v[i][1]);
+                    vl[row][2 * c + 1] = widen8<VT>(now.v[i][2], now.v[i][3]);
                 } else {
                     vl[row][c] = now.v[i];
                 }
@@ -867,11 +886,14 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.c2, -m));
-                l += e[i];
-                if constexpr (SRC == kCodes) e[i] *= vs[t][i] * vinv;
+                if constexpr (SRC == kCodes) {
+                    l += e[i];
+                    e[i] *= vs[t][i] * vinv;
+                }
             }
-            pr[2 * t] = narrow<T>(e[0], e[1]);
-            pr[2 * t + 1] = narrow<T>(e[2], e[3]);
+            pr[2 * t] = narrow<VT>(e[0], e[1]);
+            pr[2 * t + 1] = narrow<VT>(e[2], e[3]);
+            if constexpr (SRC != kCodes) l = add2<T>(pr[2 * t + 1], add2<T>(pr[2 * t], l));
         }
         // values of column 16 d + (lane & 15): keys 4 g .. + 3 and 16 + 4 g .. + 3
         __builtin_amdgcn_wave_barrier();
@@ -879,7 +901,7 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
             const uint2 lo = read_tr(at + 32 * d), hi = read_tr(at + 32 * d + 16 * L::SV * 16);
-            o[d] = mma16<T>(u4{lo.x, lo.y, hi.x, hi.y}, pr, o[d]);
+            o[d] = mma16<VT>(u4{lo.x, lo.y, hi.x, hi.y}, pr, o[d]);
         }
         __builtin_amdgcn_wave_barrier();
     }

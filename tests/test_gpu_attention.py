@@ -350,7 +350,7 @@ def _attended(q, k, v, scale, causal, seen=None, vstep=None):
     (sum p (1 + d)) lies within u sum p |v| + u |o| of o.  Below the type's normal range p is rounded by half a
     subnormal step, in units of the reference, which lies up to 2^6 above the largest score in float16 (bfloat16:
     2^24; with codes, in units of the largest scale: vstep), so against l >= 1 as here by 2^6 (2^24) of
-    those.  Sums of n terms take n 2^-24."""
+    those; beside codes p is float16 in either case.  Sums of n terms take n 2^-24."""
     nq, Hq, D = q.shape
     nk, Hk = k.shape[:2]
     q, k, v, u, dt = q.double(), k.double(), v.double(), HALF[q.dtype], q.dtype
@@ -380,7 +380,8 @@ def _attended(q, k, v, scale, causal, seen=None, vstep=None):
         a = p @ vz.abs()
         vs = vz.abs() if vstep is None else vstep[:, j:j + 1].expand(-1, D) * (vz != 0)
         bound[:, h] = (p * off) @ vz.abs() + a * (u + 4 * U + nk * 2 * U) + o[:, h].abs() * ((p * off).sum(1, keepdim=True) + nk * U + 8 * U)
-        bound[:, h] += u * o[:, h].abs() + (2.0 ** 6 if dt == torch.float16 else 2.0 ** 24) * TINY[dt] * vs.sum(0, keepdim=True) / l
+        pt = torch.float16 if vstep is not None else dt  # p's type
+        bound[:, h] += u * o[:, h].abs() + (2.0 ** 6 if pt == torch.float16 else 2.0 ** 24) * TINY[pt] * vs.sum(0, keepdim=True) / l
         bound[:, h] += TINY[dt] + u * (o[:, h].abs() + bound[:, h])
     return o, bound * 1.02 + 1e-40
 
