@@ -30,7 +30,7 @@ namespace {
 // ones, so that a key that outweighs the others comes out as it is (bfloat16 errors against 64 bits stay below 1.5
 // times those of a binary32 form, 0.0017).  E4M3 values are exact in float16, so there they take
 // float16 whatever the queries' type, after the values' scale over the largest of them, which keeps them in
-// its range; the sum adds them unrounded.
+// its range; the sum adds them unrounded (but for float16 outputs of single tokens).
 enum { kPacked, kPages, kCodes };
 
 constexpr float kLog2e = 1.44269504f;
@@ -882,18 +882,30 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
         u4 pr;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            float e[4];
+            float e[4], p0[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.c2, -m));
                 if constexpr (SRC == kCodes) {
-                    l += e[i];
+                    p0[i] = e[i];
+                    if (T != CHAM_T_F16) l += e[i];
                     e[i] *= vs[t][i] * vinv;
                 }
             }
             pr[2 * t] = narrow<VT>(e[0], e[1]);
             pr[2 * t + 1] = narrow<VT>(e[2], e[3]);
-            if constexpr (SRC != kCodes) l = add2<T>(pr[2 * t + 1], add2<T>(pr[2 * t], l));
+            if constexpr (SRC != kCodes) {
+                l = add2<T>(pr[2 * t + 1], add2<T>(pr[2 * t], l));
+            } else if constexpr (T == CHAM_T_F16) {
+                // the rounded ones here too, without their scale (where it counts): one key's rounding would be as
+                // large as the output's
+                const uint32_t w[2] = {pr[2 * t], pr[2 * t + 1]};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float by = vs[t][i] * vinv, r = i & 1 ? f16_hi(w[i >> 1]) : f16_lo(w[i >> 1]);
+                    l += by >= 0x1p-20f ? r * __builtin_amdgcn_rcpf(by) : p0[i];
+                }
+            }
         }
         // values of column 16 d + (lane & 15): keys 4 g .. + 3 and 16 + 4 g .. + 3
         __builtin_amdgcn_wave_barrier();
