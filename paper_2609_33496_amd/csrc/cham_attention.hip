@@ -3,8 +3,9 @@
 //   o_i = sum_j p_ij v_j,  p_ij = exp(s_ij - m_i) / sum_j exp(s_ij - m_i),  s_ij = scale <q_i, k_j>
 //
 // in one pass over the keys: a running reference m, the sum l and the output's sum o are rescaled
-// by exp(m_old - m_new) where m grows.  p does not depend on m, so m only follows the largest
-// score where that lies more than 2^8 above it, and most steps rescale nothing.
+// by exp(m_old - m_new) where m grows.  p does not depend on m, so m need not be the largest score: it
+// only has to keep the sums in their types' range, and most steps neither look for a maximum nor
+// rescale anything.
 //
 // The rows of a key head's queries -- G = Hq / Hk heads of each token, token by token -- form one
 // matrix, so grouped heads share the keys they read.  Products run transposed: scores as keys
@@ -248,13 +249,6 @@ CHAM_DEV u4 widen8(uint32_t lo, uint32_t hi) {
     return u4{widen2<T, false>(lo), widen2<T, true>(lo), widen2<T, false>(hi), widen2<T, true>(hi)};
 }
 
-// whether a word's two 16-bit values hold an infinity or a NaN
-template <int T>
-CHAM_DEV bool not_finite(uint32_t w) {
-    constexpr uint32_t e = T == CHAM_T_F16 ? 0x7c00u : 0x7f80u;
-    return (w & e) == e || ((w >> 16) & e) == e;
-}
-
 CHAM_DEV u4 load16(const char* p) { return *(const u4*)p; }
 
 // four transposed 16-bit values: a lane names 8 bytes of a row of LDS and receives, of the four rows
@@ -273,9 +267,20 @@ CHAM_DEV void put4(const cham_heads& o, int64_t at, float a, float b, float c, f
 // KS: steps of 16 along D for the scores, DB: blocks of 32 along D for the outputs.  Keys and values
 // lie in LDS as rows of CU chunks of 16 bytes, without gaps, so that 16-bit ones go there from memory
 // directly; a chunk's place within its row is swizzled so that neither the 16 rows of a score
-// operand nor the four of a transposing read fall on the same banks.
-typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) u2 LdsU2;
+// operand nor the four of a transposing read fall on the same banks (no conflicts counted).  Two
+// buffers; a step's loads are spread over the products of the step before (issued in one go they held a
+// wavefront up for 400 to 600 cycles).
+//
+// What bounds it, per step of a wavefront and D = 72 / 128: 22 / 32 products of 34 cycles, and about 130
+// vector instructions, 600 to 700 cycles with 32 exponentials of 8.6; two workgroups share a CU, and their
+// steps together take 2.9 / 4.1 thousand cycles, 1.9 and 2.3 times the products' (matrix cores busy 43 % over
+// 2 x 4096 x 4096, 16 heads of 72, bfloat16: 203 us, 761 TFLOP/s; 35 % over seven causal sequences of 8101
+// tokens, 32 on 8 heads of 128: 184 us, 757).  A wavefront alone on its SIMD needs as long for one step as two
+// for theirs, so it is the chain scores - exponentials - values in each that takes the time; priorities
+// (s_setprio), three workgroups a CU and a staggered start changed nothing.  Tiles of ragged causal
+// sequences end 18 % after the mean; the search for a piece takes 2 to 3 us of each.  E4M3 pages: 64 more
+// products with scales, the conversions and their way through registers make a step 1.6 times as long
+// (1100 new tokens over 36000, 32 on 8 heads of 128: 304 + 24 us, 467 TFLOP/s).
 typedef __attribute__((address_space(3))) u4 LdsU4;
 typedef __attribute__((address_space(3))) f4 LdsF4;
 typedef __attribute__((address_space(3))) float LdsFloat;
@@ -318,9 +323,9 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     const bool live = row0 + wave * 32 < rows;
     const int lim = my_row < rows ? limit(my_row) : 0;
     // of the wavefront's rows the fewest and the most, and of the tile's the most
-    const int lim_lo = __builtin_amdgcn_readfirstlane(limit(row0 + wave * 32));
-    const int lim_hi = __builtin_amdgcn_readfirstlane(limit(min(row0 + wave * 32 + 31, rows - 1)));
-    const int lim_tile = __builtin_amdgcn_readfirstlane(limit(min(row0 + kRowsTile, rows) - 1));
+    const int lim_lo = uniform(limit(row0 + wave * 32));
+    const int lim_hi = uniform(limit(min(row0 + wave * 32 + 31, rows - 1)));
+    const int lim_tile = uniform(limit(min(row0 + kRowsTile, rows) - 1));
     const int end = min(p.end, (lim_tile + kKeysTile - 1) / kKeysTile);
 
     // the queries: second operand of the scores' products
@@ -722,7 +727,9 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
 // wait for the others: keys go from memory into the products' operand as they lie (a lane's 16 bytes
 // of a row are a run of D, which only fixes the order of the sum), values through the wavefront's own
 // LDS for the transposing read; the next 32 keys' loads are under way meanwhile.  At the end
-// they join through LDS.
+// they join through LDS.  48 sequences of 200000 tokens, 8 key heads of 128, E4M3 pages of 64: 88 us, 4.8 TB/s
+// (a copy reaches 5.1), and 7.6 for the join; 16-bit pages of one sequence of 700 tokens: 12.3, three steps of
+// memory latency, 1.7 each, and 7 before and behind them.
 template <int ND, int SRC, int NW>
 struct Few {
     // rows of values 2 mod 4 chunks apart: 8 rows of 32 bytes fall on different banks
@@ -962,7 +969,8 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
 // joining the pieces of a row tile: o = sum_c w_c o_c / sum_c w_c, w_c = l_c 2^(m_c - max m)
 // ------------------------------------------------------------------------------------
 // A workgroup takes 8 rows, 32 lanes a row (4 elements a lane); where a tile has fewer, several groups of
-// lanes share a row's pieces and are added in their order.
+// lanes share a row's pieces and are added in their order.  24 us for 1044 pieces of 128 rows of 128 (68 MB);
+// one workgroup a tile took 90 for half of them.
 constexpr int kRowsJoin = 8;
 template <int T, int SRC, int BM, int BN>
 __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
@@ -1027,7 +1035,9 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
 // single tokens: one row of queries each, known on the host
 bool few_rows(const cham_attn* a) { return !a->cu_q && a->T == a->B; }
 
-// Pieces the work is cut into: what the card holds at once.
+// Pieces the work is cut into: four for each CU, of which two (three of the single-token kernel) run at once.
+// 1100 new tokens over 36000 cached: 350 us with two, 304 with four, 310 with six; single tokens 88 with two to
+// eight.
 int slots_of(bool few) { return cham_device_cus() * 4; }
 
 struct Space {
@@ -1115,9 +1125,9 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     const int64_t tiles = a.a.cu_q ? a.a.T * a.G / BM + a.a.B : a.a.B * up((int64_t)a.nq * a.G, BM);
     const int64_t blocks = up(nk_most, BN);
     bool may_split = blocks > a.least;
-    // Tiles that fill the card are not cut: the long ones start first, and what a cut saves at the end is less
-    // than the partial outputs and the second launch cost (8101 tokens, 2056 tiles: 5 us with nothing to join).
-    // A cache's sequences may be far longer than others: theirs are cut up to four such fillings.
+    // Tiles that fill the card twice are not cut: the long ones start first, and what a cut saves at the end is
+    // less than the partial outputs and the second launch cost (8101 tokens, 2056 tiles: 44 us with nothing
+    // to join).  A cache's sequences may be far longer than others: theirs are cut up to four times as many.
     if (!few && a.a.T * a.G / BM * a.Hk >= (int64_t)slots_of(few) * (SRC == kPacked ? 1 : 4)) {
         may_split = false;
         a.least = INT32_MAX / 2;

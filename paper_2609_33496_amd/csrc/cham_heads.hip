@@ -5,7 +5,13 @@
 // All are bound by memory, or by their launch where they are small.  A vector is one head of one
 // token; 8 or 16 lanes hold it, 8 consecutive elements each, from its load to its store.  A workgroup
 // takes some tokens with all or a part of their vectors and makes the tokens' cosines and sines
-// once, in LDS.
+// once, in LDS.  A group of lanes stays with one head of those tokens, so that addresses, weights and the
+// branch by kind are worked out once, and has four tokens' loads under way.
+//
+// bfloat16, 8192 x 32 heads of 72, 48 elements turned: 22.9 us, 3.3 TB/s (7 of 16 lanes hold nothing at 72;
+// with one vector at a time and a division for each 32, with sums in binary64 36); 8100 x 8 heads of 128
+// into E4M3 pages 13.8, 3.6 TB/s; 30001 tokens of 8 heads of 128 out of them 43, 4.3 TB/s (a copy reaches
+// 5.1).  One token of 40 heads: 3.8, a launch and the angle's chain.
 #include <algorithm>
 
 #include "cham_chunk.h"
