@@ -611,7 +611,7 @@ typedef struct cham_rotate {
  * all four), any strides; an output may be its input itself, with equal strides, and overlaps
  * nothing else.  Hq or Hk may be 0 (that pair is not touched).
  * Errors: CHAM_EINVAL (NULL, sizes, strides, alignment, eps, amp), CHAM_EFORMAT (types, layout),
- * CHAM_ESHAPE (D, or T >= 2^31 - 64), CHAM_EHIP. */
+ * CHAM_ESHAPE (D, H > 2^16, T >= 2^31 - 2^16, or a launch of 2^32 lanes: 256 for up to 8 tokens), CHAM_EHIP. */
 int cham_norm_rotate(const cham_rotate* r, const cham_heads* q, const cham_heads* qo, const cham_heads* k,
                      const cham_heads* ko, void* stream);
 
@@ -667,8 +667,10 @@ typedef struct cham_attn {
 /* Attention over packed keys and values k, v [Tk][Hk][D] of q's type: cu_k as cu_q, NULL: B
  * sequences of Tk / B rows.  ws: cham_attention_workspace_bytes(a, Hk) bytes, written before they are
  * read; calls that may overlap (two streams, two graphs) need workspaces of their own.
- * Errors: CHAM_EINVAL (NULL, sizes, strides, alignment, T % B without cu_q, ...), CHAM_EFORMAT
- * (types), CHAM_ESHAPE (D, H, or a stride or T of 2^22, 2^31 - 2^16 and more), CHAM_EWORKSPACE, CHAM_EHIP. */
+ * Errors: CHAM_EINVAL (NULL, sizes, strides, alignment, T % B or Tk % B without cu_q or cu_k, scale,
+ * o over q), CHAM_EFORMAT (types), CHAM_ESHAPE (D, H > 2^16, B >= 2^24, T Hq / Hk or Tk of 2^31 - 2^16 and
+ * more, a token stride of k or v of 2^24 elements and more, or a launch of 2^32 lanes), CHAM_EWORKSPACE,
+ * CHAM_EHIP. */
 int cham_attention(const cham_attn* a, const cham_heads* k, const cham_heads* v, int64_t Tk, const int32_t* cu_k,
                    void* ws, size_t ws_bytes, void* stream);
 

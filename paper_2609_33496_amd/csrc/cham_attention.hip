@@ -38,6 +38,7 @@ constexpr float kLog2e = 1.44269504f;
 constexpr float kGrow = 8.0f;    // few_kernel: the reference follows scores more than 2^8 above it
 constexpr float kVGrow = 16.0f;  // and the values' scale follows scales more than 16 times it
 
+constexpr int kNever = INT32_MAX / 2;  // steps that no sequence has: nothing is cut
 constexpr int kRowsTile = 128, kKeysTile = 64;  // of a workgroup of the tiled kernel and its step
 constexpr int kRowsFew = 16, kKeysFew = 128;    // of the single-token kernel (4 wavefronts x 32 keys)
 
@@ -149,11 +150,14 @@ CHAM_DEV bool find_piece(const AttnArgs& a, int at, int hk, bool tiles, Piece* p
     float work = 0.0f;
     Seq s{};
     int nt = 0;
-    for (int b0 = 0; b0 < B; b0 += kWave) {
-        if (b0 + lane < B) {
-            s = sequence<SRC>(a, b0 + lane);
-            nt = (s.nq * a.G + BM - 1) / BM;
-            work += (float)nt * (float)((s.nk + BN - 1) / BN);
+    if (B <= kWave || a.least < kNever) {
+#pragma unroll 4
+        for (int b0 = 0; b0 < B; b0 += kWave) {
+            if (b0 + lane < B) {
+                s = sequence<SRC>(a, b0 + lane);
+                nt = (s.nq * a.G + BM - 1) / BM;
+                work += (float)nt * (float)((s.nk + BN - 1) / BN);
+            }
         }
     }
     // more than its share of all steps, however the sum is rounded
@@ -1130,14 +1134,14 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     // to join).  A cache's sequences may be far longer than others: theirs are cut up to four times as many.
     if (!few && a.a.T * a.G / BM * a.Hk >= (int64_t)slots_of(few) * (SRC == kPacked ? 1 : 4)) {
         may_split = false;
-        a.least = INT32_MAX / 2;
+        a.least = kNever;
     }
     // Up to 1024 keys are one piece, of eight wavefronts: a step of theirs takes about 1.7 us, a second launch
     // 4 and 3 more on the host (one sequence of 700
     // tokens, 8 key heads, 16-bit pages of 16: 12.3 us, in pieces 7.2 and 4.2).
     if (few && blocks <= 8) {
         may_split = false;
-        a.least = INT32_MAX / 2;
+        a.least = kNever;
     }
     if (SRC == kPacked && !a.a.cu_q && !a.cu_k)  // every length is known here
         may_split = may_split && blocks > up(tiles * blocks * a.Hk, slots_of(few));
