@@ -664,9 +664,14 @@ typedef struct cham_attn {
                               q.p is refused)                                                 */
 } cham_attn;
 
+#define CHAM_ATTN_NO_WS 256
+#define CHAM_ATTN_NO_WS_ONE 1024
+
 /* Attention over packed keys and values k, v [Tk][Hk][D] of q's type: cu_k as cu_q, NULL: B
  * sequences of Tk / B rows.  ws: cham_attention_workspace_bytes(a, Hk) bytes, written before they are
- * read; calls that may overlap (two streams, two graphs) need workspaces of their own.
+ * read; calls that may overlap (two streams, two graphs) need workspaces of their own.  With at most
+ * CHAM_ATTN_NO_WS keys (Tk, or width * page) no call needs one, and ws may be NULL; nor does a
+ * cham_cache_attention of one query a sequence (cu_q NULL, T = B) with at most CHAM_ATTN_NO_WS_ONE.
  * Errors: CHAM_EINVAL (NULL, sizes, strides, alignment, T % B or Tk % B without cu_q or cu_k, scale,
  * o over q), CHAM_EFORMAT (types), CHAM_ESHAPE (D, H > 2^16, B >= 2^24, T Hq / Hk or Tk of 2^31 - 2^16 and
  * more, a token stride of k or v of 2^24 elements and more, or a launch of 2^32 lanes), CHAM_EWORKSPACE,

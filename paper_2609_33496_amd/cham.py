@@ -994,17 +994,20 @@ _NO_HEADS = _Heads()
 
 def _heads(t: torch.Tensor, name: str, T: int, D: int, dev, ty: int, H: int = -1) -> _Heads:
     """Check rows of heads [T, H, D] of type ty on dev, any strides along tokens and heads."""
-    at = t.get_device()
-    if at < 0 or at != dev.index:
+    if t.get_device() != dev.index:  # negative on the host
         raise ValueError(f"{name} must be a device tensor on {dev}")
     if _TYPES.get(t.dtype) != ty:
         raise ValueError(f"{name} is of type {t.dtype}, which does not fit the others")
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != T or shape[2] != D or (H >= 0 and shape[1] != H):
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError(f"{name} must be of shape (tokens, heads, D), got {tuple(shape)}")
+    n, h, d = shape
+    if n != T or d != D or (H >= 0 and h != H):
         raise ValueError(f"{name} must be of shape ({T}, {H if H >= 0 else 'heads'}, {D}), got {tuple(shape)}")
-    if stride[2] != 1 and D > 1:
+    token, head, one = t.stride()
+    if one != 1 and D > 1:
         raise ValueError(f"{name} must have unit stride along a head's elements")
-    return _Heads(t.data_ptr(), stride[0], stride[1], shape[1], ty)
+    return _Heads(t.data_ptr(), token, head, h, ty)
 
 
 def _float_type(t: torch.Tensor, name: str) -> int:
@@ -1185,7 +1188,10 @@ def cache_read(cache: Cache, table: torch.Tensor, cu: torch.Tensor, total: int, 
     return k_out, v_out
 
 
-def _attn(q, B, cu_q, causal, scale, out, Hk, ws, stream):
+_NO_WS, _NO_WS_ONE = 256, 1024  # CHAM_ATTN_NO_WS, CHAM_ATTN_NO_WS_ONE
+
+
+def _attn(q, B, cu_q, causal, scale, out, Hk, need_ws, ws, stream):
     """The descriptor, output and workspace of an attention call."""
     if q.dim() != 3:
         raise ValueError("q must be of shape (tokens, heads, D)")
@@ -1204,10 +1210,12 @@ def _attn(q, B, cu_q, causal, scale, out, Hk, ws, stream):
     cu = None if cu_q is None else _vector(cu_q, "cu_q", B + 1, torch.int32, dev)
     a = _Attn(B, T, D, int(bool(causal)), D ** -0.5 if scale is None else scale, 0, cu, qs, os)
     if ws is None:
+        if not need_ws:
+            return a, out, dev, None, 0
         ws = _empty(1, attention_workspace_bytes(D, dev), torch.uint8, dev, stream)
     elif ws.get_device() != dev.index or ws.dtype is not torch.uint8 or not ws.is_contiguous():
         raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
-    return a, out, dev, ws
+    return a, out, dev, ws.data_ptr(), ws.numel()
 
 
 _attn_ws = {}
@@ -1251,11 +1259,12 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, batch: Optio
             cu_k = cu_q
     if k.dim() != 3:
         raise ValueError("k and v must be of shape (tokens, heads, D)")
-    a, out, dev, ws = _attn(q, B, cu_q, causal, scale, out, k.shape[1], ws, stream)
-    Tk, ty = k.shape[0], a.q.type
+    Tk = k.shape[0]
+    a, out, dev, space, nb = _attn(q, B, cu_q, causal, scale, out, k.shape[1], Tk > _NO_WS, ws, stream)
+    ty = a.q.type
     ks, vs = _heads(k, "k", Tk, a.D, dev, ty), _heads(v, "v", Tk, a.D, dev, ty, k.shape[1])
     cu = None if cu_k is None else _vector(cu_k, "cu_k", B + 1, torch.int32, dev)
-    _check(_on_device(dev, stream, lib().cham_attention, a, ks, vs, Tk, cu, ws.data_ptr(), ws.numel()), "attention")
+    _check(_on_device(dev, stream, lib().cham_attention, a, ks, vs, Tk, cu, space, nb), "attention")
     return out
 
 
@@ -1271,10 +1280,11 @@ def cache_attention(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: to
     B = lens.shape[0]
     if cu_q is None and q.shape[0] != B:
         raise ValueError(f"without cu_q, q must hold one token of each of {B} sequences")
-    a, out, dev, ws = _attn(q, B, cu_q, True, scale, out, cache.H, ws, stream)
+    t, width = _table(table, B, q.device), table.shape[1]
+    need_ws = width * cache.page > (_NO_WS_ONE if cu_q is None else _NO_WS)
+    a, out, dev, space, nb = _attn(q, B, cu_q, True, scale, out, cache.H, need_ws, ws, stream)
     if cache.device != dev or cache.D != a.D:
         raise ValueError(f"the cache holds heads of {cache.D} on {cache.device}")
-    n, t = _vector(lens, "lens", B, torch.int32, dev), _table(table, B, dev)
-    _check(_on_device(dev, stream, lib().cham_cache_attention, a, cache._struct, t, table.shape[1], n, ws.data_ptr(),
-                      ws.numel()), "cache_attention")
+    n = _vector(lens, "lens", B, torch.int32, dev)
+    _check(_on_device(dev, stream, lib().cham_cache_attention, a, cache._struct, t, width, n, space, nb), "cache_attention")
     return out

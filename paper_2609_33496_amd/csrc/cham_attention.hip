@@ -493,22 +493,22 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         f16v s[2];
         const auto score = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            s[b] = f16v{};
+            for (int b = 0; b < 2; ++b) {
+                s[b] = f16v{};
 #pragma unroll
-            for (int t = 0; t < KS; ++t) {
-                s[b] = mma32<T>(*(const LdsU4*)(kb + 32 * b * L::CU * 16 + ((t << 5) ^ k_key)), q[t], s[b]);
-                if (SRC != kCodes && b == 0 && t < kLoads) load_k(t, next_k);
-            }
-            if constexpr (SRC == kCodes) {
+                for (int t = 0; t < KS; ++t) {
+                    s[b] = mma32<T>(*(const LdsU4*)(kb + 32 * b * L::CU * 16 + ((t << 5) ^ k_key)), q[t], s[b]);
+                    if (SRC != kCodes && b == 0 && t < kLoads) load_k(t, next_k);
+                }
+                if constexpr (SRC == kCodes) {
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const f4 k4 = *((const LdsF4*)lds_ks[buf] + 8 * b + i / 2 + h);
+                    for (int i = 0; i < 16; i += 4) {
+                        const f4 k4 = *((const LdsF4*)lds_ks[buf] + 8 * b + i / 2 + h);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[b][i + j] *= k4[j];
+                        for (int j = 0; j < 4; ++j) s[b][i + j] *= k4[j];
+                    }
                 }
             }
-        }
         };
         const int rel = lim - key0 - 4 * h;
         const auto seen = [&](int b, int i) {
@@ -1113,7 +1113,6 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     const int BM = few ? kRowsFew : kRowsTile, BN = few ? kKeysFew : kKeysTile;
     const Space sp = space(&a.a, few);
     if (a.a.T == 0 || a.a.B == 0) return CHAM_OK;
-    if (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)sp.bytes) return CHAM_EWORKSPACE;
     a.G = a.a.q.H / a.Hk;
     a.nq = (int)(a.a.T / a.a.B);
     a.c2 = a.a.scale * kLog2e;
@@ -1122,7 +1121,7 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     while ((1 << l) < a.G) ++l;
     a.group_shift = 31 + l;
     a.group_mul = (uint32_t)((((uint64_t)1 << a.group_shift) + a.G - 1) / a.G);
-    a.least = few ? 1 : 4;
+    a.least = few ? 1 : CHAM_ATTN_NO_WS / kKeysTile;
     a.most = (int)sp.pieces;
     a.part_o = (float*)ws;
     a.part_s = a.part_o + sp.pieces * sp.rows * a.a.D;
@@ -1134,17 +1133,15 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     // to join).  A cache's sequences may be far longer than others: theirs are cut up to four times as many.
     if (!few && a.a.T * a.G / BM * a.Hk >= (int64_t)slots_of(few) * (SRC == kPacked ? 1 : 4)) {
         may_split = false;
-        a.least = kNever;
     }
     // Up to 1024 keys are one piece, of eight wavefronts: a step of theirs takes about 1.7 us, a second launch
     // 4 and 3 more on the host (one sequence of 700
     // tokens, 8 key heads, 16-bit pages of 16: 12.3 us, in pieces 7.2 and 4.2).
-    if (few && blocks <= 8) {
-        may_split = false;
-        a.least = kNever;
-    }
+    if (few && blocks <= CHAM_ATTN_NO_WS_ONE / kKeysFew) may_split = false;
     if (SRC == kPacked && !a.a.cu_q && !a.cu_k)  // every length is known here
         may_split = may_split && blocks > up(tiles * blocks * a.Hk, slots_of(few));
+    if (!may_split) a.least = kNever;  // the device is to find the same
+    if (may_split && (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)sp.bytes)) return CHAM_EWORKSPACE;
     if (a.a.q.type == CHAM_T_F16) return launch_d<CHAM_T_F16, SRC>(a, few, tiles, may_split, s);
     return launch_d<CHAM_T_BF16, SRC>(a, few, tiles, may_split, s);
 }

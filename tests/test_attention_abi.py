@@ -135,9 +135,9 @@ def test_attention_other_refusals():
     assert L.cham_attention(_attn(B=3), h, h, 4, None, 256, need, None) == cham.EINVAL  # keys of 4 / 3 rows
     assert L.cham_attention(a, h, h, 3, 66, 256, need, None) == cham.EINVAL
     assert L.cham_attention(a, _heads(token=1 << 24), h, 3, None, 256, need, None) == cham.ESHAPE
-    assert L.cham_attention(a, h, h, 3, None, None, need, None) == cham.EWORKSPACE
-    assert L.cham_attention(a, h, h, 3, None, 320, need, None) == cham.EWORKSPACE
-    assert L.cham_attention(_attn(T=1), h, h, 3, None, 256, 0, None) == cham.EWORKSPACE
+    assert L.cham_attention(a, h, h, 1000, None, None, need, None) == cham.EWORKSPACE
+    assert L.cham_attention(a, h, h, 1000, None, 320, need, None) == cham.EWORKSPACE
+    assert L.cham_attention(_attn(T=1), h, h, 1000, None, 256, 0, None) == cham.EWORKSPACE
     assert L.cham_attention(_attn(o=_heads()), h, h, 3, None, 256, need, None) == cham.EINVAL  # over its queries
     c = _cache()
     assert L.cham_cache_attention(a, c, None, 2, 64, 256, need, None) == cham.EINVAL
@@ -146,7 +146,7 @@ def test_attention_other_refusals():
     assert L.cham_cache_attention(a, c, 64, BIG, 64, 256, need, None) == cham.ESHAPE
     assert L.cham_cache_attention(a, _cache(D=32), 64, 2, 64, 256, need, None) == cham.EINVAL
     assert L.cham_cache_attention(a, _cache(type=1, ks=None, vs=None), 64, 2, 64, 256, need, None) == cham.EFORMAT
-    assert L.cham_cache_attention(a, c, 64, 2, 64, 256, 1024, None) == cham.EWORKSPACE
+    assert L.cham_cache_attention(a, c, 64, 200, 64, 256, 1024, None) == cham.EWORKSPACE
 
 
 def test_empty_calls():
