@@ -14,8 +14,9 @@ class AttentionBlock:
     """y = attention(q, k, v) W_out^T with the heads of (q, k, v) = n W_qkv^T, n = rms_norm(x +
     residual) * norm_weight; q and k are normed (where q_weight and k_weight are given) and turned (freq).
 
-    x is float16 or bfloat16.  W_qkv [(heads + 2 kv_heads) D, K] and W_out [K, heads D] are brought to the block format once, on the
-    current stream: a call on another one has to wait for it.  pow2 and exact are FeedForward's."""
+    x is float16 or bfloat16.  W_qkv [(heads + 2 kv_heads) D, K] and W_out [K, heads D] are brought to the
+    block format once, on the current stream: a call on another one has to wait for it.  pow2 and exact are
+    FeedForward's."""
 
     def __init__(self, w_qkv: torch.Tensor, w_out: torch.Tensor, heads: int, kv_heads: Optional[int] = None,
                  norm_weight: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,

@@ -1131,12 +1131,10 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     // Tiles that fill the card twice are not cut: the long ones start first, and what a cut saves at the end is
     // less than the partial outputs and the second launch cost (8101 tokens, 2056 tiles: 44 us with nothing
     // to join).  A cache's sequences may be far longer than others: theirs are cut up to four times as many.
-    if (!few && a.a.T * a.G / BM * a.Hk >= (int64_t)slots_of(few) * (SRC == kPacked ? 1 : 4)) {
-        may_split = false;
-    }
+    if (!few && a.a.T * a.G / BM * a.Hk >= (int64_t)slots_of(few) * (SRC == kPacked ? 1 : 4)) may_split = false;
     // Up to 1024 keys are one piece, of eight wavefronts: a step of theirs takes about 1.7 us, a second launch
-    // 4 and 3 more on the host (one sequence of 700
-    // tokens, 8 key heads, 16-bit pages of 16: 12.3 us, in pieces 7.2 and 4.2).
+    // 4 and 3 more on the host (one sequence of 700 tokens, 8 key heads, 16-bit pages of 16: 12.3 us, in pieces
+    // 7.2 and 4.2).
     if (few && blocks <= CHAM_ATTN_NO_WS_ONE / kKeysFew) may_split = false;
     if (SRC == kPacked && !a.a.cu_q && !a.cu_k)  // every length is known here
         may_split = may_split && blocks > up(tiles * blocks * a.Hk, slots_of(few));
