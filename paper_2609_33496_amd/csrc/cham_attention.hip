@@ -30,7 +30,7 @@ namespace {
 // their product with the values.  Beside 16-bit values they take those's type, and their sum adds the rounded
 // ones, so that a key that outweighs the others comes out as it is (bfloat16 errors against 64 bits stay below 1.5
 // times those of a binary32 form, 0.0017).  E4M3 values are exact in float16, so there they take
-// float16 whatever the queries' type, after the values' scale over the largest of them, which keeps them in
+// float16 whatever the queries' type, after the values' scale and a factor of the row's own, which keeps them in
 // its range; the sum adds them unrounded (but for float16 outputs of single tokens).
 enum { kPacked, kPages, kCodes };
 
@@ -432,9 +432,6 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
             load_v(i, vb);
         }
     };
-    // kCodes: o is the sum over vref, and vs hold the values' scales over it.  All wavefronts see all
-    // scales, so they have one vref; it follows the largest finite scale of a step.
-    float vref = 0.0f, vinv = 0.0f, v_fall = 1.0f;
     const auto store = [&](int buf, Lds* kb, Lds* vb) __attribute__((always_inline)) {
         if constexpr (SRC == kCodes) {
 #pragma unroll
@@ -448,26 +445,16 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                     *(LdsU4*)(vb + 16 * (row + ((c + 1) ^ L::key_v(in)))) = widen8<VT>(rv[i][2], rv[i][3]);
                 }
             }
-            const float kx = held ? k_scale : 0.0f, vx = held ? v_scale : 0.0f;
-            uint32_t m = __float_as_uint(vx) & 0x7fffffffu;
-            m = m < kInfBits ? m : 0;
-            m = dpp_maxu<0x140>(dpp_maxu<0x141>(dpp_maxu<0x4E>(dpp_maxu<0xB1>(m))));
-            const float vm = __uint_as_float(uniform(__float_as_uint(max_halves(max_rows16(__uint_as_float(m))))));
-            v_fall = 1.0f;
-            if (vm > kVGrow * vref) {
-                const float next = fmaxf(vm, FLT_MIN);
-                v_fall = vref / next;
-                vref = next;
-                vinv = 1.0f / next;
-            }
-            if (wave == 0) *((LdsFloat*)lds_ks[buf] + lane) = kx * a.c2;
-            if (wave == 1) *((LdsFloat*)lds_vs[buf] + lane) = vx * vinv;
+            if (wave == 0) *((LdsFloat*)lds_ks[buf] + lane) = held ? k_scale * a.c2 : 0.0f;
+            if (wave == 1) *((LdsFloat*)lds_vs[buf] + lane) = held ? v_scale : 0.0f;
         }
     };
 
     f16v o[DB] = {};
     // the reference (in powers of two; none before a score), and this lane's part of the sum
     float m = -INFINITY, l = 0.0f;
+    // kCodes: o is the sum times 2^r, a factor of each row's own
+    int r = 0;
     // where the lane reads: row col of the keys, its chunks 2 t + h; rows 4 h + (lane & 15) / 4 of the
     // values, 8 bytes of their chunks 4 d ..
     const int k_at = col * L::CU * 16, k_key = (h ^ L::key_k(col)) << 4;
@@ -476,12 +463,20 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
 
     // The reference is set kAbove powers of two above the largest score and stays until a lane's 32
     // probabilities add up to kBig: where none has, none is as large.  float16 holds a probability's 11 bits
-    // between 2^-14 and 2^16 (2^12 before the values' scale, which may be kVGrow times the reference's); binary32
+    // between 2^-14 and 2^16; binary32
     // sums of bfloat16 ones and values hold 24 bits for values from 2^-78 up and stay finite for the largest.  So
     // a reference moves where scores grow by 2^20 (2^16, 2^25).  4096 x 4096, scores of 5 nats' standard deviation:
     // 119 us a piece where it moves at 2^8, which is every few steps, 91 so.
-    constexpr float kAbove = VT == CHAM_T_F16 ? 6.0f : 24.0f;
-    constexpr float kBig = SRC == kCodes ? 1024.0f : T == CHAM_T_F16 ? 16384.0f : 2.0f;
+    constexpr float kAbove = T == CHAM_T_F16 ? 6.0f : 24.0f;
+    constexpr float kBig = SRC == kCodes ? 0x1p20f : T == CHAM_T_F16 ? 16384.0f : 2.0f;
+    // kCodes: what is rounded to float16 is a probability times its value's scale, and what counts among those of a
+    // row is how they compare with the row's largest, whatever the probabilities and the scales are
+    // alone (a scale may be anything in binary32).  2^r brings the largest to 2^kTop when it is set, so those down to
+    // 2^-16 of it keep 11 bits and none above 2^-27 is lost; it falls when one is past float16, 2^14 larger.
+    // Keys that the row does not see are 0 there and have no say in it; nor have other rows.  Chunks of 1100 new
+    // tokens over 36000, three draws: 300 to 338 us with 2^6, 295 to 312 with 2^2, 296 to 303 with 1.
+    constexpr int kTop = 2;
+    constexpr uint32_t kFull = 0x7c00;  // an infinity
 
     // One step's keys against the wavefront's rows; masked: some row does not see all of them.  The
     // outputs' sums are touched in three places only, whatever branch made the probabilities, so that they
@@ -514,10 +509,21 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         const auto seen = [&](int b, int i) {
             return 32 * b + 2 * (i & ~3) + (i & 3) < rel && !(no_page >> (2 * b + (i >> 3)) & 1);
         };
+        const auto mask = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!seen(b, i)) s[b][i] = -INFINITY;
+        };
         // their probabilities over the reference, and the lane's sum of them
         u4 pr[4];
-        const auto weigh = [&](float ref) __attribute__((always_inline)) {
+        typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+        ushort2v most = {0, 0};  // kCodes: the largest (as integers: none is below 0)
+        const auto weigh = [&](float ref, bool hide) __attribute__((always_inline)) {
             float sum[2] = {0.0f, 0.0f};
+            const float by = __uint_as_float((uint32_t)(r + 127) << 23);
+            most = ushort2v{0, 0};
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -531,10 +537,15 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                     if constexpr (SRC == kCodes) {
                         const f4 v4 = *((const LdsF4*)lds_vs[buf] + 8 * b + i / 2 + h);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) e[j] *= v4[j];
+                        for (int j = 0; j < 4; ++j) {
+                            e[j] = e[j] * v4[j] * by;
+                            if (hide && !seen(b, i + j)) e[j] = 0.0f;  // its scale may be anything, NaN too
+                        }
                     }
-                    const uint32_t lo = narrow<VT>(e[0], e[1]), hi = narrow<VT>(e[2], e[3]);
+                    uint32_t lo = narrow<VT>(e[0], e[1]), hi = narrow<VT>(e[2], e[3]);
+                    if constexpr (SRC == kCodes) asm("" : "+v"(lo), "+v"(hi));  // or each is rounded twice, for `most` too
                     if constexpr (SRC != kCodes) sum[0] = add2<T>(hi, add2<T>(lo, sum[0]));
+                    else most = __builtin_elementwise_max(most, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, lo), __builtin_bit_cast(ushort2v, hi)));
                     pr[2 * b + i / 8][i % 8 / 2] = lo;
                     pr[2 * b + i / 8][i % 8 / 2 + 1] = hi;
                 }
@@ -545,46 +556,62 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         if (masked) {
             asm volatile("; some keys hidden");  // two forms, which the compiler is not to join again
             score();
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!seen(b, i)) s[b][i] = -INFINITY;
-            sum = weigh(m);
+            mask();
+            sum = weigh(m, true);
             asm volatile("; some keys hidden");
         } else {
             asm volatile("; all keys seen");
             score();
-            sum = weigh(m);
+            sum = weigh(m, false);
             asm volatile("; all keys seen");
         }
-        if (__builtin_expect(__any(!(sum < kBig)), 0)) {  // a probability may be large, or there is no reference yet
+        bool big = !(sum < kBig);  // a probability may be large, or there is no reference yet
+        if constexpr (SRC == kCodes) big = big || max((uint32_t)most[0], (uint32_t)most[1]) >= kFull;
+        if (__builtin_expect(__any(big), 0)) {
             // every row's reference follows its largest score, and its probabilities with it
+            if constexpr (SRC == kCodes) {  // the scores once more: kept until here they would not fit the registers
+                asm volatile("" ::: "memory");
+                score();
+                if (masked) mask();
+            }
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
             if constexpr (SRC != kCodes) top *= a.c2;
             // (a row's own sums decide, so that no other row's keys change how it rounds)
-            const bool mine = max_halves(sum < kBig ? 0.0f : 1.0f) > 0.0f;
-            const float next = mine ? fmaxf(m, max_halves(top) + kAbove) : m;
+            const bool mine = max_halves(big ? 1.0f : 0.0f) > 0.0f;
+            top = max_halves(top);
+            // (codes: whole numbers, so that factors between references are exact)
+            const float next = mine ? fmaxf(m, SRC == kCodes ? __builtin_ceilf(top) : top + kAbove) : m;
             f = next > m ? __builtin_amdgcn_exp2f(m - next) : 1.0f;
-            m = next;
             l *= f;
-            sum = weigh(m == -INFINITY ? 0.0f : m);
+            if constexpr (SRC == kCodes) {
+                float w = 0.0f;  // the row's largest product in this step; scales that are not finite have no say
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const f4 v4 = *((const LdsF4*)lds_vs[buf] + 8 * b + i / 2 + h);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float x = fabsf(__builtin_amdgcn_exp2f(s[b][i + j] - (next == -INFINITY ? 0.0f : next)) * v4[j]);
+                            w = x < INFINITY ? fmaxf(w, x) : w;
+                        }
+                    }
+                w = fmaxf(max_halves(w), FLT_MIN);
+                // products behind the reference's move keep their place or fall; r grows with it, at most
+                const float by = next - m;
+                int to = kTop + 1 - __builtin_amdgcn_frexp_expf(w);
+                if (by < 512.0f) to = min(to, r + (int)by);
+                to = mine ? min(to, 126) : r;
+                f = __builtin_amdgcn_ldexpf(f, to - r);
+                r = to;
+            }
+            m = next;
+            sum = weigh(m == -INFINITY ? 0.0f : m, masked);
             moved = 1;
         }
         l += sum;
-        if constexpr (SRC == kCodes) {
-            moved |= uniform(v_fall != 1.0f);
-            f *= v_fall;
-            if (masked) {  // a scale that is not finite
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        pr[t][j] &= (seen(t >> 1, 8 * (t & 1) + 2 * j) ? 0xffffu : 0) | (seen(t >> 1, 8 * (t & 1) + 2 * j + 1) ? 0xffff0000u : 0);
-            }
-        }
         moved = uniform(moved);
         asm volatile("" : "+s"(moved));  // a branch of its own
         if (__builtin_expect(moved, 0)) {
@@ -704,7 +731,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
 
     if (!live || my_row >= rows || (p.pieces > 1 && (unsigned)p.index >= (unsigned)a.most)) return;
     l = add_halves(l);
-    const float f = l == 0.0f ? 0.0f : 1.0f / l;  // before the values' scale: the product stays in range
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;  // before 2^-r: the product stays in range
     m = m == -INFINITY ? 0.0f : m;
     const int64_t o_at = (int64_t)(p.q0 + token) * a.a.o.token + (int64_t)head * a.a.o.head;
     float* po = a.part_o + ((int64_t)p.index * kRowsTile + wave * 32 + col) * D;
@@ -714,11 +741,11 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         for (int i = 0; i < 16; i += 4) {
             const int e = 32 * d + 2 * i + 4 * h;
             if (e >= D) continue;
-            float r[4];
+            float y[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r[j] = o[d][i + j] * f * (SRC == kCodes ? vref : 1.0f);
-            if (p.pieces == 1) put4<T>(a.a.o, o_at + e, r[0], r[1], r[2], r[3]);
-            else *(f4*)(po + e) = f4{r[0], r[1], r[2], r[3]};
+            for (int j = 0; j < 4; ++j) y[j] = SRC == kCodes ? __builtin_amdgcn_ldexpf(o[d][i + j] * f, -r) : o[d][i + j] * f;
+            if (p.pieces == 1) put4<T>(a.a.o, o_at + e, y[0], y[1], y[2], y[3]);
+            else *(f4*)(po + e) = f4{y[0], y[1], y[2], y[3]};
         }
     if (p.pieces > 1 && h == 0)
         *(float2*)(a.part_s + ((int64_t)p.index * kRowsTile + wave * 32 + col) * 2) = make_float2(m, l);

@@ -1,0 +1,156 @@
+"""The attention operators where scores, scales and values lie far apart, against plain forms in 64 bits.
+
+A key counts as much as its probability times its value's scale, whatever the other keys hold: not those that a
+row does not see, nor those whose probability is next to nothing."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_33496_amd import cham
+from test_gpu_attention import DEV, E4, HALF, INF, TINY, U, _cached_case, _gather, _ints, _within, case
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+def _want(q, k, v, scale, causal, vscale=None):
+    """(o, bound) of one sequence in 64 bits; q [nq, Hq, D], k, v [nk, Hk, D], vscale [nk, Hk]: the scales of v's codes.
+
+    With t = scale s / ln 2 relative to the row's largest, p = 2^t and l = sum p: a score's sum of D products is off by
+    at most D 2^-23 sum |q k|, a scale rounds once more; the exponent's argument by a rounding of a number up
+    to |t| + 32 and of the reference; the exponential by 2^-22.  p (over codes p times the scale) is rounded to
+    bfloat16, or to binary16 beside float16 and codes: u relative, or half a subnormal step, 2^-25, where the
+    row's largest is 2^4 and more (over codes 2^2): 2^-29 (2^-27) of that largest.  Where the sum adds the rounded ones, it is off by as much.
+    Sums of n terms take n 2^-24, two of them."""
+    nq, Hq, D = q.shape
+    nk, Hk = k.shape[:2]
+    dt = q.dtype
+    half = vscale is not None or dt == F16
+    u = HALF[F16] if half else HALF[BF16]
+    q, k, v = q.double(), k.double(), v.double()
+    o, bound = torch.zeros_like(q), torch.zeros_like(q)
+    hidden = torch.zeros(nq, nk, dtype=torch.bool, device=DEV)
+    if causal:
+        hidden = torch.arange(nk, device=DEV)[None] > (nk - nq) + torch.arange(nq, device=DEV)[:, None]
+    for h in range(Hq):
+        j = h // (Hq // Hk)
+        c = scale * math.log2(math.e)
+        kk, vv = k[:, j], v[:, j]
+        t = (q[:, h] @ kk.t() * c).masked_fill(hidden, -INF)
+        top = t.amax(1, keepdim=True)
+        p = torch.exp2(t - top)
+        off = math.log(2) * (c * (D + 2) * 2 * U * (q[:, h].abs() @ kk.abs().t()) +
+                             U * ((t - top).abs().nan_to_num(posinf=0.0) + 32 + 2 * top.abs())) + 2.0 ** -21
+        l = p.sum(1, keepdim=True)
+        w = p if vscale is None else p * vscale[:, j].double()
+        codes = vv.abs() if vscale is None else vv.abs() / vscale[:, j:j + 1].double()
+        tiny = 0.0 if not half else 2.0 ** -29 if vscale is None else 2.0 ** -27
+        o[:, h] = p @ vv / l
+        b = ((p * off) @ vv.abs() + p @ vv.abs() * (u + (8 + 2 * nk) * U) +
+             tiny * w.amax(1, keepdim=True) * ((~hidden).double() @ codes)) / l
+        b += o[:, h].abs() * (((p * off).sum(1, keepdim=True) + (tiny * nk if vscale is None else 0.0)) / l + (nk + 8) * U + u)
+        bound[:, h] = (b + TINY[dt] + HALF[dt] * (o[:, h].abs() + b)) * 1.02
+    return o, bound
+
+
+def _scales(c, table, n):
+    ids = table[0, :-(-n // c.page)].long()
+    return c.v_scale[ids].transpose(1, 2).reshape(-1, c.H)[:n]
+
+
+def _check(got, q, c, table, n, scale=None):
+    """got: one sequence of n tokens, q its newest."""
+    (k, _), (v, _) = _gather(c, table, 0, n, "k"), _gather(c, table, 0, n, "v")
+    o, bound = _want(q, k, v, c.D ** -0.5 if scale is None else scale, True, None if c.v_scale is None else _scales(c, table, n))
+    _within(got, o, bound)
+
+
+def _place(c, table, t):
+    return int(table[0, t // c.page]), t % c.page
+
+
+# ---------------------------------------------------------------------------------------------
+# scales of values
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("factor", [20.0, 2.0 ** 12, 2.0 ** 21])
+@pytest.mark.parametrize("n,lq,at", [(128, 128, 40), (128, 128, 70), (128, 128, 100), (200, 150, 199), (1000, 128, 912), (5000, 130, 4990), (300, 64, 270)])
+def test_later_scales_do_not_change_earlier_rows(dt, factor, n, lq, at):
+    """A later token of the same chunk with a larger scale of its value: in a step that some wavefronts have no
+    row for, and hidden among keys that they see."""
+    case(f"later scales {dt} factor={factor} n={n} lq={lq} at={at}")
+    q, c, table = _cached_case(21, [lq], [n], 2, 1, 64, 16, dt, E4)
+    c.v_scale.mul_(2.0 ** -8)  # all outputs are within float16
+    cu = _ints([0, lq])
+    want = cham.cache_attention(q, c, table, _ints([n]), cu)
+    page, place = _place(c, table, at)
+    c.v_scale[page, :, place] *= factor
+    got = cham.cache_attention(q, c, table, _ints([n]), cu)
+    row = at - (n - lq)  # the first that sees it
+    assert torch.equal(got[:row], want[:row])
+    _check(want[:row], q[:row], c, table, n - lq + row)
+    _check(got, q, c, table, n)
+
+
+def _steered(seed, dt, cache, lq, score, Hq=4, Hk=2, D=64, page=16):
+    """One sequence whose token t has the score `score[t]` (float tensor) for every query, scale 1."""
+    n = score.numel()
+    q, c, table = _cached_case(seed, [lq], [n], Hq, Hk, D, page, dt, cache)
+    q.zero_()
+    q[..., 0] = 1.0
+    ids = table[0, torch.arange(n, device=DEV) // page].long()
+    at = torch.arange(n, device=DEV) % page
+    c.k.view(torch.uint8).zero_()
+    if cache is E4:
+        c.k.view(torch.uint8)[ids, :, at, 0] = torch.where(score < 0, 0xfe, 0x7e).to(torch.uint8)[:, None]  # -448 and 448
+        c.k_scale[ids, :, at] = (score.abs() / 448.0)[:, None]
+    else:
+        c.k[ids, :, at, 0] = score.to(cache)[:, None]
+    return q, c, table, ids, at
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("chunk", [True])
+@pytest.mark.parametrize("which", ["first", "middle", "half", "all but the last", "every third"])
+def test_large_scales_of_small_probabilities(dt, chunk, which):
+    """Keys 40 nats below the others with scales of 2^30 times theirs: they count for 2^-27."""
+    case(f"large scales of small probabilities {dt} chunk={chunk} {which}")
+    n = 700
+    t = torch.arange(n, device=DEV)
+    low = {"first": t == 0, "middle": t == n // 2, "half": t < n // 2, "all but the last": t < n - 9, "every third": t % 3 == 0}[which]
+    q, c, table, ids, at = _steered(22, dt, E4, 9 if chunk else 1, torch.where(low, -40.0, 0.0))
+    c.v_scale.fill_(2.0 ** -9)
+    c.v_scale[ids[low], :, at[low]] = 2.0 ** 21
+    o = cham.cache_attention(q, c, table, _ints([n]), _ints([0, 9]) if chunk else None, scale=1.0)
+    _check(o, q, c, table, n, 1.0)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("chunk", [True])
+@pytest.mark.parametrize("n,power,scale", [(32, 6.1, 19), (1000, 6.1, 19), (10000, 13.1, 12), (10000, 0.0, 22), (300, 2.0, 30)])
+def test_small_scales_of_large_sums(dt, chunk, n, power, scale):
+    """One value of scale 1 and n - 1 of scale 2^-scale, whose probabilities are 2^-power of its: they count in
+    the sum alone."""
+    case(f"small scales {dt} chunk={chunk} n={n} power={power} scale={scale}")
+    score = torch.full((n,), -power * math.log(2), device=DEV)
+    score[0] = 0.0
+    q, c, table, ids, at = _steered(23, dt, E4, 3 if chunk else 1, score)
+    c.v_scale.fill_(2.0 ** -scale)
+    c.v_scale[ids[0], :, at[0]] = 1.0
+    o = cham.cache_attention(q, c, table, _ints([n]), _ints([0, 3]) if chunk else None, scale=1.0)
+    _check(o, q, c, table, n, 1.0)
+
+
+@pytest.mark.parametrize("chunk", [True])
+def test_scales_and_scores_that_wander(chunk):
+    """Scores and scales that both run over dozens of powers of two, apart and together."""
+    case(f"wandering chunk={chunk}")
+    n = 2000
+    t = torch.arange(n, device=DEV).float()
+    for a, b in ((0.01, 0.0), (0.0, 0.01), (0.02, 0.013), (0.013, -0.02), (-0.02, 0.021)):
+        score = 60.0 * torch.sin(a * t) - (10.0 if a else 0.0)
+        q, c, table, ids, at = _steered(24, BF16, E4, 20 if chunk else 1, score)
+        c.v_scale[ids, :, at] = torch.exp2(80.0 * torch.sin(b * t))[:, None]
+        o = cham.cache_attention(q, c, table, _ints([n]), _ints([0, 20]) if chunk else None, scale=1.0)
+        _check(o, q, c, table, n, 1.0)
