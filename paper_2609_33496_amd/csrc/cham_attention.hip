@@ -35,8 +35,23 @@ namespace {
 enum { kPacked, kPages, kCodes };
 
 constexpr float kLog2e = 1.44269504f;
-constexpr float kGrow = 8.0f;    // few_kernel: the reference follows scores more than 2^8 above it
-constexpr float kVGrow = 16.0f;  // and the values' scale follows scales more than 16 times it
+constexpr float kGrow = 8.0f;  // few_kernel: the reference follows scores more than 2^8 above it
+
+// kCodes: what is rounded to float16 is a probability times its value's scale, and what counts among those of a
+// row is how they compare with the row's largest, whatever the probabilities and the scales are
+// alone (a scale may be anything in binary32).  2^r brings the largest to 2^kTop when it is set, so those down to
+// 2^-16 of it keep 11 bits and none above 2^-27 is lost; it falls when one is past float16, 2^14 larger.
+// Keys that the row does not see are 0 there and have no say in it; nor have other rows.  Chunks of 1100 new
+// tokens over 36000, three draws: 300 to 338 us with 2^6, 295 to 312 with 2^2, 296 to 303 with 1.
+constexpr int kTop = 2;
+constexpr float kCodesGrow = 20.0f;  // log2 of how far probabilities may be above 1: only binary32 holds them alone
+// The next r: of a row whose largest product is w where its reference moves up by `up`, a whole number or
+// infinite.  Products behind the move keep their place or fall, so r grows with it at most.
+CHAM_DEV int next_r(int r, float up, float w) {
+    const int to = min(kTop + 1 - __builtin_amdgcn_frexp_expf(fmaxf(w, FLT_MIN)), 126);
+    return up < 512.0f ? min(to, r + (int)up) : to;
+}
+CHAM_DEV float two_to(int r) { return __uint_as_float((uint32_t)(r + 127) << 23); }  // -126 <= r <= 127
 
 constexpr int kNever = INT32_MAX / 2;  // steps that no sequence has: nothing is cut
 constexpr int kRowsTile = 128, kKeysTile = 64;  // of a workgroup of the tiled kernel and its step
@@ -469,14 +484,6 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     // 119 us a piece where it moves at 2^8, which is every few steps, 91 so.
     constexpr float kAbove = T == CHAM_T_F16 ? 6.0f : 24.0f;
     constexpr float kBig = SRC == kCodes ? 0x1p20f : T == CHAM_T_F16 ? 16384.0f : 2.0f;
-    // kCodes: what is rounded to float16 is a probability times its value's scale, and what counts among those of a
-    // row is how they compare with the row's largest, whatever the probabilities and the scales are
-    // alone (a scale may be anything in binary32).  2^r brings the largest to 2^kTop when it is set, so those down to
-    // 2^-16 of it keep 11 bits and none above 2^-27 is lost; it falls when one is past float16, 2^14 larger.
-    // Keys that the row does not see are 0 there and have no say in it; nor have other rows.  Chunks of 1100 new
-    // tokens over 36000, three draws: 300 to 338 us with 2^6, 295 to 312 with 2^2, 296 to 303 with 1.
-    constexpr int kTop = 2;
-    constexpr uint32_t kFull = 0x7c00;  // an infinity
 
     // One step's keys against the wavefront's rows; masked: some row does not see all of them.  The
     // outputs' sums are touched in three places only, whatever branch made the probabilities, so that they
@@ -522,7 +529,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
         ushort2v most = {0, 0};  // kCodes: the largest (as integers: none is below 0)
         const auto weigh = [&](float ref, bool hide) __attribute__((always_inline)) {
             float sum[2] = {0.0f, 0.0f};
-            const float by = __uint_as_float((uint32_t)(r + 127) << 23);
+            const float by = two_to(r);
             most = ushort2v{0, 0};
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -566,7 +573,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
             asm volatile("; all keys seen");
         }
         bool big = !(sum < kBig);  // a probability may be large, or there is no reference yet
-        if constexpr (SRC == kCodes) big = big || max((uint32_t)most[0], (uint32_t)most[1]) >= kFull;
+        if constexpr (SRC == kCodes) big = big || max((uint32_t)most[0], (uint32_t)most[1]) >= 0x7c00;
         if (__builtin_expect(__any(big), 0)) {
             // every row's reference follows its largest score, and its probabilities with it
             if constexpr (SRC == kCodes) {  // the scores once more: kept until here they would not fit the registers
@@ -598,12 +605,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                             w = x < INFINITY ? fmaxf(w, x) : w;
                         }
                     }
-                w = fmaxf(max_halves(w), FLT_MIN);
-                // products behind the reference's move keep their place or fall; r grows with it, at most
-                const float by = next - m;
-                int to = kTop + 1 - __builtin_amdgcn_frexp_expf(w);
-                if (by < 512.0f) to = min(to, r + (int)by);
-                to = mine ? min(to, 126) : r;
+                w = max_halves(w);
+                const int to = mine ? next_r(r, next - m, w) : r;
                 f = __builtin_amdgcn_ldexpf(f, to - r);
                 r = to;
             }
@@ -769,7 +772,8 @@ struct Few {
     static constexpr int kUnits = SRC == kCodes ? ND : 2 * ND;                   // chunks of a row of values
     static constexpr int kVLoads = (32 * kUnits + kWave - 1) / kWave;
     u4 v[NW][32][SV];
-    float m[NW][kRowsFew], l[NW][kRowsFew], vref[NW];
+    float m[NW][kRowsFew], l[NW][kRowsFew];
+    int r[NW][kRowsFew];
 };
 
 template <int T, int ND, int SRC, int NW>
@@ -838,8 +842,9 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
     };
 
     f4 o[ND] = {};
-    float m = 0.0f, l = 0.0f, vref = 0.0f, vinv = 0.0f;
+    float m = 0.0f, l = 0.0f;
     bool any = false;
+    int r = 0;  // kCodes: o is the sum times 2^r, see kTop
     u4(&vl)[32][L::SV] = lds.v[wave];
     const int end = min(p.end * kKeys, p.nk);
     int key0 = p.first * kKeys + 32 * wave;
@@ -888,61 +893,82 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
         top *= a.c2;
-        if (__any(top > m + kGrow || (!any && top > -INFINITY))) {
-            top = max_halves(max_rows16(top));
-            if (top > -INFINITY && (!any || top > m)) {
-                const float f = any ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
-                m = top;
-                any = true;
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < ND; ++d) o[d] *= f;
-            }
-        }
-        if constexpr (SRC == kCodes) {
-            float vm = 0.0f;
+        float e[2][4], w[2][4];  // probabilities; kCodes: times their scales and 2^r
+        const auto weigh = [&]() __attribute__((always_inline)) {
+            const float by = two_to(r);
+            float most = 0.0f;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = fabsf(vs[t][i]);
-                    vm = x < INFINITY ? fmaxf(vm, x) : vm;
+                    e[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.c2, -m));
+                    if constexpr (SRC == kCodes) {
+                        w[t][i] = e[t][i] * vs[t][i] * by;
+                        most = fmaxf(most, w[t][i]);
+                    }
                 }
-            if (__any(vm > kVGrow * vref)) {  // vref is one for the wavefront: its columns share the values
-                vm = fmaxf(max_halves(max_rows16(vm)), FLT_MIN);
-                const float f = vref / vm;
-                vref = vm;
-                vinv = 1.0f / vm;
+            return most;
+        };
+        if constexpr (SRC == kCodes) {
+            const bool past = weigh() >= 65520.0f;  // infinite in float16
+            const bool big = past || top > m + kCodesGrow || (!any && top > -INFINITY);
+            if (__any(big)) {
+                const bool mine = max_halves(max_rows16(big ? 1.0f : 0.0f)) > 0.0f;
+                top = max_halves(max_rows16(top));
+                const float next = mine && top > -INFINITY ? (any ? fmaxf(m, __builtin_ceilf(top)) : __builtin_ceilf(top)) : m;
+                float most = 0.0f;
 #pragma unroll
-                for (int d = 0; d < ND; ++d) o[d] *= f;
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = fabsf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.c2, -next)) * vs[t][i]);
+                        most = x < INFINITY ? fmaxf(most, x) : most;
+                    }
+                most = max_halves(max_rows16(most));
+                const int to = mine ? next_r(r, any ? next - m : INFINITY, most) : r;
+                const float f = any ? __builtin_amdgcn_exp2f(m - next) : 0.0f;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) o[d] *= __builtin_amdgcn_ldexpf(f, to - r);
+                m = next;
+                r = to;
+                any = any || top > -INFINITY;
+                weigh();
             }
+        } else {
+            if (__any(top > m + kGrow || (!any && top > -INFINITY))) {
+                top = max_halves(max_rows16(top));
+                if (top > -INFINITY && (!any || top > m)) {
+                    const float f = any ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
+                    m = top;
+                    any = true;
+                    l *= f;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) o[d] *= f;
+                }
+            }
+            weigh();
         }
         u4 pr;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            float e[4], p0[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.c2, -m));
-                if constexpr (SRC == kCodes) {
-                    p0[i] = e[i];
-                    if (T != CHAM_T_F16) l += e[i];
-                    e[i] *= vs[t][i] * vinv;
-                }
-            }
-            pr[2 * t] = narrow<VT>(e[0], e[1]);
-            pr[2 * t + 1] = narrow<VT>(e[2], e[3]);
+            const float(&x)[4] = SRC == kCodes ? w[t] : e[t];
+            pr[2 * t] = narrow<VT>(x[0], x[1]);
+            pr[2 * t + 1] = narrow<VT>(x[2], x[3]);
             if constexpr (SRC != kCodes) {
                 l = add2<T>(pr[2 * t + 1], add2<T>(pr[2 * t], l));
             } else if constexpr (T == CHAM_T_F16) {
                 // the rounded ones here too, without their scale (where it counts): one key's rounding would be as
                 // large as the output's
-                const uint32_t w[2] = {pr[2 * t], pr[2 * t + 1]};
+                const uint32_t p2[2] = {pr[2 * t], pr[2 * t + 1]};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float by = vs[t][i] * vinv, r = i & 1 ? f16_hi(w[i >> 1]) : f16_lo(w[i >> 1]);
-                    l += by >= 0x1p-20f ? r * __builtin_amdgcn_rcpf(by) : p0[i];
+                    const float by = vs[t][i] * two_to(r), p0 = i & 1 ? f16_hi(p2[i >> 1]) : f16_lo(p2[i >> 1]);
+                    l += by >= 0x1p-20f ? p0 * __builtin_amdgcn_rcpf(by) : e[t][i];
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l += e[t][i];
             }
         }
         // values of column 16 d + (lane & 15): keys 4 g .. + 3 and 16 + 4 g .. + 3
@@ -961,10 +987,10 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
     float* mine = (float*)&lds.v[wave][0][0];
 #pragma unroll
     for (int d = 0; d < ND; ++d) *(f4*)(mine + col * (16 * ND) + 16 * d + 4 * g) = o[d];
-    if (lane == 0) lds.vref[wave] = SRC == kCodes ? vref : 1.0f;
     if (g == 0) {
         lds.m[wave][col] = any ? m : -INFINITY;
         lds.l[wave][col] = l;
+        if (SRC == kCodes) lds.r[wave][col] = r;
     }
     __syncthreads();
     if (p.pieces > 1 && (unsigned)p.index >= (unsigned)a.most) return;
@@ -984,8 +1010,14 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
         f4 sum = {};
 #pragma unroll
         for (int w = 0; w < NW; ++w)
-            if (weight[w] != 0.0f)
-                sum += weight[w] * f * *(const f4*)((const float*)&lds.v[w][0][0] + row * (16 * ND) + e) * lds.vref[w];
+            if (weight[w] != 0.0f) {
+                f4 v = weight[w] * f * *(const f4*)((const float*)&lds.v[w][0][0] + row * (16 * ND) + e);
+                if constexpr (SRC == kCodes) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_ldexpf(v[i], -lds.r[w][row]);
+                }
+                sum += v;
+            }
         if (p.pieces == 1) {
             put4<T>(a.a.o, (int64_t)p.q0 * a.a.o.token + (int64_t)(head0 + row) * a.a.o.head + e, sum[0], sum[1], sum[2], sum[3]);
         } else {

@@ -111,7 +111,7 @@ def _steered(seed, dt, cache, lq, score, Hq=4, Hk=2, D=64, page=16):
 
 
 @pytest.mark.parametrize("dt", [F16, BF16])
-@pytest.mark.parametrize("chunk", [True])
+@pytest.mark.parametrize("chunk", [False, True])
 @pytest.mark.parametrize("which", ["first", "middle", "half", "all but the last", "every third"])
 def test_large_scales_of_small_probabilities(dt, chunk, which):
     """Keys 40 nats below the others with scales of 2^30 times theirs: they count for 2^-27."""
@@ -142,7 +142,7 @@ def test_small_scales_of_large_sums(dt, chunk, n, power, scale):
     _check(o, q, c, table, n, 1.0)
 
 
-@pytest.mark.parametrize("chunk", [True])
+@pytest.mark.parametrize("chunk", [False, True])
 def test_scales_and_scores_that_wander(chunk):
     """Scores and scales that both run over dozens of powers of two, apart and together."""
     case(f"wandering chunk={chunk}")
