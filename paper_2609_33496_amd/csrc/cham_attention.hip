@@ -958,13 +958,14 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
             if constexpr (SRC != kCodes) {
                 l = add2<T>(pr[2 * t + 1], add2<T>(pr[2 * t], l));
             } else if constexpr (T == CHAM_T_F16) {
-                // the rounded ones here too, without their scale (where it counts): one key's rounding would be as
-                // large as the output's
+                // the rounded ones here too, without their scale: one key's rounding would be as large as the
+                // output's.  But for those that float16 holds with fewer than 11 bits, or not at all: their products
+                // are next to nothing beside the row's largest, which their probabilities may not be.
                 const uint32_t p2[2] = {pr[2 * t], pr[2 * t + 1]};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float by = vs[t][i] * two_to(r), p0 = i & 1 ? f16_hi(p2[i >> 1]) : f16_lo(p2[i >> 1]);
-                    l += by >= 0x1p-20f ? p0 * __builtin_amdgcn_rcpf(by) : e[t][i];
+                    const float p0 = i & 1 ? f16_hi(p2[i >> 1]) : f16_lo(p2[i >> 1]);
+                    l += x[i] >= 0x1p-14f ? e[t][i] * (p0 * __builtin_amdgcn_rcpf(x[i])) : e[t][i];
                 }
             } else {
 #pragma unroll

@@ -127,7 +127,7 @@ def test_large_scales_of_small_probabilities(dt, chunk, which):
 
 
 @pytest.mark.parametrize("dt", [F16, BF16])
-@pytest.mark.parametrize("chunk", [True])
+@pytest.mark.parametrize("chunk", [False, True])
 @pytest.mark.parametrize("n,power,scale", [(32, 6.1, 19), (1000, 6.1, 19), (10000, 13.1, 12), (10000, 0.0, 22), (300, 2.0, 30)])
 def test_small_scales_of_large_sums(dt, chunk, n, power, scale):
     """One value of scale 1 and n - 1 of scale 2^-scale, whose probabilities are 2^-power of its: they count in
