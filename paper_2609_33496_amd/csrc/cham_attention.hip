@@ -35,7 +35,6 @@ namespace {
 enum { kPacked, kPages, kCodes };
 
 constexpr float kLog2e = 1.44269504f;
-constexpr float kGrow = 8.0f;  // few_kernel: the reference follows scores more than 2^8 above it
 
 // kCodes: what is rounded to float16 is a probability times its value's scale, and what counts among those of a
 // row is how they compare with the row's largest, whatever the probabilities and the scales are
@@ -477,13 +476,13 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     const int v_at = v_row * L::CU * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8, v_key = L::key_v(v_row) << 4;
 
     // The reference is set kAbove powers of two above the largest score and stays until a lane's 32
-    // probabilities add up to kBig: where none has, none is as large.  float16 holds a probability's 11 bits
-    // between 2^-14 and 2^16; binary32
-    // sums of bfloat16 ones and values hold 24 bits for values from 2^-78 up and stay finite for the largest.  So
-    // a reference moves where scores grow by 2^20 (2^16, 2^25).  4096 x 4096, scores of 5 nats' standard deviation:
-    // 119 us a piece where it moves at 2^8, which is every few steps, 91 so.
-    constexpr float kAbove = T == CHAM_T_F16 ? 6.0f : 24.0f;
-    constexpr float kBig = SRC == kCodes ? 0x1p20f : T == CHAM_T_F16 ? 16384.0f : 2.0f;
+    // probabilities add up to kBig: where none has, none is as large.  float16 holds 11 bits of a probability
+    // between 2^-14 and 2^16 and nothing below 2^-25, so there the largest is set to 2^2: none above 2^-27 of it is lost,
+    // of which 2^15 make half a rounding of the output.  binary32 sums of bfloat16 ones and values hold
+    // 24 bits for values from 2^-78 up.  So a reference moves where scores grow by 2^14 (2^25).  2 x 4096 x 4096, 16 heads
+    // of 72, float16, scores of 4 nats' standard deviation: 221 us with 1, 226 with 2^2, 236 with 2^4, 243 with 2^6.
+    constexpr float kAbove = T == CHAM_T_F16 ? -2.0f : 24.0f;
+    constexpr float kBig = SRC == kCodes ? 0x1p20f : T == CHAM_T_F16 ? 61440.0f : 2.0f;
 
     // One step's keys against the wavefront's rows; masked: some row does not see all of them.  The
     // outputs' sums are touched in three places only, whatever branch made the probabilities, so that they
@@ -936,8 +935,10 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
                 weigh();
             }
         } else {
+            // the largest is set to 1 (float16: 2^2, see the tiled kernel) and may grow to kGrow
+            constexpr float kAbove = T == CHAM_T_F16 ? -2.0f : 0.0f, kGrow = T == CHAM_T_F16 ? 15.0f : 8.0f;
             if (__any(top > m + kGrow || (!any && top > -INFINITY))) {
-                top = max_halves(max_rows16(top));
+                top = max_halves(max_rows16(top)) + kAbove;
                 if (top > -INFINITY && (!any || top > m)) {
                     const float f = any ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
                     m = top;

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2609_33496_amd import cham
-from test_gpu_attention import DEV, E4, HALF, INF, TINY, U, _cached_case, _gather, _ints, _within, case
+from test_gpu_attention import DEV, E4, HALF, INF, TINY, U, _cached_case, _gather, _gen, _ints, _starts, _within, case
 
 pytestmark = pytest.mark.gpu
 F16, BF16 = torch.float16, torch.bfloat16
@@ -21,7 +21,7 @@ def _want(q, k, v, scale, causal, vscale=None):
     at most D 2^-23 sum |q k|, a scale rounds once more; the exponent's argument by a rounding of a number up
     to |t| + 32 and of the reference; the exponential by 2^-22.  p (over codes p times the scale) is rounded to
     bfloat16, or to binary16 beside float16 and codes: u relative, or half a subnormal step, 2^-25, where the
-    row's largest is 2^4 and more (over codes 2^2): 2^-29 (2^-27) of that largest.  Where the sum adds the rounded ones, it is off by as much.
+    row's largest is 2^2 and more: 2^-27 of that largest.  Where the sum adds the rounded ones, it is off by as much.
     Sums of n terms take n 2^-24, two of them."""
     nq, Hq, D = q.shape
     nk, Hk = k.shape[:2]
@@ -45,7 +45,7 @@ def _want(q, k, v, scale, causal, vscale=None):
         l = p.sum(1, keepdim=True)
         w = p if vscale is None else p * vscale[:, j].double()
         codes = vv.abs() if vscale is None else vv.abs() / vscale[:, j:j + 1].double()
-        tiny = 0.0 if not half else 2.0 ** -29 if vscale is None else 2.0 ** -27
+        tiny = 2.0 ** -27 if half else 0.0
         o[:, h] = p @ vv / l
         b = ((p * off) @ vv.abs() + p @ vv.abs() * (u + (8 + 2 * nk) * U) +
              tiny * w.amax(1, keepdim=True) * ((~hidden).double() @ codes)) / l
@@ -154,3 +154,45 @@ def test_scales_and_scores_that_wander(chunk):
         c.v_scale[ids, :, at] = torch.exp2(80.0 * torch.sin(b * t))[:, None]
         o = cham.cache_attention(q, c, table, _ints([n]), _ints([0, 20]) if chunk else None, scale=1.0)
         _check(o, q, c, table, n, 1.0)
+
+
+# ---------------------------------------------------------------------------------------------
+# the tail of the softmax
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("low", [-13.5, -15.0, -9.0])
+@pytest.mark.parametrize("dt", [F16, BF16])
+def test_prompts_keep_the_tail(dt, low):
+    """8192 keys far below one add up to a part of the row that shows (work that fills the card, so not cut)."""
+    case(f"tail of prompts {dt} {low}")
+    n, H, D = 8193, 16, 8
+    q = torch.zeros((8192, H, D), dtype=dt, device=DEV)
+    q[..., 0] = 1.0
+    k = torch.zeros((n, H, D), dtype=dt, device=DEV)
+    k[..., 0] = low
+    k[5, :, 0] = 0.0
+    v = (1.0 + 0.1 * torch.randn((n, H, D), generator=_gen(1), device=DEV)).to(dt)
+    v[5] = 0.0
+    got = cham.attention(q, k, v, scale=1.0)
+    for h in (0, 15):
+        for r in (0, 77, 8191):
+            o, bound = _want(q[r:r + 1, h:h + 1], k[:, h:h + 1], v[:, h:h + 1], 1.0, False)
+            _within(got[r:r + 1, h:h + 1], o, bound)
+
+
+@pytest.mark.parametrize("chunk", [False, True])
+@pytest.mark.parametrize("dt,cache", [(F16, F16), (BF16, BF16), (F16, E4), (BF16, E4)])
+def test_caches_keep_the_tail(dt, cache, chunk):
+    """The same over pages, 1024 sequences of which are the same pages."""
+    case(f"tail of caches {dt} {cache} chunk={chunk}")
+    n, B = 8193, 1024
+    score = torch.full((n,), -13.5, device=DEV)
+    score[5] = 0.0
+    q, c, table, ids, at = _steered(25, dt, cache, 2 if chunk else 1, score, 1, 1, 16)
+    if cache is E4:
+        c.v_scale.fill_(2.0 ** -8)
+    c.v.copy_((256.0 if cache is E4 else 1.0) * (1.0 + torch.randint(0, 2, c.v.shape, generator=_gen(2), device=DEV) / 8.0))
+    c.v.view(torch.uint8)[int(ids[5]), :, int(at[5])] = 0
+    lq = q.shape[0]
+    o = cham.cache_attention(q.repeat(B, 1, 1), c, table.repeat(B, 1), _ints([n] * B), _starts([lq] * B) if chunk else None, scale=1.0)
+    for b in (0, B - 1):
+        _check(o[lq * b:lq * (b + 1)], q, c, table, n, 1.0)
