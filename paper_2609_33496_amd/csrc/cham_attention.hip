@@ -937,16 +937,17 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
         } else {
             // the largest is set to 1 (float16: 2^2, see the tiled kernel) and may grow to kGrow
             constexpr float kAbove = T == CHAM_T_F16 ? -2.0f : 0.0f, kGrow = T == CHAM_T_F16 ? 15.0f : 8.0f;
-            if (__any(top > m + kGrow || (!any && top > -INFINITY))) {
+            const bool big = top > m + kGrow || (!any && top > -INFINITY);
+            if (__any(big)) {
+                // (a row's own scores decide, so that no other head's change how it rounds)
+                const bool mine = max_halves(max_rows16(big ? 1.0f : 0.0f)) > 0.0f;
                 top = max_halves(max_rows16(top)) + kAbove;
-                if (top > -INFINITY && (!any || top > m)) {
-                    const float f = any ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
-                    m = top;
-                    any = true;
-                    l *= f;
+                const float f = !mine ? 1.0f : any ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
+                m = mine ? top : m;
+                any = any || mine;
+                l *= f;
 #pragma unroll
-                    for (int d = 0; d < ND; ++d) o[d] *= f;
-                }
+                for (int d = 0; d < ND; ++d) o[d] *= f;
             }
             weigh();
         }

@@ -196,3 +196,20 @@ def test_caches_keep_the_tail(dt, cache, chunk):
     o = cham.cache_attention(q.repeat(B, 1, 1), c, table.repeat(B, 1), _ints([n] * B), _starts([lq] * B) if chunk else None, scale=1.0)
     for b in (0, B - 1):
         _check(o[lq * b:lq * (b + 1)], q, c, table, n, 1.0)
+
+
+# ---------------------------------------------------------------------------------------------
+# other heads
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt,cache", [(F16, F16), (BF16, BF16), (F16, E4), (BF16, E4)])
+@pytest.mark.parametrize("n", [40, 900, 6000])
+def test_heads_of_a_token_do_not_change_one_another(dt, cache, n):
+    """A head's result has the same bits whatever queries share its key head."""
+    case(f"heads apart {dt} {cache} n={n}")
+    q, c, table = _cached_case(26, [1], [n], 8, 2, 64, 16, dt, cache)
+    want = cham.cache_attention(q, c, table, _ints([n]))
+    other = q.clone()
+    other[:, 1::2] *= 30.0
+    other[:, 6] = INF
+    got = cham.cache_attention(other, c, table, _ints([n]))
+    assert torch.equal(got[:, [0, 2, 4]], want[:, [0, 2, 4]])
