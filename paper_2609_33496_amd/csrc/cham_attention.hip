@@ -476,13 +476,14 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     const int v_at = v_row * L::CU * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8, v_key = L::key_v(v_row) << 4;
 
     // The reference is set kAbove powers of two above the largest score and stays until a lane's 32
-    // probabilities add up to kBig: where none has, none is as large.  float16 holds 11 bits of a probability
+    // probabilities (bfloat16: all up to here) add up to kBig: where they have not, none is as large.  float16 holds 11 bits of a probability
     // between 2^-14 and 2^16 and nothing below 2^-25, so there the largest is set to 2^2: none above 2^-27 of it is lost,
     // of which 2^15 make half a rounding of the output.  binary32 sums of bfloat16 ones and values hold
-    // 24 bits for values from 2^-78 up.  So a reference moves where scores grow by 2^14 (2^25).  2 x 4096 x 4096, 16 heads
+    // 24 bits for values from 2^-78 up, and are finite for the largest as the probabilities of a row's two lanes
+    // stay below 1/2.  So a reference moves where scores grow by 2^14 (2^17 and more).  2 x 4096 x 4096, 16 heads
     // of 72, float16, scores of 4 nats' standard deviation: 221 us with 1, 226 with 2^2, 236 with 2^4, 243 with 2^6.
     constexpr float kAbove = T == CHAM_T_F16 ? -2.0f : 24.0f;
-    constexpr float kBig = SRC == kCodes ? 0x1p20f : T == CHAM_T_F16 ? 61440.0f : 2.0f;
+    constexpr float kBig = SRC == kCodes ? 0x1p20f : T == CHAM_T_F16 ? 61440.0f : 0.25f;
 
     // One step's keys against the wavefront's rows; masked: some row does not see all of them.  The
     // outputs' sums are touched in three places only, whatever branch made the probabilities, so that they
@@ -571,7 +572,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
             sum = weigh(m, false);
             asm volatile("; all keys seen");
         }
-        bool big = !(sum < kBig);  // a probability may be large, or there is no reference yet
+        constexpr bool kAll = SRC != kCodes && T == CHAM_T_BF16;
+        bool big = !((kAll ? l + sum : sum) < kBig);  // a probability may be large, or there is no reference yet
         if constexpr (SRC == kCodes) big = big || max((uint32_t)most[0], (uint32_t)most[1]) >= 0x7c00;
         if (__builtin_expect(__any(big), 0)) {
             // every row's reference follows its largest score, and its probabilities with it
@@ -588,7 +590,11 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
             const bool mine = max_halves(big ? 1.0f : 0.0f) > 0.0f;
             top = max_halves(top);
             // (codes: whole numbers, so that factors between references are exact)
-            const float next = mine ? fmaxf(m, SRC == kCodes ? __builtin_ceilf(top) : top + kAbove) : m;
+            float next = mine ? fmaxf(m, SRC == kCodes ? __builtin_ceilf(top) : top + kAbove) : m;
+            if constexpr (kAll) {  // those before this step
+                const float before = max_halves(l);
+                if (mine && before > 0.5f * kBig) next = fmaxf(next, m + kAbove);
+            }
             f = next > m ? __builtin_amdgcn_exp2f(m - next) : 1.0f;
             l *= f;
             if constexpr (SRC == kCodes) {
@@ -935,13 +941,16 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
                 weigh();
             }
         } else {
-            // the largest is set to 1 (float16: 2^2, see the tiled kernel) and may grow to kGrow
-            constexpr float kAbove = T == CHAM_T_F16 ? -2.0f : 0.0f, kGrow = T == CHAM_T_F16 ? 15.0f : 8.0f;
-            const bool big = top > m + kGrow || (!any && top > -INFINITY);
+            // the largest is set to 2^2 or 2^-16 (see the tiled kernel) and may grow to 2^kGrow; the sum of a row's four
+            // lanes stays below 1/2 in bfloat16
+            constexpr float kAbove = T == CHAM_T_F16 ? -2.0f : 16.0f, kGrow = T == CHAM_T_F16 ? 15.0f : -8.0f;
+            const float full = T == CHAM_T_F16 ? INFINITY : 0x1p-4f;
+            const bool big = top > m + kGrow || (!any && top > -INFINITY) || l > full;
             if (__any(big)) {
                 // (a row's own scores decide, so that no other head's change how it rounds)
                 const bool mine = max_halves(max_rows16(big ? 1.0f : 0.0f)) > 0.0f;
                 top = max_halves(max_rows16(top)) + kAbove;
+                if (max_halves(max_rows16(l)) > full) top = fmaxf(top, m + kAbove);
                 const float f = !mine ? 1.0f : any ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
                 m = mine ? top : m;
                 any = any || mine;
@@ -1053,6 +1062,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
     const int parts = 8 >> shift;
     const bool live = row < rows && e < D;
     const int64_t at = (int64_t)p.index * BM + row0 + row, stride = (int64_t)a.Hk * BM;
+    // every output is weighed with its share of the whole, so that sums of the largest values stay finite
     float top = -INFINITY, total = 0.0f;
     f4 sum = {};
     if (live) {
@@ -1061,13 +1071,14 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
             const float2 s = *(const float2*)(a.part_s + (at + c * stride) * 2);
             top = s.y != 0.0f ? fmaxf(top, s.x) : top;
         }
+        const auto weight = [&](float2 s) { return s.y == 0.0f ? 0.0f : s.y * __builtin_amdgcn_exp2f(s.x - top); };  // 0: saw no key
+#pragma unroll 4
+        for (int c = part; c < p.pieces; c += parts) total += weight(*(const float2*)(a.part_s + (at + c * stride) * 2));
+        const float f = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll 4
         for (int c = part; c < p.pieces; c += parts) {
-            const float2 s = *(const float2*)(a.part_s + (at + c * stride) * 2);
             const f4 v = *(const f4*)(a.part_o + (at + c * stride) * D + e);
-            const float w = s.y == 0.0f ? 0.0f : s.y * __builtin_amdgcn_exp2f(s.x - top);  // 0: saw no key, its output is 0
-            total += w;
-            sum += w * v;
+            sum += weight(*(const float2*)(a.part_s + (at + c * stride) * 2)) * f * v;
         }
     }
     if (parts > 1) {  // a group's sums are over its own largest reference
@@ -1076,20 +1087,18 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
         __syncthreads();
         if (part > 0) return;
         for (int c = 0; c < parts; ++c) top = fmaxf(top, stats[row + (c << shift)].x);
+        const auto weight = [&](float2 s) { return s.x == top || s.y != s.y ? s.y : s.y == 0.0f ? 0.0f : s.y * __builtin_amdgcn_exp2f(s.x - top); };
         total = 0.0f;
+        for (int c = 0; c < parts; ++c) total += weight(stats[row + (c << shift)]);
+        const float f = total == 0.0f ? 0.0f : 1.0f / total;
         sum = f4{};
         for (int c = 0; c < parts; ++c) {
             const int g = row + (c << shift);
-            const float2 s = stats[g];
             const float4 v = sums[g][threadIdx.x % 32];
-            const float w = s.x == top || s.y != s.y ? 1.0f : __builtin_amdgcn_exp2f(s.x - top);
-            if (s.y == 0.0f) continue;
-            total += w * s.y;
-            sum += w * f4{v.x, v.y, v.z, v.w};
+            sum += weight(stats[g]) * f * f4{v.x, v.y, v.z, v.w};
         }
     }
     if (!live) return;
-    sum *= total == 0.0f ? 0.0f : 1.0f / total;
     const int in = p.tile * BM + row0 + row, token = by_group(a, in);
     put4<T>(a.a.o, (int64_t)(p.q0 + token) * a.a.o.token + (int64_t)(hk * a.G + in - token * a.G) * a.a.o.head + e, sum[0], sum[1],
             sum[2], sum[3]);

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2609_33496_amd import cham
-from test_gpu_attention import DEV, E4, HALF, INF, TINY, U, _cached_case, _gather, _gen, _ints, _starts, _within, case
+from test_gpu_attention import DEV, E4, HALF, INF, TINY, U, _cached_case, _gather, _gen, _ints, _rows, _starts, _within, case
 
 pytestmark = pytest.mark.gpu
 F16, BF16 = torch.float16, torch.bfloat16
@@ -213,3 +213,59 @@ def test_heads_of_a_token_do_not_change_one_another(dt, cache, n):
     other[:, 6] = INF
     got = cham.cache_attention(other, c, table, _ints([n]))
     assert torch.equal(got[:, [0, 2, 4]], want[:, [0, 2, 4]])
+
+
+# ---------------------------------------------------------------------------------------------
+# values near the largest
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("growth", [0.0, 12.9, -12.9])
+def test_prompts_of_values_near_the_largest(growth):
+    """Values of 2^126 in bfloat16, whose mean is as large: one long step after another, behind scores that are
+    lower or higher by 2^18.6 in the first."""
+    case(f"large values of prompts growth={growth}")
+    n, H, D = 12864, 16, 8
+    q = torch.zeros((8192, H, D), dtype=BF16, device=DEV)
+    q[..., 0] = 1.0
+    k = torch.zeros((n, H, D), dtype=BF16, device=DEV)
+    k[64:, :, 0] = growth
+    v = ((1.0 + 0.2 * torch.rand((n, H, D), generator=_gen(1), device=DEV)) * 2.0 ** 126).to(BF16)
+    got = cham.attention(q, k, v, scale=1.0)
+    for r in (0, 8191):
+        o, bound = _want(q[r:r + 1, :1], k[:, :1], v[:, :1], 1.0, False)
+        _within(got[r:r + 1, :1], o, bound)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("most", [9.0, 16.0, 40.0])
+def test_rows_of_rising_scores_do_not_change_one_another(dt, most):
+    """A row's reference moves where its own probabilities have added up, not where those of a row beside it have."""
+    case(f"rising scores {dt} {most}")
+    n, H, D = 4000, 16, 8  # work that is not cut: slow growth over many steps
+    q, k, v = _rows(28, 8192, H, D, dt, 0.1), _rows(29, n, H, D, dt, 0.1), _rows(30, n, H, D, dt)
+    q[..., 0] = torch.linspace(0.3, 1.0, 8192, device=DEV)[torch.randperm(8192, generator=_gen(3), device=DEV), None].to(dt)
+    k[..., 0] = torch.linspace(0.0, most, n, device=DEV)[:, None].to(dt)
+    want = cham.attention(q, k, v, scale=1.0)
+    for by in (2.0, 4.0):
+        other = q.clone()
+        other[1::2] *= by
+        got = cham.attention(other, k, v, scale=1.0)
+        assert torch.equal(got[::2], want[::2])
+    for r in (0, 8191):
+        o, bound = _want(q[r:r + 1, :1], k[:, :1], v[:, :1], 1.0, False)
+        _within(want[r:r + 1, :1], o, bound)
+
+
+@pytest.mark.parametrize("chunk", [False, True])
+@pytest.mark.parametrize("cache", [BF16, E4])
+@pytest.mark.parametrize("n", [40, 1000, 20000])
+@pytest.mark.parametrize("growth", [0.0, 5.0, -5.0])
+def test_caches_of_values_near_the_largest(cache, chunk, n, growth):
+    case(f"large values of caches {cache} chunk={chunk} n={n} growth={growth}")
+    score = torch.full((n,), growth, device=DEV)
+    score[:32] = 0.0
+    q, c, table, ids, at = _steered(27, BF16, cache, 5 if chunk else 1, score, 2, 1)
+    if cache is E4:
+        c.v_scale.fill_(2.0 ** 118)
+    c.v.copy_((256.0 if cache is E4 else 2.0 ** 126) * (1.0 + torch.randint(0, 3, c.v.shape, generator=_gen(2), device=DEV) / 8.0))
+    o = cham.cache_attention(q, c, table, _ints([n]), _ints([0, 5]) if chunk else None, scale=1.0)
+    _check(o, q, c, table, n, 1.0)
