@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const RowsArgs a) {
     if (half > 0) {
         for (int i = threadIdx.x; i < nt * kMaxHalf; i += kThreads) {
             const int k = i % kMaxHalf;
-            float2 v = make_float2(1.0f, 0.0f);  // pairs behind R stay as they are
+            float2 v = make_float2(1.0f, 0.0f);  // pairs behind R are read, but not turned
             if (k < half) {
                 v = cos_sin((double)a.r.pos[t0 + i / kMaxHalf] * a.r.freq[k]);
                 v.x *= a.r.amp;
@@ -196,11 +196,24 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const RowsArgs a) {
                         if (a.r.layout == CHAM_ROT_PAIRS) {
                             const float4 c4 = *(const float4*)(co + d0 / 2), s4 = *(const float4*)(si + d0 / 2);
                             const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+                            // (a pair behind R times (1, 0) would pass an infinity on to its neighbour)
+                            const int turned = half - d0 / 2;
+                            if (half % 4 == 0) {
+                                if (turned > 0) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float u = y[2 * j], v = y[2 * j + 1];
-                                y[2 * j] = u * c[j] - v * s[j];
-                                y[2 * j + 1] = v * c[j] + u * s[j];
+                                for (int j = 0; j < 4; ++j) {
+                                    const float u = y[2 * j], v = y[2 * j + 1];
+                                    y[2 * j] = u * c[j] - v * s[j];
+                                    y[2 * j + 1] = v * c[j] + u * s[j];
+                                }
+                                }
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const float u = y[2 * j], v = y[2 * j + 1];
+                                    y[2 * j] = j < turned ? u * c[j] - v * s[j] : u;
+                                    y[2 * j + 1] = j < turned ? v * c[j] + u * s[j] : v;
+                                }
                             }
                         } else if (half % kChunk == 0) {
                             // a partner is another lane's element of the same place

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2609_33496_amd import cham
-from test_gpu_attention import DEV, E4, HALF, INF, TINY, U, _cached_case, _gather, _gen, _ints, _rows, _starts, _within, case
+from test_gpu_attention import DEV, E4, HALF, INF, NAN, TINY, U, _cached_case, _gather, _gen, _ints, _rows, _starts, _within, case
 
 pytestmark = pytest.mark.gpu
 F16, BF16 = torch.float16, torch.bfloat16
@@ -269,3 +269,33 @@ def test_caches_of_values_near_the_largest(cache, chunk, n, growth):
     c.v.copy_((256.0 if cache is E4 else 2.0 ** 126) * (1.0 + torch.randint(0, 3, c.v.shape, generator=_gen(2), device=DEV) / 8.0))
     o = cham.cache_attention(q, c, table, _ints([n]), _ints([0, 5]) if chunk else None, scale=1.0)
     _check(o, q, c, table, n, 1.0)
+
+
+# ---------------------------------------------------------------------------------------------
+# rotation
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("layout", [cham.ROT_HALF, cham.ROT_PAIRS])
+@pytest.mark.parametrize("dt", [torch.float32, F16, BF16])
+@pytest.mark.parametrize("R", [2, 10, 16, 62])
+def test_elements_behind_the_rotation_stay(dt, layout, R):
+    """Bit by bit: infinities, NaN and zeros of either sign, whatever lies beside them."""
+    case(f"behind the rotation {dt} layout={layout} R={R}")
+    T, H, D = 5, 3, 64
+    x = _rows(31, T, H, D, dt)
+    tail = x[..., R:]
+    tail[0, 0, 0], tail[1, 1, -1], tail[2] = INF, NAN, -0.0
+    tail[3, 2, 0], tail[3, 2, 1], tail[4, 0, -2] = -0.0, -INF, -INF
+    how = dict(norm=False, positions=_ints([0, 7, 100, 3, 9]), freq=torch.rand(R // 2, generator=_gen(1), device=DEV, dtype=torch.float64),
+               layout=layout)
+    bits = torch.int32 if dt == torch.float32 else torch.int16
+    want = tail.contiguous().view(bits)
+    q, k = cham.norm_rotate(x, x, **how)
+    keep = ~tail.isnan()
+    for y in (q, k):
+        assert torch.equal(y[..., R:].contiguous().view(bits)[keep], want[keep]) and bool(y[..., R:][~keep].isnan().all())
+        assert bool(y[..., :R].isfinite().all())
+    if dt != torch.float32:
+        c = cham.alloc_cache(1, H, 16, D, dt, DEV)
+        cham.cache_write(c, _ints([3, 1, 0, 2, 9]), x, x, **how)
+        y = c.k[0].transpose(0, 1)[[3, 1, 0, 2, 9]][..., R:]
+        assert torch.equal(y.contiguous().view(bits)[keep], want[keep])
