@@ -51,7 +51,7 @@ class AttentionBlock:
         """(y, h) of whole sequences: `batch` of equal lengths, or packed rows cu[b] .. cu[b + 1].  h = x +
         residual (None without one); positions int32 [T] where there is a rotation."""
         q, k, v, h = self._heads(x, residual, residual_out, stream)
-        if self.how["norm"] or self.freq is not None:  # in place: the product's output is this call's own
+        if self.how["norm"] or self.freq is not None or positions is not None:  # in place: the product's output is this call's own
             cham.norm_rotate(q, k, q_out=q, k_out=k, positions=positions, stream=stream, **self.how)
         o = cham.attention(q, k, v, batch=batch, cu_q=cu, causal=causal, stream=stream)
         return self._out(o, x, stream), h
