@@ -55,11 +55,17 @@ CHAM_DEV uint32_t vector_max(uint32_t v) {
 
 // cos t and sin t.  t is reduced by multiples of pi/2 in binary64 (pi/2 in two parts: the rest is
 // within 2^-53 |t|), the remainder's series, |r| <= pi/4, are cut off below 2^-29 and run in binary32.
+// From 2^51 on a multiple's own rounding may leave several pi/2, which a second turn takes off; from 2^55 on
+// every angle is within 2^-53 |t|, and 0 is taken.
 CHAM_DEV float2 cos_sin(double t) {
-    const double n = __builtin_rint(t * 0.63661977236758134308);
-    double r = __builtin_fma(-n, 0x1.921fb54442d18p+0, t);
-    r = __builtin_fma(-n, 0x1.1a62633145c07p-54, r);
-    const int quarter = (int)(n - 4.0 * __builtin_floor(n * 0.25));
+    const auto reduce = [](double t, int* quarter) {
+        const double n = __builtin_rint(t * 0.63661977236758134308);
+        *quarter += (int)(n - 4.0 * __builtin_floor(n * 0.25));
+        return __builtin_fma(-n, 0x1.1a62633145c07p-54, __builtin_fma(-n, 0x1.921fb54442d18p+0, t));
+    };
+    t = __builtin_fabs(t) < 0x1p55 ? t : t * 0.0;
+    int quarter = 0;
+    const double r = reduce(reduce(t, &quarter), &quarter);
     const float x = (float)r, z = x * x;
     float s = __builtin_fmaf(z, 1.0f / 362880.0f, -1.0f / 5040.0f);
     s = __builtin_fmaf(z, s, 1.0f / 120.0f);
@@ -201,11 +207,11 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const RowsArgs a) {
                             if (half % 4 == 0) {
                                 if (turned > 0) {
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    const float u = y[2 * j], v = y[2 * j + 1];
-                                    y[2 * j] = u * c[j] - v * s[j];
-                                    y[2 * j + 1] = v * c[j] + u * s[j];
-                                }
+                                    for (int j = 0; j < 4; ++j) {
+                                        const float u = y[2 * j], v = y[2 * j + 1];
+                                        y[2 * j] = u * c[j] - v * s[j];
+                                        y[2 * j + 1] = v * c[j] + u * s[j];
+                                    }
                                 }
                             } else {
 #pragma unroll

@@ -302,6 +302,28 @@ def test_elements_behind_the_rotation_stay(dt, layout, R):
         assert torch.equal(y.contiguous().view(bits)[keep], want[keep])
 
 
+@pytest.mark.parametrize("power", [20, 45, 52, 60, 100, 900])
+def test_angles_of_any_size(power):
+    """Far angles keep their error of 2^-53 |t| and, where that says nothing, their length: a pair's is
+    within 2^-20 of what it was, (7 + 2^-23 / 2^-24) U of each product."""
+    case(f"angles of 2^{power}")
+    T, H, D = 64, 1, 64
+    x = _rows(33, T, H, D, torch.float32)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)
+    freq = (1.0 + torch.rand(D // 2, generator=_gen(5), device=DEV, dtype=torch.float64)) * 2.0 ** (power - 6)
+    for layout in (cham.ROT_HALF, cham.ROT_PAIRS):
+        y, _ = cham.norm_rotate(x, None, norm=False, positions=pos, freq=freq, layout=layout)
+        a, b = (y[..., 0::2], y[..., 1::2]) if layout == cham.ROT_PAIRS else (y[..., :32], y[..., 32:])
+        u, v = (x[..., 0::2], x[..., 1::2]) if layout == cham.ROT_PAIRS else (x[..., :32], x[..., 32:])
+        u, v = u.double(), v.double()
+        size = torch.hypot(u, v)
+        _within(torch.hypot(a.double(), b.double()), size, size * 2.0 ** -20)
+        if power <= 45:
+            t = pos.double()[:, None, None] * freq
+            bound = size * (2.0 ** -20 + 2.0 ** -51 * t)
+            _within(a, u * torch.cos(t) - v * torch.sin(t), bound)
+            _within(b, v * torch.cos(t) + u * torch.sin(t), bound)
+
 def test_block_refuses_positions_without_a_rotation():
     case("block positions")
     g = _gen(1)
