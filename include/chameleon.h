@@ -590,7 +590,8 @@ typedef struct cham_heads {
  * R elements turn by the angle t = pos freq[i]: (a cos t - b sin t, b cos t + a sin t) * amp.
  * The squares, their sum and the root are binary64 for binary32 elements and where a row's mean square lies
  * outside 2^-60 .. 2^100, else binary32 (y within 2^-20): every finite row has its norm.  Angles are binary64
- * up to their reduction by pi/2, so far positions keep their angle (absolute error below 2^-53 |t| + 2^-24);
+ * up to their reduction by pi/2, so far positions keep their angle (absolute error below 2^-53 |t| + 2^-24, and a
+ * pair its length at any t); elements behind R are not touched but by the norm;
  * the rest is binary32, rounded once to the output's type. */
 typedef struct cham_rotate {
     int64_t T;             /* tokens                                                          */
@@ -649,8 +650,10 @@ int cham_cache_read(const cham_cache* c, const int32_t* table, int64_t width, co
 /* o_i = sum_j p_ij v_j, p_i the softmax over the keys j that query i sees of scale <q_i, k_j>.
  * causal: query i of a sequence's nq sees its first nk - nq + i + 1 of nk keys (the last query sees all
  * of them); else all.  A query that sees none gets zeros; keys that are not seen have no influence,
- * whatever they hold.  Products in 16 bits (q, k, v as they are; p rounded to their type, to
- * binary16 over E4M3 values), sums, maxima and statistics in binary32, one rounding at the end.  Results are bitwise reproducible. */
+ * whatever they hold; nor have other rows of q.  Products in 16 bits (q, k, v as they are; p rounded to their type;
+ * over E4M3 values p times the value's scale rounded to binary16), sums, maxima and statistics in binary32, one
+ * rounding at the end.  In binary16 terms below 2^-27 of a row's largest may be left out, and those below 2^-16 of it
+ * have fewer than 11 bits.  Results are bitwise reproducible. */
 typedef struct cham_attn {
     int64_t B;             /* sequences, < 2^24                                               */
     int64_t T;             /* rows of q and o                                                 */

@@ -292,13 +292,13 @@ CHAM_DEV void put4(const cham_heads& o, int64_t at, float a, float b, float c, f
 // What bounds it, per step of a wavefront and D = 72 / 128: 22 / 32 products of 34 cycles, and about 130
 // vector instructions, 600 to 700 cycles with 32 exponentials of 8.6; two workgroups share a CU, and their
 // steps together take 2.9 / 4.1 thousand cycles, 1.9 and 2.3 times the products' (matrix cores busy 43 % over
-// 2 x 4096 x 4096, 16 heads of 72, bfloat16: 203 us, 761 TFLOP/s; 35 % over seven causal sequences of 8101
-// tokens, 32 on 8 heads of 128: 184 us, 757).  A wavefront alone on its SIMD needs as long for one step as two
+// 2 x 4096 x 4096, 16 heads of 72, bfloat16: 204 us, 758 TFLOP/s; 35 % over seven causal sequences of 8101
+// tokens, 32 on 8 heads of 128: 185 us, 752).  A wavefront alone on its SIMD needs as long for one step as two
 // for theirs, so it is the chain scores - exponentials - values in each that takes the time; priorities
 // (s_setprio), three workgroups a CU and a staggered start changed nothing.  Tiles of ragged causal
 // sequences end 18 % after the mean; the search for a piece takes 2 to 3 us of each.  E4M3 pages: 64 more
-// products with scales, the conversions and their way through registers make a step 1.6 times as long
-// (1100 new tokens over 36000, 32 on 8 heads of 128: 304 + 24 us, 467 TFLOP/s).
+// products with scales, the row's factor and what finds the largest, the conversions and their way through
+// registers make a step 1.5 times as long (1100 new tokens over 36000, 32 on 8 heads of 128: 289 + 23 us, 491 TFLOP/s).
 typedef __attribute__((address_space(3))) u4 LdsU4;
 typedef __attribute__((address_space(3))) f4 LdsF4;
 typedef __attribute__((address_space(3))) float LdsFloat;
@@ -476,19 +476,21 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
     const int v_at = v_row * L::CU * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8, v_key = L::key_v(v_row) << 4;
 
     // The reference is set kAbove powers of two above the largest score and stays until a lane's 32
-    // probabilities (bfloat16: all up to here) add up to kBig: where they have not, none is as large.  float16 holds 11 bits of a probability
-    // between 2^-14 and 2^16 and nothing below 2^-25, so there the largest is set to 2^2: none above 2^-27 of it is lost,
-    // of which 2^15 make half a rounding of the output.  binary32 sums of bfloat16 ones and values hold
-    // 24 bits for values from 2^-78 up, and are finite for the largest as the probabilities of a row's two lanes
-    // stay below 1/2.  So a reference moves where scores grow by 2^14 (2^17 and more).  2 x 4096 x 4096, 16 heads
-    // of 72, float16, scores of 4 nats' standard deviation: 221 us with 1, 226 with 2^2, 236 with 2^4, 243 with 2^6.
+    // probabilities (bfloat16: all up to here) add up to kBig: where they have not, none is as large.  float16 holds
+    // 11 bits of a probability between 2^-14 and 2^16 and nothing below 2^-25, so there the largest is set to 2^2: none
+    // above 2^-27 of it is lost, of which 2^15 make half a rounding of the output.  binary32 sums of bfloat16 ones and
+    // values hold 24 bits for values from 2^-78 up, and are finite for the largest as the probabilities of a row's two
+    // lanes stay below 1/2.  So a reference moves where scores grow by 2^14 (2^17 and more; codes: 2^kCodesGrow).
+    // 2 x 4096 x 4096, 16 heads of 72, float16, scores of 4 nats' standard deviation: 221 us with 1, 226 with 2^2, 236
+    // with 2^4, 243 with 2^6.
     constexpr float kAbove = T == CHAM_T_F16 ? -2.0f : 24.0f;
     constexpr float kBig = SRC == kCodes ? 0x1p20f : T == CHAM_T_F16 ? 61440.0f : 0.25f;
 
     // One step's keys against the wavefront's rows; masked: some row does not see all of them.  The
     // outputs' sums are touched in three places only, whatever branch made the probabilities, so that they
     // stay in their registers.
-    const auto compute = [&](bool masked, bool bad, int step, int buf, const Lds* keys, const Lds* vals, Lds* next_k, Lds* next_v) __attribute__((always_inline)) {
+    const auto compute = [&](bool masked, bool bad, int step, int buf, const Lds* keys, const Lds* vals, Lds* next_k,
+                             Lds* next_v) __attribute__((always_inline)) {
         const int key0 = step * kKeysTile;
         const Lds *kb = keys + k_at, *vb = vals + v_at;
         // the scores of 32 keys; element i: key 32 b + 8 (i / 4) + 4 h + i % 4
@@ -550,9 +552,10 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
                         }
                     }
                     uint32_t lo = narrow<VT>(e[0], e[1]), hi = narrow<VT>(e[2], e[3]);
-                    if constexpr (SRC == kCodes) asm("" : "+v"(lo), "+v"(hi));  // or each is rounded twice, for `most` too
+                    if constexpr (SRC == kCodes) asm("" : "+v"(lo), "+v"(hi));  // or the compiler rounds each once more, for `most`
+                    const ushort2v l2 = __builtin_bit_cast(ushort2v, lo), h2 = __builtin_bit_cast(ushort2v, hi);
                     if constexpr (SRC != kCodes) sum[0] = add2<T>(hi, add2<T>(lo, sum[0]));
-                    else most = __builtin_elementwise_max(most, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, lo), __builtin_bit_cast(ushort2v, hi)));
+                    else most = __builtin_elementwise_max(most, __builtin_elementwise_max(l2, h2));
                     pr[2 * b + i / 8][i % 8 / 2] = lo;
                     pr[2 * b + i / 8][i % 8 / 2 + 1] = hi;
                 }
@@ -766,7 +769,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const AttnArgs a) {
 // wait for the others: keys go from memory into the products' operand as they lie (a lane's 16 bytes
 // of a row are a run of D, which only fixes the order of the sum), values through the wavefront's own
 // LDS for the transposing read; the next 32 keys' loads are under way meanwhile.  At the end
-// they join through LDS.  48 sequences of 200000 tokens, 8 key heads of 128, E4M3 pages of 64: 88 us, 4.8 TB/s
+// they join through LDS.  48 sequences of 200000 tokens, 8 key heads of 128, E4M3 pages of 64: 87 us, 4.8 TB/s
 // (a copy reaches 5.1), and 7.6 for the join; 16-bit pages of one sequence of 700 tokens: 12.3, three steps of
 // memory latency, 1.7 each, and 7 before and behind them.
 template <int ND, int SRC, int NW>
@@ -909,7 +912,7 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
                     e[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.c2, -m));
                     if constexpr (SRC == kCodes) {
                         w[t][i] = e[t][i] * vs[t][i] * by;
-                        most = fmaxf(most, w[t][i]);
+                        most = fmaxf(most, fabsf(w[t][i]));
                     }
                 }
             return most;
@@ -1044,7 +1047,7 @@ __global__ __launch_bounds__(64 * NW, 2) void few_kernel(const AttnArgs a) {
 // joining the pieces of a row tile: o = sum_c w_c o_c / sum_c w_c, w_c = l_c 2^(m_c - max m)
 // ------------------------------------------------------------------------------------
 // A workgroup takes 8 rows, 32 lanes a row (4 elements a lane); where a tile has fewer, several groups of
-// lanes share a row's pieces and are added in their order.  24 us for 1044 pieces of 128 rows of 128 (68 MB);
+// lanes share a row's pieces and are added in their order.  23 us for 1044 pieces of 128 rows of 128 (68 MB);
 // one workgroup a tile took 90 for half of them.
 constexpr int kRowsJoin = 8;
 template <int T, int SRC, int BM, int BN>
@@ -1071,7 +1074,9 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
             const float2 s = *(const float2*)(a.part_s + (at + c * stride) * 2);
             top = s.y != 0.0f ? fmaxf(top, s.x) : top;
         }
-        const auto weight = [&](float2 s) { return s.y == 0.0f ? 0.0f : s.y * __builtin_amdgcn_exp2f(s.x - top); };  // 0: saw no key
+        const auto weight = [&](float2 s) {
+            return s.y == 0.0f ? 0.0f : s.y * __builtin_amdgcn_exp2f(s.x - top);  // 0: saw no key, its output is 0
+        };
 #pragma unroll 4
         for (int c = part; c < p.pieces; c += parts) total += weight(*(const float2*)(a.part_s + (at + c * stride) * 2));
         const float f = total == 0.0f ? 0.0f : 1.0f / total;
@@ -1087,7 +1092,9 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
         __syncthreads();
         if (part > 0) return;
         for (int c = 0; c < parts; ++c) top = fmaxf(top, stats[row + (c << shift)].x);
-        const auto weight = [&](float2 s) { return s.x == top || s.y != s.y ? s.y : s.y == 0.0f ? 0.0f : s.y * __builtin_amdgcn_exp2f(s.x - top); };
+        const auto weight = [&](float2 s) {
+            return s.x == top || s.y != s.y ? s.y : s.y == 0.0f ? 0.0f : s.y * __builtin_amdgcn_exp2f(s.x - top);
+        };
         total = 0.0f;
         for (int c = 0; c < parts; ++c) total += weight(stats[row + (c << shift)]);
         const float f = total == 0.0f ? 0.0f : 1.0f / total;
@@ -1111,9 +1118,9 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
 bool few_rows(const cham_attn* a) { return !a->cu_q && a->T == a->B; }
 
 // Pieces the work is cut into: four for each CU, of which two (three of the single-token kernel) run at once.
-// 1100 new tokens over 36000 cached: 350 us with two, 304 with four, 310 with six; single tokens 88 with two to
-// eight.
-int slots_of(bool few) { return cham_device_cus() * 4; }
+// 1100 new tokens over 36000 cached, two draws: 319 and 335 us a call with two, 294 and 311 with four, 304 and 320 with
+// six; 48 single tokens over 200000 95, 97 and 93.
+int slots() { return cham_device_cus() * 4; }
 
 struct Space {
     int64_t pieces, rows, bytes;
@@ -1122,7 +1129,7 @@ struct Space {
 // work would make: all together at most 2 slots.
 Space space(const cham_attn* a, bool few) {
     Space s;
-    s.pieces = 2 * (int64_t)slots_of(few);
+    s.pieces = 2 * (int64_t)slots();
     s.rows = few ? kRowsFew : kRowsTile;
     s.bytes = s.pieces * s.rows * (a->D + 2) * 4;
     return s;
@@ -1148,21 +1155,24 @@ int attn_check(const cham_attn* a, int32_t Hk) {
 // Grid of the pieces: every tile is a piece, and the cuts make at most `slots` more.
 template <int T, int SRC, int KS, int DB, int ND>
 int launch(AttnArgs& a, bool few, int64_t tiles, bool may_split, hipStream_t s) {
-    const int64_t all = tiles * a.Hk, grid = may_split ? all + slots_of(few) : all;
-    if (!cham_launchable(may_split ? std::max(grid, all * (few ? kRowsFew : kRowsTile) / kRowsJoin) : grid, few && !may_split ? 512 : 256)) return CHAM_ESHAPE;
+    const int64_t all = tiles * a.Hk, grid = may_split ? all + slots() : all;
+    const int64_t most = may_split ? std::max(grid, all * (few ? kRowsFew : kRowsTile) / kRowsJoin) : grid;
+    if (!cham_launchable(most, few && !may_split ? 512 : 256)) return CHAM_ESHAPE;
     if constexpr (SRC != kPacked) {
         if (few) {
             if (may_split) hipLaunchKernelGGL((few_kernel<T, ND, SRC, 4>), dim3((unsigned)grid), dim3(256), 0, s, a);
             else hipLaunchKernelGGL((few_kernel<T, ND, SRC, 8>), dim3((unsigned)grid), dim3(512), 0, s, a);
             CHAM_CHECK_LAUNCH();
-            if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsFew, kKeysFew>), dim3((unsigned)all, a.G > kRowsJoin ? kRowsFew / kRowsJoin : 1), dim3(256), 0, s, a);
+            const dim3 join((unsigned)all, a.G > kRowsJoin ? kRowsFew / kRowsJoin : 1);
+            if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsFew, kKeysFew>), join, dim3(256), 0, s, a);
             CHAM_CHECK_LAUNCH();
             return CHAM_OK;
         }
     }
     hipLaunchKernelGGL((tile_kernel<T, KS, DB, SRC>), dim3((unsigned)grid), dim3(256), 0, s, a);
     CHAM_CHECK_LAUNCH();
-    if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsTile, kKeysTile>), dim3((unsigned)all, kRowsTile / kRowsJoin), dim3(256), 0, s, a);
+    const dim3 join((unsigned)all, kRowsTile / kRowsJoin);
+    if (may_split) hipLaunchKernelGGL((join_kernel<T, SRC, kRowsTile, kKeysTile>), join, dim3(256), 0, s, a);
     CHAM_CHECK_LAUNCH();
     return CHAM_OK;
 }
@@ -1187,7 +1197,7 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     a.G = a.a.q.H / a.Hk;
     a.nq = (int)(a.a.T / a.a.B);
     a.c2 = a.a.scale * kLog2e;
-    a.share = (float)a.Hk / (float)slots_of(few) * 1.001f;
+    a.share = (float)a.Hk / (float)slots() * 1.001f;
     int l = 0;
     while ((1 << l) < a.G) ++l;
     a.group_shift = 31 + l;
@@ -1202,13 +1212,13 @@ int attend(AttnArgs& a, int64_t nk_most, void* ws, size_t ws_bytes, hipStream_t 
     // Tiles that fill the card twice are not cut: the long ones start first, and what a cut saves at the end is
     // less than the partial outputs and the second launch cost (8101 tokens, 2056 tiles: 44 us with nothing
     // to join).  A cache's sequences may be far longer than others: theirs are cut up to four times as many.
-    if (!few && a.a.T * a.G / BM * a.Hk >= (int64_t)slots_of(few) * (SRC == kPacked ? 1 : 4)) may_split = false;
+    if (!few && a.a.T * a.G / BM * a.Hk >= (int64_t)slots() * (SRC == kPacked ? 1 : 4)) may_split = false;
     // Up to 1024 keys are one piece, of eight wavefronts: a step of theirs takes about 1.7 us, a second launch
     // 4 and 3 more on the host (one sequence of 700 tokens, 8 key heads, 16-bit pages of 16: 12.3 us, in pieces
-    // 7.2 and 4.2).
+    // 7.2 and 4.2, which is less only where a graph spares the host).
     if (few && blocks <= CHAM_ATTN_NO_WS_ONE / kKeysFew) may_split = false;
     if (SRC == kPacked && !a.a.cu_q && !a.cu_k)  // every length is known here
-        may_split = may_split && blocks > up(tiles * blocks * a.Hk, slots_of(few));
+        may_split = may_split && blocks > up(tiles * blocks * a.Hk, slots());
     if (!may_split) a.least = kNever;  // the device is to find the same
     if (may_split && (!ws || (uintptr_t)ws % 256 != 0 || ws_bytes < (size_t)sp.bytes)) return CHAM_EWORKSPACE;
     if (a.a.q.type == CHAM_T_F16) return launch_d<CHAM_T_F16, SRC>(a, few, tiles, may_split, s);

@@ -8,8 +8,8 @@
 // once, in LDS.  A group of lanes stays with one head of those tokens, so that addresses, weights and the
 // branch by kind are worked out once, and has four tokens' loads under way.
 //
-// bfloat16, 8192 x 32 heads of 72, 48 elements turned: 22.9 us, 3.3 TB/s (7 of 16 lanes hold nothing at 72;
-// with one vector at a time and a division for each 32, with sums in binary64 36); 8100 x 8 heads of 128
+// bfloat16, 8192 x 32 heads of 72, 48 elements turned: 22.3 us, 3.4 TB/s (with one vector at a time and a division
+// for each 32, with sums in binary64 36; 2 % of it leave what lies behind R untouched); 8100 x 8 heads of 128
 // into E4M3 pages 13.8, 3.6 TB/s; 30001 tokens of 8 heads of 128 out of them 43, 4.3 TB/s (a copy reaches
 // 5.1).  One token of 40 heads: 3.8, a launch and the angle's chain.
 #include <algorithm>
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const RowsArgs a) {
                             q32 = q32 * __builtin_fmaf(-0.5f * s * q32, q32, 1.5f);
                             wide = !(s > 0x1p-60f && s < 0x1p+100f);
                         }
-                            if (wide) {
+                        if (wide) {
                             double s = 0.0;
 #pragma unroll
                             for (int j = 0; j < kChunk; ++j) s = __builtin_fma((double)y[j], (double)y[j], s);
